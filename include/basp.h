@@ -24,6 +24,11 @@
  *                  own shard <-> one contiguous block per member
  *   basp_a2a_pack_bf16  the send side for an fp32 tensor, cast to bf16
  *   basp_attn_bwd_noalloc  the backward with a static device workspace
+ *   basp_qk_norm_rope / basp_qk_norm_rope_bwd   RMS norm of every query and
+ *                  key head and the position rotation, and their gradients
+ *   basp_kv_write / basp_kv_read   the rank's K and V into the pages of a
+ *                  key-value cache (bf16, or 8 bits with a scale), and back
+ *   basp_attn_decode   attention of one new token per sequence over the pages
  *
  * The exchange itself (RCCL) is not part of this library.
  *
@@ -83,12 +88,15 @@ typedef enum basp_status {
   BASP_ERR_DP_FALLBACK = 8  /* micro-batch larger than the world (plain DP)  */
 } basp_status;
 
-/* Element type of a permuted tensor.  Values other than the two listed are
- * rejected with BASP_ERR_UNSUPPORTED (the last two enumerators only make the
- * type span every int, so that any int a caller passes is representable). */
+/* Element type of a tensor.  The permutations take BASP_BF16 and BASP_F32, the
+ * pages of a key-value cache are BASP_BF16 or BASP_E4M3 (8 bits, the OCP format
+ * with 4 exponent and 3 mantissa bits); other values are rejected with
+ * BASP_ERR_UNSUPPORTED (the last two enumerators only make the type span every
+ * int, so that any int a caller passes is representable). */
 typedef enum basp_dtype {
   BASP_BF16 = 0,
   BASP_F32 = 1,
+  BASP_E4M3 = 2,
   BASP_DTYPE_INT_MAX_ = 0x7fffffff,
   BASP_DTYPE_INT_MIN_ = -0x7fffffff - 1
 } basp_dtype;
@@ -370,6 +378,155 @@ int basp_attn_bwd_sharded(const void *const *q_shards,
                           void *workspace, size_t workspace_bytes, int b,
                           int S, int H, int H_kv, int d, int G, int rank,
                           float scale, void *stream);
+
+/* ------------------------------------------- norm and rotation of Q and K
+ *
+ * Between the projections and attention many models normalise every query and
+ * key head over its d elements (RMS norm with a learned weight) and rotate
+ * pairs of elements by an angle that grows with the token's position.  Both
+ * are per token and head, so they commute with the head exchange of Sec. II-C
+ * (a permutation of whole heads): a program calls this on its sequence shard,
+ * all heads, before the exchange (n_q = H, n_k = H_kv, pos0 = the shard's first
+ * token), or on the rank's head-sharded tensors after it (n_q = H/G,
+ * n_k = Hkl, pos0 = 0), with the same result. */
+
+/* For every row x of q (weight qw) and k (weight kw), a token's d elements of a head:
+ *   n = x * w / sqrt(mean(x^2) + eps)            (n = x without weights)
+ *   y[a] = n[a] cos[p][i] - n[b] sin[p][i],  y[b] = n[b] cos[p][i] + n[a] sin[p][i]
+ * for i < rot/2 and p the token's position; the pair (a, b) is (i, i + rot/2),
+ * or (2i, 2i + 1) when interleaved; elements from rot on are n.
+ * q [b, S, n_q, d], k [b, S, n_k, d] in dtype (bf16, rounded once at the end, or
+ * fp32); tokens are q_row (k_row) elements apart, b*S of them in one run, so q
+ * and k may be columns of one projection's output (q_row >= n_q*d).  qo and ko
+ * likewise, tokens qo_row (ko_row) apart; qo may be q itself when the row
+ * strides agree, and ko k; else outputs must not overlap inputs.
+ * qw, kw: fp32 [d]; both NULL: no norm.  cos, sin: fp32 [table_rows, rot/2];
+ * both NULL with rot = 0: no rotation.
+ * positions: int32 [b, S], or NULL for pos0 + t (t the token's index in its
+ * sequence).  A negative position marks a row of padding: its outputs are
+ * zeros.  A position of table_rows or more gives NaN.
+ * Alignment: q, k, qo, ko and their row strides to 4 elements; weights and
+ * tables 16 bytes; positions 4.
+ * Head dims 64, 80, 96 and 128; rot a multiple of 8, 0 <= rot <= d.
+ * Errors: NULL (a pointer, or one weight or table without the other), SHAPE
+ * (negative size, rot as above, q_row < n_q*d, pos0 < 0, or pos0 + S >
+ * table_rows without positions), UNSUPPORTED (d, dtype, eps negative or not
+ * finite, b*S*n_q or b*S*n_k >= 2^29), ALIGN, HIP. */
+int basp_qk_norm_rope(const void *q, const void *k, void *qo, void *ko, const float *qw,
+                      const float *kw, const float *cos, const float *sin,
+                      const int *positions, int b, int S, int n_q, int n_k, int d, int rot,
+                      int table_rows, long long q_row, long long k_row, long long qo_row,
+                      long long ko_row, float eps, int pos0, int interleaved,
+                      basp_dtype dtype, void *stream);
+
+/* Bytes of device workspace basp_qk_norm_rope_bwd needs for the weights'
+ * gradients (partial sums of dqw and dkw per workgroup).  0 for an invalid or
+ * empty shape. */
+size_t basp_qk_norm_rope_bwd_workspace_bytes(int b, int S, int n_q, int n_k, int d);
+
+/* Backward of basp_qk_norm_rope.  With z the rotation's transpose applied to
+ * dy, r = 1/sqrt(mean(x^2) + eps) and g = z w:
+ *   dw = sum over b, S and heads of z x r,   dx = r (g - x r^2 mean(g x))
+ * (dx = z without weights).  q, k: the forward's inputs, as there (not read, and
+ * may be NULL, without weights).  dqo, dko: gradients of its outputs; dq, dk:
+ * gradients of q and k, all in grad_dtype (fp32, as basp_attn_bwd gives them, or
+ * bf16, rounded once at the end) and contiguous ([b, S, n_q, d], [b, S, n_k, d]).
+ * dq may be dqo itself, and dk dko.  dqw, dkw: fp32 [d], fully overwritten.
+ * When a kv head is shared by several members (H_kv < G) dko is a member's part
+ * of that head's gradient, and dk and dkw are its parts of theirs: the map is
+ * linear in dko.  Rows of padding (negative position) have zero gradients and
+ * add nothing to dqw, dkw; a position past the table gives NaN in both.
+ * Sums are taken in fp32 in a fixed order: results are deterministic.
+ * workspace: basp_qk_norm_rope_bwd_workspace_bytes(), 16-byte aligned, contents
+ * ignored on entry (not read, and may be NULL, without weights).  Alignment as
+ * there; dqw, dkw 4 bytes.  Empty (b == 0 or S == 0): dqw, dkw are left as they
+ * were.  Errors: as there, plus WORKSPACE. */
+int basp_qk_norm_rope_bwd(const void *q, const void *k, const void *dqo, const void *dko,
+                          void *dq, void *dk, const float *qw, const float *kw, float *dqw,
+                          float *dkw, const float *cos, const float *sin,
+                          const int *positions, void *workspace, size_t workspace_bytes,
+                          int b, int S, int n_q, int n_k, int d, int rot, int table_rows,
+                          long long q_row, long long k_row, float eps, int pos0,
+                          int interleaved, basp_dtype dtype, basp_dtype grad_dtype,
+                          void *stream);
+
+/* -------------------------------------------------------- key-value cache
+ *
+ * A rank that holds head-sharded K and V of a whole sequence (Sec. II-C) can go
+ * on to generate tokens from it: each new token attends to all before it, on
+ * the rank's own heads.  Their K and V live in pages of `page` tokens:
+ *   k_pages, v_pages  [n_pages, n_k, page, d]  in cache_dtype (BF16 or E4M3)
+ *   k_scales, v_scales  [n_pages, n_k, page] bytes (E4M3 only; else NULL)
+ *   block_table       int32 [b, max_pages]: token t of sequence s is row
+ *                     t % page of page block_table[s][t / page]
+ * Pages may stand in several places of the table (a shared prompt) as long as
+ * no call writes one of their tokens twice.  In E4M3 a row (one token of one
+ * head) is held as x = v * 2^e: e is the least whole number, -110 or more, for
+ * which the row's largest finite magnitude is at most 448 * 2^e, the scale byte
+ * is e + 127, and v is x * 2^-e rounded to nearest even, so a value is off by at
+ * most 2^-4 of itself, or 2^-10 * 2^e where it is below 2^-6 * 2^e (what would
+ * round to 2^128 is held as 240 * 2^120); infinities and NaN are held as NaN.
+ * Conditions of the three calls: d 64, 80, 96 or 128; page 16, 32, 64, 128 or
+ * 256; n_pages * n_k < 2^31; pages 16-byte aligned, scales 4, block_table and
+ * the other int32 arrays 4.  Page numbers and lengths are read on the device and
+ * checked there against n_pages, max_pages and max_len: no call reads or writes
+ * outside its buffers, whatever they hold.  Errors: NULL, SHAPE (negative size,
+ * or page, n_pages or max_pages < 1), UNSUPPORTED (d, page, cache_dtype, sizes),
+ * ALIGN, HIP; b == 0 enqueues nothing. */
+
+/* Writes K and V (bf16, [b, T, n_k, d], tokens k_row (v_row) elements apart, 16-byte
+ * aligned, strides multiples of 8) of T new tokens per sequence: token t of
+ * sequence s goes to position start[s] + t for t < count[s] (count NULL: T).
+ * A sequence with start[s] < 0 is skipped, and so are tokens whose position is
+ * past the table or whose page number is outside [0, n_pages); every other byte of
+ * the pages and scales stays as it was.  Also SHAPE when k_row < n_k*d, and
+ * UNSUPPORTED when b*T*n_k >= 2^28. */
+int basp_kv_write(const void *k, const void *v, void *k_pages, void *v_pages,
+                  unsigned char *k_scales, unsigned char *v_scales, const int *block_table,
+                  const int *start, const int *count, int b, int T, int n_k, int d, int page,
+                  int n_pages, int max_pages, long long k_row, long long v_row,
+                  basp_dtype cache_dtype, void *stream);
+
+/* Reads positions start[s] .. start[s] + count[s] - 1 of every sequence back
+ * (start NULL: 0, count NULL: T) into k and v (bf16, [b, T, n_k, d], contiguous,
+ * 16-byte aligned).  Rows t >= count[s], and all rows of a sequence with
+ * start[s] < 0, are zeros; rows past the table or on a page number outside
+ * [0, n_pages) are NaN.  UNSUPPORTED when b*T*n_k >= 2^28. */
+int basp_kv_read(const void *k_pages, const void *v_pages, const unsigned char *k_scales,
+                 const unsigned char *v_scales, const int *block_table, const int *start,
+                 const int *count, void *k, void *v, int b, int T, int n_k, int d, int page,
+                 int n_pages, int max_pages, basp_dtype cache_dtype, void *stream);
+
+/* Bytes of device workspace basp_attn_decode needs: partial results of the
+ * splits of a sequence, for lengths up to max_len.  0 for an invalid or empty
+ * shape, and where no sequence is split. */
+size_t basp_attn_decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_len);
+
+/* Attention of one new token per sequence (Sec. II-A for the last row, causal):
+ *   O = sum_{j < lens[s]} softmax_j(scale * q . k_j) v_j,
+ *   LSE = log sum_{j < lens[s]} exp(scale * q . k_j)
+ * over the cached tokens of sequence s (the new token's own K and V written
+ * before, and counted in lens).  q [b, n_q, d] bf16, sequences q_row elements
+ * apart (a multiple of 8, >= n_q*d); n_q a multiple of n_k, query head h takes
+ * kv head h / (n_q/n_k); o [b, n_q, d] bf16 contiguous; lse [b, n_q] fp32
+ * natural logarithm (NULL: not wanted).  lens: int32 [b].  A length of 0 (or
+ * less) gives O = 0 and LSE = -inf (a slot of a padded batch); a length above
+ * max_len or max_pages*page, or a page number outside [0, n_pages) among the
+ * pages the length reaches, gives NaN.  max_len: the longest sequence the caller
+ * expects, 1 or more; it sizes the split and the workspace.
+ * Products in bf16 with fp32 accumulation (an 8-bit key or value is exact in
+ * bf16; scales are applied in fp32), softmax in fp32; deterministic.
+ * workspace: basp_attn_decode_workspace_bytes() or more, 16-byte aligned;
+ * contents ignored on entry; calls that may overlap on the device, two captured
+ * graphs among them, need one each.  q and o 16-byte aligned, lse 4.
+ * Also SHAPE when n_q % n_k != 0, UNSUPPORTED when scale is not finite and positive,
+ * b*n_q >= 2^22 or max_len > 2^30, and WORKSPACE. */
+int basp_attn_decode(const void *q, const void *k_pages, const void *v_pages,
+                     const unsigned char *k_scales, const unsigned char *v_scales,
+                     const int *block_table, const int *lens, void *o, float *lse,
+                     void *workspace, size_t workspace_bytes, int b, int n_q, int n_k, int d,
+                     int page, int n_pages, int max_pages, int max_len, long long q_row,
+                     float scale, basp_dtype cache_dtype, void *stream);
 
 #ifdef __cplusplus
 }

@@ -7,7 +7,8 @@ kernels; there is no fallback.  If ``libbasp.so`` has not been built, importing
 the library raises.
 
 Names follow the C ABI: ``pack``, ``unpack``, ``attn_fwd``, ``attn_bwd``,
-``attn_bwd_workspace_bytes``, ``validate``, ``group_of``, ``status_str``.
+``attn_bwd_workspace_bytes``, ``qk_norm_rope``, ``kv_write``, ``attn_decode``,
+``validate``, ``group_of``, ``status_str``.
 """
 from __future__ import annotations
 
@@ -19,7 +20,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbasp.so")
 
-BASP_BF16, BASP_F32 = 0, 1
+BASP_BF16, BASP_F32, BASP_E4M3 = 0, 1, 2
 STATUS = {
     0: "BASP_OK", 1: "BASP_ERR_NULL", 2: "BASP_ERR_SHAPE", 3: "BASP_ERR_RANK",
     4: "BASP_ERR_UNSUPPORTED", 5: "BASP_ERR_ALIGN", 6: "BASP_ERR_WORKSPACE",
@@ -32,7 +33,10 @@ EXPORTS = ("basp_status_str", "basp_group_of", "basp_validate", "basp_pack",
            "basp_a2a_pack_bf16", "basp_attn_fwd",
            "basp_attn_fwd_sharded", "basp_attn_bwd_workspace_bytes", "basp_attn_bwd",
            "basp_attn_bwd_noalloc", "basp_attn_bwd_sharded_workspace_bytes",
-           "basp_attn_bwd_sharded")
+           "basp_attn_bwd_sharded",
+           "basp_qk_norm_rope", "basp_qk_norm_rope_bwd",
+           "basp_qk_norm_rope_bwd_workspace_bytes", "basp_kv_write", "basp_kv_read",
+           "basp_attn_decode", "basp_attn_decode_workspace_bytes")
 # Bytes of the static device buffer basp_attn_bwd_noalloc works in.
 NOALLOC_SCRATCH_BYTES = 128 << 20
 
@@ -82,6 +86,17 @@ def lib() -> ctypes.CDLL:
     L.basp_attn_fwd_sharded.argtypes = [tab] * 4 + [vp] + [i] * 7 + [f, vp]
     L.basp_attn_bwd_sharded.argtypes = ([tab] * 4 + [vp] + [tab] * 4 + [vp, sz] + [i] * 7
                                         + [f, vp])
+    ll = ctypes.c_longlong
+    L.basp_qk_norm_rope.argtypes = [vp] * 9 + [i] * 7 + [ll] * 4 + [f] + [i] * 3 + [vp]
+    L.basp_qk_norm_rope_bwd_workspace_bytes.argtypes = [i] * 5
+    L.basp_qk_norm_rope_bwd_workspace_bytes.restype = sz
+    L.basp_qk_norm_rope_bwd.argtypes = ([vp] * 14 + [sz] + [i] * 7 + [ll] * 2 + [f] + [i] * 4
+                                        + [vp])
+    L.basp_kv_write.argtypes = [vp] * 9 + [i] * 7 + [ll] * 2 + [i, vp]
+    L.basp_kv_read.argtypes = [vp] * 9 + [i] * 8 + [vp]
+    L.basp_attn_decode_workspace_bytes.argtypes = [i] * 5
+    L.basp_attn_decode_workspace_bytes.restype = sz
+    L.basp_attn_decode.argtypes = [vp] * 10 + [sz] + [i] * 8 + [ll, f, i, vp]
     for name in ("basp_group_of", "basp_validate", "basp_pack", "basp_unpack",
                  "basp_a2a_pack", "basp_a2a_unpack", "basp_a2a_pack_bf16", "basp_attn_fwd",
                  "basp_attn_bwd",
@@ -431,3 +446,266 @@ def attn_bwd_sharded(q_shards, k_shards, v_shards, o_shards, lse, do_shards, dq_
         _shards(dv_shards, "dv", f32, G),
         _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(),
         b, S, H, H_kv, d, G, rank, float(scale), _stream(lse)), "basp_attn_bwd_sharded")
+
+
+# --------------------------------------- operators around attention
+# Their tensors have to lie on one device; a call whose device is not the
+# current one makes it current for the launch.
+def _call(name: str, t: torch.Tensor, *args):
+    dev = t.get_device()
+    fn = getattr(lib(), name)
+    if dev == torch._C._cuda_getDevice():
+        rc = fn(*args, _stream(t))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _stream(t))
+    if rc != 0:
+        raise BaspError(rc, name)
+
+
+def _on(t: torch.Tensor, name: str, dtype, shape, like: torch.Tensor) -> int:
+    """Pointer of a contiguous tensor of this type and shape on ``like``'s device."""
+    p = _dev(t, name, dtype)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} and the first tensor are on different devices")
+    return p
+
+
+def _rows(t: torch.Tensor, name: str, dtype, shape, like: torch.Tensor):
+    """(pointer, elements between tokens) of a [..., n, d] tensor whose tokens lie one stride apart
+    and whose heads lie side by side: contiguous, or columns of a wider contiguous tensor."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} and the first tensor are on different devices")
+    n, d = shape[-2:]
+    if t.is_contiguous():
+        return t.data_ptr(), n * d
+    st = t.stride()
+    lead = [(s, z) for s, z in zip(st[:-2], shape[:-2]) if z > 1]  # outermost first
+    row = lead[-1][0] if lead else n * d
+    ok = (d == 1 or st[-1] == 1) and (n == 1 or st[-2] == d) and row >= n * d
+    want = row
+    for s, z in reversed(lead):
+        ok = ok and s == want
+        want = s * z
+    if not ok and t.numel():
+        raise ValueError(f"{name} must have its heads side by side and its tokens one stride apart")
+    return t.data_ptr(), row
+
+
+def _opt(t, name: str, dtype, shape, like):
+    return None if t is None else _on(t, name, dtype, shape, like)
+
+
+def _norm_args(q, k, q_weight, k_weight, cos, sin, positions):
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be [b, S, n_q, d]")
+    if not isinstance(k, torch.Tensor) or k.dim() != 4 or (k.shape[0], k.shape[1], k.shape[3]) != (
+            q.shape[0], q.shape[1], q.shape[3]):
+        raise ValueError("q and k disagree in shape")
+    b, S, n_q, d = q.shape
+    f32 = torch.float32
+    if (cos is None) != (sin is None) or (q_weight is None) != (k_weight is None):
+        raise ValueError("cos and sin, and q_weight and k_weight, go together")
+    if cos is not None and (not isinstance(cos, torch.Tensor) or cos.dim() != 2):
+        raise ValueError("cos and sin must be [positions, rot/2]")
+    table_rows, half = (0, 0) if cos is None else cos.shape
+    if half == 0:  # no columns: nothing is rotated
+        cos = sin = None
+    tail = (_opt(q_weight, "q_weight", f32, (d,), q), _opt(k_weight, "k_weight", f32, (d,), q))
+    turn = (_opt(cos, "cos", f32, (table_rows, half), q),
+            _opt(sin, "sin", f32, (table_rows, half), q),
+            _opt(positions, "positions", torch.int32, (b, S), q))
+    return (b, S, n_q, k.shape[2], d, 2 * half, table_rows), tail, turn
+
+
+def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, eps: float = 1e-6, positions=None,
+                 pos0: int = 0, interleaved: bool = False, q_out=None, k_out=None):
+    """RMS norm of every query and key head, and the position rotation, in one pass.
+
+    ``q`` [b, S, n_q, d], ``k`` [b, S, n_k, d] bf16 or fp32 (columns of a fused projection's output
+    will do); weights fp32 [d], or both None for no norm; ``cos``, ``sin`` fp32 [positions, rot/2]
+    (``rope_table`` makes them), or both None for no rotation.  A token's position is
+    ``positions`` int32 [b, S] (negative: a row of padding, zeros out), or pos0 + its index.
+    Returns (q_out, k_out) in q's type."""
+    (b, S, n_q, n_k, d, rot, rows), w, turn = _norm_args(q, k, q_weight, k_weight, cos, sin,
+                                                         positions)
+    dt = q.dtype
+    code = _dtype_code(q)
+    if q_out is None:
+        q_out = torch.empty((b, S, n_q, d), dtype=dt, device=q.device)
+    if k_out is None:
+        k_out = torch.empty((b, S, n_k, d), dtype=dt, device=q.device)
+    qp, q_row = _rows(q, "q", dt, q.shape, q)
+    kp, k_row = _rows(k, "k", dt, k.shape, q)
+    qop, qo_row = _rows(q_out, "q_out", dt, q.shape, q)
+    kop, ko_row = _rows(k_out, "k_out", dt, k.shape, q)
+    _call("basp_qk_norm_rope", q, qp, kp, qop, kop, *w, *turn, b, S, n_q, n_k, d, rot, rows, q_row,
+          k_row, qo_row, ko_row, eps, pos0, interleaved, code)
+    return q_out, k_out
+
+
+def qk_norm_rope_bwd_workspace_bytes(b, S, n_q, n_k, d) -> int:
+    return int(lib().basp_qk_norm_rope_bwd_workspace_bytes(b, S, n_q, n_k, d))
+
+
+def qk_norm_rope_bwd(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, eps: float = 1e-6,
+                     positions=None, pos0: int = 0, interleaved: bool = False, dq=None, dk=None,
+                     dq_weight=None, dk_weight=None, workspace=None):
+    """Backward of qk_norm_rope at its inputs ``q``, ``k``: from the gradients of its outputs (fp32
+    or bf16, contiguous) to (dq, dk, dq_weight, dk_weight): dq, dk in the gradients' type (``dq``
+    may be ``dq_out`` itself, ``dk`` ``dk_out``), the weights' in fp32 (None without weights)."""
+    (b, S, n_q, n_k, d, rot, rows), w, turn = _norm_args(q, k, q_weight, k_weight, cos, sin,
+                                                         positions)
+    code = _dtype_code(q)
+    gt, gcode = dq_out.dtype, _dtype_code(dq_out)
+    if dq is None:
+        dq = torch.empty((b, S, n_q, d), dtype=gt, device=q.device)
+    if dk is None:
+        dk = torch.empty((b, S, n_k, d), dtype=gt, device=q.device)
+    if q_weight is None:
+        dq_weight = dk_weight = workspace = None
+    else:
+        if dq_weight is None:
+            dq_weight = torch.empty(d, dtype=torch.float32, device=q.device)
+        if dk_weight is None:
+            dk_weight = torch.empty(d, dtype=torch.float32, device=q.device)
+        if b * S == 0:
+            dq_weight.zero_()
+            dk_weight.zero_()
+        if workspace is None:
+            need = qk_norm_rope_bwd_workspace_bytes(b, S, n_q, n_k, d)
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    qp, q_row = _rows(q, "q", q.dtype, q.shape, q)
+    kp, k_row = _rows(k, "k", q.dtype, k.shape, q)
+    f32 = torch.float32
+    _call("basp_qk_norm_rope_bwd", q, qp, kp, _on(dq_out, "dq_out", gt, q.shape, q),
+          _on(dk_out, "dk_out", gt, k.shape, q), _on(dq, "dq", gt, q.shape, q),
+          _on(dk, "dk", gt, k.shape, q), *w, _opt(dq_weight, "dq_weight", f32, (d,), q),
+          _opt(dk_weight, "dk_weight", f32, (d,), q), *turn, *_space(workspace, q), b, S, n_q,
+          n_k, d, rot, rows, q_row, k_row, eps, pos0, interleaved, code, gcode)
+    return dq, dk, dq_weight, dk_weight
+
+
+def _space(workspace, like):
+    """(pointer, bytes) of a workspace tensor of any type, or of none."""
+    if workspace is None:
+        return None, 0
+    return (_on(workspace, "workspace", None, workspace.shape, like),
+            workspace.numel() * workspace.element_size())
+
+
+def rope_table(n: int, rot: int, base: float = 10000.0, device="cuda"):
+    """cos, sin fp32 [n, rot/2] of positions 0 .. n-1, angle p * base^(-2i/rot), formed in 64 bits
+    (an fp32 angle is off by 2^-8 at a position of 128K)."""
+    freq = base ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=device) / rot)
+    ang = torch.arange(n, dtype=torch.float64, device=device)[:, None] * freq
+    return ang.cos().float(), ang.sin().float()
+
+
+# --------------------------------------------------------- key-value cache
+def _pages(k_pages, v_pages, k_scales, v_scales, table, like):
+    """((k_pages, v_pages, k_scales, v_scales, table) pointers, (n_k, d, page, n_pages, max_pages),
+    dtype code) of a paged cache."""
+    if not isinstance(k_pages, torch.Tensor) or k_pages.dim() != 4:
+        raise ValueError("k_pages must be [n_pages, n_k, page, d]")
+    n_pages, n_k, page, d = shape = k_pages.shape
+    dt = k_pages.dtype
+    if dt == torch.bfloat16:
+        code = BASP_BF16
+    elif dt == torch.float8_e4m3fn:
+        code = BASP_E4M3
+    else:
+        raise TypeError(f"unsupported dtype {dt}")
+    if (k_scales is None) != (dt == torch.bfloat16) or (v_scales is None) != (k_scales is None):
+        raise ValueError("an 8-bit cache has k_scales and v_scales, a bf16 cache neither")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("block_table must be [b, max_pages]")
+    u8 = torch.uint8
+    ptrs = (_on(k_pages, "k_pages", dt, shape, like), _on(v_pages, "v_pages", dt, shape, like),
+            _opt(k_scales, "k_scales", u8, shape[:3], like),
+            _opt(v_scales, "v_scales", u8, shape[:3], like),
+            _on(table, "block_table", torch.int32, table.shape, like))
+    return ptrs, (n_k, d, page, n_pages, table.shape[1]), code
+
+
+def kv_write(k, v, k_pages, v_pages, block_table, start, count=None, k_scales=None,
+             v_scales=None):
+    """Write K, V [b, T, n_k, d] bf16 (columns of a fused projection's output will do) of T new tokens
+    per sequence into the pages [n_pages, n_k, page, d] of a cache, bf16 or e4m3 (then with
+    scale bytes [n_pages, n_k, page]): token t of sequence s at position start[s] + t, for
+    t < count[s] (count None: all T).  Sequences with a negative start are skipped."""
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError("k must be [b, T, n_k, d]")
+    b, T = k.shape[:2]
+    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, k)
+    if k.shape[2:] != (dims[0], dims[1]) or block_table.shape[0] != b:
+        raise ValueError("k, the pages and block_table disagree in shape")
+    kp, k_row = _rows(k, "k", torch.bfloat16, k.shape, k)
+    vp, v_row = _rows(v, "v", torch.bfloat16, k.shape, k)
+    _call("basp_kv_write", k, kp, vp, *ptrs, _on(start, "start", torch.int32, (b,), k),
+          _opt(count, "count", torch.int32, (b,), k), b, T, *dims, k_row, v_row, code)
+
+
+def kv_read(k_pages, v_pages, block_table, T: int, start=None, count=None, k_scales=None,
+            v_scales=None, k=None, v=None):
+    """Positions start[s] .. start[s] + count[s] - 1 of every sequence (start None: from 0, count None:
+    T) out of a paged cache, as (k, v) [b, T, n_k, d] bf16; rows past count[s] are zeros."""
+    like = k_pages
+    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, like)
+    b, shape = block_table.shape[0], (block_table.shape[0], T, dims[0], dims[1])
+    bf = torch.bfloat16
+    if k is None:
+        k = torch.empty(shape, dtype=bf, device=like.device)
+    if v is None:
+        v = torch.empty(shape, dtype=bf, device=like.device)
+    _call("basp_kv_read", like, *ptrs, _opt(start, "start", torch.int32, (b,), like),
+          _opt(count, "count", torch.int32, (b,), like), _on(k, "k", bf, shape, like),
+          _on(v, "v", bf, shape, like), b, T, *dims, code)
+    return k, v
+
+
+def attn_decode_workspace_bytes(b, n_q, n_k, d, max_len) -> int:
+    return int(lib().basp_attn_decode_workspace_bytes(b, n_q, n_k, d, max_len))
+
+
+def attn_decode(q, k_pages, v_pages, block_table, lens, scale: float | None = None,
+                max_len: int | None = None, k_scales=None, v_scales=None, out=None, lse=None,
+                workspace=None):
+    """Attention of one new token per sequence, q [b, n_q, d] bf16, over the first lens[s] tokens of
+    a paged cache (the new token's own K, V written before, and counted): returns (o bf16 [b, n_q,
+    d], lse fp32 [b, n_q]).  A length of 0 gives zeros and -inf.  ``max_len``: the longest sequence
+    expected (default: all the table holds).  Two calls that may overlap on the device, captured
+    graphs among them, need a ``workspace`` each (default: one of its own per call)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be [b, n_q, d]")
+    b, n_q, d = q.shape
+    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, q)
+    n_k, dp, page, n_pages, max_pages = dims
+    if dp != d or block_table.shape[0] != b:
+        raise ValueError("q, the pages and block_table disagree in shape")
+    scale = d ** -0.5 if scale is None else scale
+    if max_len is None:
+        max_len = max_pages * page
+    bf = torch.bfloat16
+    if out is None:
+        out = torch.empty((b, n_q, d), dtype=bf, device=q.device)
+    if lse is None:
+        lse = torch.empty((b, n_q), dtype=torch.float32, device=q.device)
+    if workspace is None:
+        need = attn_decode_workspace_bytes(b, n_q, n_k, d, max_len)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    qp, q_row = _rows(q, "q", bf, q.shape, q)
+    _call("basp_attn_decode", q, qp, *ptrs, _on(lens, "lens", torch.int32, (b,), q),
+          _on(out, "out", bf, q.shape, q), _on(lse, "lse", torch.float32, (b, n_q), q),
+          *_space(workspace, q), b, n_q, n_k, d, page, n_pages, max_pages, max_len, q_row,
+          float(scale), code)
+    return out, lse

@@ -1,0 +1,359 @@
+// basp_norm.hip -- RMS norm of every query and key head and the position
+// rotation in one pass, and its backward.
+//
+// Row x (d elements of one head of one token at position p), weight w:
+//   r = 1/sqrt(mean(x^2) + eps),  n = x r w
+//   y_a = n_a c - n_b s,  y_b = n_b c + n_a s     (c, s: cos, sin of pair (a, b) at p)
+// and with z the transpose of the rotation applied to dy (z_a = dy_a c + dy_b s,
+// z_b = dy_b c - dy_a s) and g = z w:
+//   dw = sum over rows of z x r,   dx = r (g - x r^2 mean(g x)).
+//
+// Both kernels are bound by HBM: every row is read once and written once.  A
+// row is held by d/8 of a group of 16 lanes (8 at d = 64), eight elements a
+// lane, chosen so that both elements of a pair lie in the same lane: four
+// pairs, that is two runs of four elements, rot/2 apart or side by side when
+// the pairs are interleaved.  Each run is one 8-byte (bf16) or 16-byte (fp32)
+// access, and the 16 lanes of a row cover two contiguous stretches of it; the
+// rotation then needs no lane exchange, and a pair's cos and sin are loaded
+// once (16 bytes of each per lane).  Sums over a row are four DPP adds.  All
+// arithmetic is fp32; the one rounding to bf16 is that of the result.
+#include <math.h>
+
+#include "basp_device.hpp"
+#include "basp_ops.hpp"
+
+namespace basp {
+
+namespace {
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true);
+  return x + __builtin_bit_cast(float, y);
+}
+
+// Sum over a group of L = 8 or 16 lanes, in every lane: lanes 1 and 2 away
+// (quad_perm), then the mirrored half row and row, whose lanes hold the other
+// half's sum by then.
+template <int L>
+__device__ __forceinline__ float group_sum(float x) {
+  x = dpp_add<0xB1>(x);
+  x = dpp_add<0x4E>(x);
+  x = dpp_add<0x141>(x);
+  if (L == 16) x = dpp_add<0x140>(x);
+  return x;
+}
+
+// Four elements in fp32.
+__device__ __forceinline__ f32x4 load4(const uint16_t *p) {
+  const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
+  return f32x4{__builtin_bit_cast(float, v.x << 16), __builtin_bit_cast(float, v.x & 0xFFFF0000u),
+               __builtin_bit_cast(float, v.y << 16), __builtin_bit_cast(float, v.y & 0xFFFF0000u)};
+}
+__device__ __forceinline__ f32x4 load4(const float *p) {
+  return *reinterpret_cast<const f32x4 *>(p);
+}
+__device__ __forceinline__ void store4(uint16_t *p, f32x4 v) {
+  *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
+}
+__device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
+
+// The elements of a row that a lane holds: runs [a, a+4) and [b, b+4), and the
+// first of the four pairs (a column of the cos and sin tables), or turns =
+// false where they are not rotated.
+struct LaneCols {
+  int a, b, pair;
+  bool turns;
+};
+template <bool INTER>
+__device__ __forceinline__ LaneCols lane_cols(int m, int rot) {
+  LaneCols c;
+  c.pair = 4 * m;
+  c.turns = c.pair < rot / 2;
+  if (INTER || !c.turns) {
+    // side by side; past the rotated elements both orders are the same
+    c.a = 8 * m;
+    c.b = 8 * m + 4;
+  } else {
+    c.a = c.pair;
+    c.b = c.pair + rot / 2;
+  }
+  return c;
+}
+
+// (a, b) turned by (c, s); the transpose is the turn by (c, -s).
+template <bool INTER>
+__device__ __forceinline__ void turn(f32x4 &a, f32x4 &b, f32x4 c, f32x4 s) {
+  const f32x4 x = a, y = b;
+  if (INTER) {
+    a = f32x4{x.x * c.x - x.y * s.x, x.y * c.x + x.x * s.x, x.z * c.y - x.w * s.y,
+              x.w * c.y + x.z * s.y};
+    b = f32x4{y.x * c.z - y.y * s.z, y.y * c.z + y.x * s.z, y.z * c.w - y.w * s.w,
+              y.w * c.w + y.z * s.w};
+  } else {
+    a = f32x4{x.x * c.x - y.x * s.x, x.y * c.y - y.y * s.y, x.z * c.z - y.z * s.z,
+              x.w * c.w - y.w * s.w};
+    b = f32x4{y.x * c.x + x.x * s.x, y.y * c.y + x.y * s.y, y.z * c.z + x.z * s.z,
+              y.w * c.w + x.w * s.w};
+  }
+}
+
+__device__ __forceinline__ float dot8(f32x4 a, f32x4 b, f32x4 c, f32x4 d) {
+  return a.x * c.x + a.y * c.y + a.z * c.z + a.w * c.w + b.x * d.x + b.y * d.y + b.z * d.z +
+         b.w * d.w;
+}
+
+// Where row `row` of a side lies, and its position (below zero: padding).
+struct RowAt {
+  uint32_t token, head;
+  int pos;
+};
+__device__ __forceinline__ RowAt row_at(const NormArgs &a, const NormSide &s, uint32_t row) {
+  RowAt r;
+  r.token = s.by_n.div(row);
+  r.head = row - r.token * s.n;
+  r.pos = a.positions ? a.positions[r.token]
+                      : a.pos0 + (int)(r.token - a.by_S.div(r.token) * a.S);
+  return r;
+}
+
+constexpr int kThreads = 256;
+
+template <int D>
+constexpr int kLanes = D <= 64 ? 8 : 16;  // lanes per row
+template <int D>
+constexpr int kGroups = kThreads / kLanes<D>;  // rows a workgroup holds at once
+
+constexpr int kU = 4;  // rows in flight per group, forward
+
+template <typename T, int D, bool INTER>
+__global__ __launch_bounds__(kThreads) void norm_rope_kernel(const NormArgs a, uint32_t q_blocks) {
+  constexpr int L = kLanes<D>, R = kGroups<D>;
+  const bool is_k = blockIdx.x >= q_blocks;
+  const NormSide &s = a.side[is_k];
+  const uint32_t blk = blockIdx.x - (is_k ? q_blocks : 0);
+  const int m = threadIdx.x % L;
+  const LaneCols lc = lane_cols<INTER>(m, a.rot);
+  const bool on = 8 * m < D;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f}, one = {1.f, 1.f, 1.f, 1.f};
+  f32x4 wa = one, wb = one;
+  if (s.w && on) wa = load4(s.w + lc.a), wb = load4(s.w + lc.b);
+  const uint32_t row0 = blk * (R * kU) + threadIdx.x / L;
+  f32x4 xa[kU], xb[kU], c[kU], sn[kU];
+  RowAt at[kU];
+#pragma unroll
+  for (int u = 0; u < kU; ++u) {
+    const uint32_t row = row0 + u * R;
+    xa[u] = xb[u] = zero;
+    c[u] = one, sn[u] = zero;
+    at[u].pos = -1;
+    if (row < s.rows && on) {
+      at[u] = row_at(a, s, row);
+      const T *x = static_cast<const T *>(s.x) + (long long)at[u].token * s.x_row +
+                   (size_t)at[u].head * D;
+      xa[u] = load4(x + lc.a);
+      xb[u] = load4(x + lc.b);
+      if (lc.turns && at[u].pos >= 0 && at[u].pos < a.table_rows) {
+        const size_t t = (size_t)at[u].pos * (a.rot / 2) + lc.pair;
+        c[u] = load4(a.cos + t);
+        sn[u] = load4(a.sin + t);
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kU; ++u) {
+    const uint32_t row = row0 + u * R;
+    if (s.w) {
+      const float ss = group_sum<L>(dot8(xa[u], xb[u], xa[u], xb[u]));
+      const float r = rsqrtf(ss * (1.f / D) + a.eps);
+      xa[u] *= r * wa;
+      xb[u] *= r * wb;
+    }
+    if (lc.turns) turn<INTER>(xa[u], xb[u], c[u], sn[u]);
+    if (at[u].pos < 0) xa[u] = xb[u] = zero;
+    if (a.rot > 0 && at[u].pos >= a.table_rows) xa[u] = xb[u] = one * __builtin_nanf("");
+    if (row < s.rows && on) {
+      T *y = static_cast<T *>(s.y) + (long long)at[u].token * s.y_row + (size_t)at[u].head * D;
+      store4(y + lc.a, xa[u]);
+      store4(y + lc.b, xb[u]);
+    }
+  }
+}
+
+// Backward.  A lane's columns are the same in every row it holds, so dw's
+// partial sums stay in its eight registers over all rows of its workgroup
+// (rows blk*R.., a grid stride apart); the workgroup's groups are then added
+// in LDS in a fixed order and written as one row of `partials`.
+template <typename TX, typename TG, int D, bool INTER>
+__global__ __launch_bounds__(kThreads) void norm_rope_bwd_kernel(const NormArgs a,
+                                                                 float *partials,
+                                                                 uint32_t q_blocks) {
+  constexpr int L = kLanes<D>, R = kGroups<D>;
+  const bool is_k = blockIdx.x >= q_blocks;
+  const NormSide &s = a.side[is_k];
+  const uint32_t blk = blockIdx.x - (is_k ? q_blocks : 0);
+  const uint32_t blocks = is_k ? gridDim.x - q_blocks : q_blocks;
+  const int m = threadIdx.x % L;
+  const LaneCols lc = lane_cols<INTER>(m, a.rot);
+  const bool on = 8 * m < D;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f}, one = {1.f, 1.f, 1.f, 1.f};
+  f32x4 wa = one, wb = one;
+  if (s.w && on) wa = load4(s.w + lc.a), wb = load4(s.w + lc.b);
+  f32x4 dwa = zero, dwb = zero;
+  const uint64_t step = (uint64_t)blocks * R;
+  for (uint64_t r0 = (uint64_t)blk * R; r0 < s.rows; r0 += step) {  // workgroup-uniform
+    const uint64_t row = r0 + threadIdx.x / L;
+    f32x4 xa = zero, xb = zero, za = zero, zb = zero;
+    RowAt at;
+    at.pos = -1;
+    if (row < s.rows && on) {
+      at = row_at(a, s, (uint32_t)row);
+      if (at.pos >= 0) {
+        const TG *dy = static_cast<const TG *>(s.dy) + row * D;
+        za = load4(dy + lc.a);
+        zb = load4(dy + lc.b);
+        if (s.w) {
+          const TX *x = static_cast<const TX *>(s.x) + (long long)at.token * s.x_row +
+                        (size_t)at.head * D;
+          xa = load4(x + lc.a);
+          xb = load4(x + lc.b);
+        }
+        if (lc.turns && at.pos < a.table_rows) {
+          const size_t t = (size_t)at.pos * (a.rot / 2) + lc.pair;
+          turn<INTER>(za, zb, load4(a.cos + t), -load4(a.sin + t));
+        }
+        if (a.rot > 0 && at.pos >= a.table_rows) za = zb = one * __builtin_nanf("");
+      }
+    }
+    if (s.w) {
+      const f32x4 ga = za * wa, gb = zb * wb;
+      const float ss = group_sum<L>(dot8(xa, xb, xa, xb));
+      const float gx = group_sum<L>(dot8(ga, gb, xa, xb));
+      const float r = rsqrtf(ss * (1.f / D) + a.eps);
+      const float k = r * r * (gx * (1.f / D));
+      if (at.pos >= 0) {  // a row of padding adds nothing, also where eps = 0
+        dwa += za * (xa * r);
+        dwb += zb * (xb * r);
+        za = r * (ga - xa * k);
+        zb = r * (gb - xb * k);
+      }
+    }
+    if (row < s.rows && on) {
+      TG *dx = static_cast<TG *>(s.y) + row * D;
+      store4(dx + lc.a, za);
+      store4(dx + lc.b, zb);
+    }
+  }
+  if (!s.w) return;
+  __shared__ float part[R][D];
+  if (on) {
+    float *p = part[threadIdx.x / L];
+    store4(p + lc.a, dwa);
+    store4(p + lc.b, dwb);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < D; e += kThreads) {
+    float t = 0.f;
+#pragma unroll
+    for (int g = 0; g < R; ++g) t += part[g][e];
+    partials[(size_t)blockIdx.x * D + e] = t;
+  }
+}
+
+// dw of one side: the sum of its workgroups' partial rows, 16 columns per
+// workgroup, 16 threads a column, each over every 16th row.
+template <int D>
+__global__ __launch_bounds__(kThreads) void norm_dw_kernel(const NormArgs a, const float *partials,
+                                                           uint32_t q_blocks, uint32_t k_blocks) {
+  const bool is_k = blockIdx.y;
+  const uint32_t first = is_k ? q_blocks : 0, n = is_k ? k_blocks : q_blocks;
+  const int col = blockIdx.x * 16 + threadIdx.x % 16, lane = threadIdx.x / 16;
+  float t = 0.f;
+#pragma unroll 8
+  for (uint32_t i = lane; i < n; i += 16) t += partials[(size_t)(first + i) * D + col];
+  __shared__ float part[16][16];
+  part[lane][threadIdx.x % 16] = t;
+  __syncthreads();
+  if (lane == 0) {
+    t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += part[i][threadIdx.x];
+    a.side[is_k].dw[col] = t;
+  }
+}
+
+template <typename T, int D>
+hipError_t fwd_typed(const NormArgs &a, bool interleaved, hipStream_t stream) {
+  const uint64_t per = kGroups<D> * kU;
+  const uint64_t qb = (a.side[0].rows + per - 1) / per, kb = (a.side[1].rows + per - 1) / per;
+  const dim3 grid((unsigned)(qb + kb));
+  if (interleaved)
+    hipLaunchKernelGGL((norm_rope_kernel<T, D, true>), grid, dim3(kThreads), 0, stream, a,
+                       (uint32_t)qb);
+  else
+    hipLaunchKernelGGL((norm_rope_kernel<T, D, false>), grid, dim3(kThreads), 0, stream, a,
+                       (uint32_t)qb);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t fwd_dim(const NormArgs &a, int d, bool interleaved, hipStream_t stream) {
+  switch (d) {
+    case 64: return fwd_typed<T, 64>(a, interleaved, stream);
+    case 80: return fwd_typed<T, 80>(a, interleaved, stream);
+    case 96: return fwd_typed<T, 96>(a, interleaved, stream);
+    default: return fwd_typed<T, 128>(a, interleaved, stream);
+  }
+}
+
+template <typename TX, typename TG, int D>
+hipError_t bwd_typed(const NormArgs &a, float *partials, bool interleaved, hipStream_t stream) {
+  const uint32_t qb = norm_bwd_blocks(a.side[0].rows, D), kb = norm_bwd_blocks(a.side[1].rows, D);
+  if (interleaved)
+    hipLaunchKernelGGL((norm_rope_bwd_kernel<TX, TG, D, true>), dim3(qb + kb), dim3(kThreads), 0,
+                       stream, a, partials, qb);
+  else
+    hipLaunchKernelGGL((norm_rope_bwd_kernel<TX, TG, D, false>), dim3(qb + kb), dim3(kThreads), 0,
+                       stream, a, partials, qb);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.side[0].w) return e;
+  hipLaunchKernelGGL((norm_dw_kernel<D>), dim3(D / 16, 2), dim3(kThreads), 0, stream, a, partials,
+                     qb, kb);
+  return hipGetLastError();
+}
+
+template <typename TX, typename TG>
+hipError_t bwd_dim(const NormArgs &a, float *partials, int d, bool interleaved,
+                   hipStream_t stream) {
+  switch (d) {
+    case 64: return bwd_typed<TX, TG, 64>(a, partials, interleaved, stream);
+    case 80: return bwd_typed<TX, TG, 80>(a, partials, interleaved, stream);
+    case 96: return bwd_typed<TX, TG, 96>(a, partials, interleaved, stream);
+    default: return bwd_typed<TX, TG, 128>(a, partials, interleaved, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_norm_rope(const NormArgs &a, int d, bool interleaved, bool f32,
+                            hipStream_t stream) {
+  return f32 ? fwd_dim<float>(a, d, interleaved, stream)
+             : fwd_dim<uint16_t>(a, d, interleaved, stream);
+}
+
+int norm_bwd_blocks(uint32_t rows, int d) {
+  const uint32_t per = kThreads / (d <= 64 ? 8 : 16);
+  const uint64_t blocks = ((uint64_t)rows + per - 1) / per;
+  return (int)(blocks < 1024 ? blocks : 1024);
+}
+
+hipError_t launch_norm_rope_bwd(const NormArgs &a, float *partials, int d, bool interleaved,
+                                bool f32, bool grad_f32, hipStream_t stream) {
+  if (f32)
+    return grad_f32 ? bwd_dim<float, float>(a, partials, d, interleaved, stream)
+                    : bwd_dim<float, uint16_t>(a, partials, d, interleaved, stream);
+  return grad_f32 ? bwd_dim<uint16_t, float>(a, partials, d, interleaved, stream)
+                  : bwd_dim<uint16_t, uint16_t>(a, partials, d, interleaved, stream);
+}
+
+}  // namespace basp
