@@ -229,12 +229,13 @@ int run_cache(bool write, const void *k, const void *v, const void *k_pages, con
                           : basp::launch_kv_read(a, (hipStream_t)stream));
 }
 
-// Shape rules of basp_attn_decode.  A (sequence, query head) pair is one join
-// workgroup, and its splits are chosen to keep a launch's threads a 32-bit
-// count.
+// Shape rules of basp_attn_decode.  The kernel counts units of 128 keys or more
+// per (sequence, head), and keys up to a unit past a length, in 32 bits.
 int check_decode(int b, int n_q, int n_k, int d, int max_len) {
   if (b < 0 || n_q < 1 || n_k < 1 || d < 1 || max_len < 1 || n_q % n_k != 0) return BASP_ERR_SHAPE;
   if (!head_dim(d) || (uint64_t)b * (uint64_t)n_q >= (1ull << 22) || max_len > (1 << 30))
+    return BASP_ERR_UNSUPPORTED;
+  if ((uint64_t)b * (uint64_t)n_q * (((uint64_t)max_len + 127) / 128) >= (1ull << 31))
     return BASP_ERR_UNSUPPORTED;
   return BASP_OK;
 }
@@ -300,7 +301,7 @@ int basp_attn_decode(const void *q, const void *k_pages, const void *v_pages,
   a.n_q = n_q;
   a.max_len = max_len;
   a.scale = scale;
-  a.workspace = workspace;
+  a.workspace = need > 0 ? workspace : nullptr;
   (void)hipGetLastError();
   return hip_status(basp::launch_attn_decode(a, (hipStream_t)stream));
 }

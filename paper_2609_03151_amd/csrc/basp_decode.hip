@@ -6,10 +6,15 @@
 // operations a byte of bf16 (16 on 8 query heads a kv head), which is more than
 // the vector units do beside such a stream and little for the matrix cores.
 //
-// A workgroup takes one split of a sequence's keys for the (up to 16) query
-// heads of one kv head; its four waves take blocks of 32 keys (64 in 8 bits)
-// in turn, each with a running maximum, sum and O of its own, joined in LDS at
-// the end.  Splits of one sequence are joined by a second kernel:
+// The keys of all sequences are dealt out evenly: a unit is 128 keys (256 in 8
+// bits) of one kv head and up to 16 of its query heads, and each of at
+// most 512 workgroups, two per CU, takes one run of units, in the order of
+// sequences, heads and keys.  The lengths are known on the device only, so each
+// workgroup adds them up to find its run.  Its four waves take a block of 32 (64)
+// keys of each unit, each with a running maximum, sum and O of its own, joined in LDS
+// at the end of a sequence's head or of the run.  Only the first and the last
+// head of a run can be shared with other workgroups; their partial results are
+// joined by a second kernel:
 //   M = max_i m_i,  O = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i
 // (scores in log2 units).
 //
@@ -41,6 +46,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kRows = 16;  // query heads of a workgroup
+constexpr int kCus = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -84,8 +90,7 @@ __device__ __forceinline__ float pow2_of_byte(uint32_t w, int i) {
   return __builtin_bit_cast(float, ((w >> (8 * i)) & 0xFFu) << 23);
 }
 
-// What a wave loads of one block of keys.  W: words of V per key and lane
-// before widening.
+// What a wave loads of one block of keys.
 template <int D, bool E4M3>
 struct Block {
   static constexpr int kElem = E4M3 ? 1 : 2;
@@ -95,7 +100,7 @@ struct Block {
   static constexpr int kLoads = (kRowBytes + 63) / 64;  // of 64 bytes per key
   static constexpr int kSteps = E4M3 ? 2 * kLoads : kLoads;
   static constexpr int kCols = D <= 64 ? 4 : 8;       // elements of d per lane of V
-  static constexpr int kWords = kCols * kElem / 4;
+  static constexpr int kWords = kCols * kElem / 4;    // 32-bit words of V per key and lane
   u32x4 k[kTiles][kLoads];
   uint32_t v[kTiles / 2][8][kWords];
   uint32_t ks[kTiles], vs[kTiles];  // scale bytes of keys 4(l/16)..
@@ -110,6 +115,30 @@ struct Pages {
   int page_log2, n_pages, max_pages, n_k, kvh;
 };
 
+// A wave-uniform value in a scalar register.  The compiler would move address
+// arithmetic that it placed in vector registers (integer division, clamps) back
+// only by a loop over the lanes around every load.
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// A load at a scalar base plus a 32-bit offset per lane.
+typedef const __attribute__((address_space(1))) char *gptr;
+__device__ __forceinline__ gptr scalar_base(const void *p) {
+  const uint64_t a = (uint64_t)(uintptr_t)p;
+  const uint32_t lo = (uint32_t)scalar((int)(uint32_t)a), hi = (uint32_t)scalar((int)(a >> 32));
+  return (gptr)(((uint64_t)hi << 32) | lo);
+}
+template <typename T>
+__device__ __forceinline__ T load_at(gptr base, uint32_t off) {
+  return *(const __attribute__((address_space(1))) T *)(base + off);
+}
+
+// An entry of the block table or of lens: a load through the scalar cache, which
+// the counter that the pages' loads are waited by does not see (nothing writes
+// either while the kernel runs).
+__device__ __forceinline__ int scalar_load(const int *p, size_t i) {
+  return *((const __attribute__((address_space(4))) int *)(uintptr_t)p + i);
+}
+
 // Page numbers of a block's tiles (tiles do not cross pages: both are
 // multiples of 16).
 template <typename B>
@@ -118,57 +147,62 @@ __device__ __forceinline__ void load_ids(const Pages &p, int t0, int hi, int (&i
   for (int t = 0; t < B::kTiles; ++t) {
     const int at = t0 + 16 * t, pi = at >> p.page_log2;
     id[t] = -1;
-    if (at < hi && pi < p.max_pages) id[t] = p.table[pi];
+    if (at < hi && pi < p.max_pages) id[t] = scalar_load(p.table, pi);
   }
 }
 
+// Loads of the block from key t0 on.  Keys from `hi` on read the last row before
+// it instead (take_block drops them), tiles with no key before `hi` or on no valid
+// page the first row of page 0: the loads in flight are the same in every turn,
+// so the compiler can wait for one block's and leave the next one's.
 template <int D, bool E4M3>
 __device__ __forceinline__ void load_block(Block<D, E4M3> &b, const Pages &p, int t0, int hi,
                                            const int (&ids)[Block<D, E4M3>::kTiles]) {
   using B = Block<D, E4M3>;
   const int lane = threadIdx.x % 64, m = lane % 16, c = lane / 16;
-  uint32_t ko[B::kLoads];
-#pragma unroll
-  for (int s = 0; s < B::kLoads; ++s) {
-    const uint32_t at = 64 * s + 16 * c;
-    ko[s] = at < (uint32_t)B::kRowBytes ? m * B::kRowBytes + at : kZeroOffset;
-  }
-  const uint32_t vo = m * B::kCols < D ? 4 * c * B::kRowBytes + m * B::kCols * B::kElem
-                                       : kZeroOffset;
   b.bad = false;
 #pragma unroll
   for (int t = 0; t < B::kTiles; ++t) {
     const int at = t0 + 16 * t;
-    const int id = __builtin_amdgcn_readfirstlane(ids[t]);
+    const int id = scalar(ids[t]);
     const bool there = id >= 0 && id < p.n_pages;
-    int rows = hi - at;
-    rows = rows < 0 ? 0 : rows > 16 ? 16 : rows;
-    if (!there && rows > 0) b.bad = true;
-    if (!there) rows = 0;
-    const size_t row = (((size_t)(there ? id : 0) * p.n_k + p.kvh) << p.page_log2) +
-                       (at & ((1 << p.page_log2) - 1));
-    const rsrc_t kr = make_rsrc(p.k + row * B::kRowBytes, rows * B::kRowBytes);
-    const rsrc_t vr = make_rsrc(p.v + row * B::kRowBytes, rows * B::kRowBytes);
+    if (!there && at < hi) b.bad = true;
+    const uint32_t in_pool = there ? (uint32_t)id * p.n_k + p.kvh : 0;  // n_pages * n_k < 2^31
+    const size_t row = ((size_t)in_pool << p.page_log2) +
+                       (there ? at & ((1 << p.page_log2) - 1) : 0);
+    const int last = scalar(there ? hi - at - 1 : 0);  // 15 or more in a full tile
+    const gptr kb = scalar_base(p.k + row * B::kRowBytes);
+    const gptr vb = scalar_base(p.v + row * B::kRowBytes);
+    const uint32_t kr = (uint32_t)(m < last ? m : last) * B::kRowBytes;
 #pragma unroll
-    for (int s = 0; s < B::kLoads; ++s) b.k[t][s] = buf_load16(kr, ko[s]);
+    for (int s = 0; s < B::kLoads; ++s) {
+      // past a row's end (d = 80, 96; Q is zero there): its first bytes
+      const uint32_t col = 64 * s + 16 * c;
+      if constexpr (B::kRowBytes % 64 == 0)
+        b.k[t][s] = load_at<u32x4>(kb, kr + 16 * c + 64 * s);
+      else
+        b.k[t][s] = load_at<u32x4>(kb, kr + (col < (uint32_t)B::kRowBytes ? col : 0));
+    }
+    // past a row's end: rows of the product that are not stored
+    const uint32_t vc = m * B::kCols < D ? m * B::kCols * B::kElem : 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       uint32_t(&v)[B::kWords] = b.v[t / 2][4 * (t % 2) + e];
-      const uint32_t o = vo + e * B::kRowBytes;
+      const int r = 4 * c + e;
+      const uint32_t o = (uint32_t)(r < last ? r : last) * B::kRowBytes + vc;
       if constexpr (B::kWords == 4) {
-        const u32x4 x = buf_load16(vr, o);
+        const u32x4 x = load_at<u32x4>(vb, o);
         v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
       } else if constexpr (B::kWords == 2) {
-        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(vr, o, 0, 0));
+        const u32x2 x = load_at<u32x2>(vb, o);
         v[0] = x.x, v[1] = x.y;
       } else {
-        v[0] = __builtin_amdgcn_raw_buffer_load_b32(vr, o, 0, 0);
+        v[0] = load_at<uint32_t>(vb, o);
       }
     }
     if constexpr (E4M3) {
-      const uint32_t bytes = rows > 0 ? 16 : 0;
-      b.ks[t] = __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(p.ks + row, bytes), 4 * c, 0, 0);
-      b.vs[t] = __builtin_amdgcn_raw_buffer_load_b32(make_rsrc(p.vs + row, bytes), 4 * c, 0, 0);
+      b.ks[t] = load_at<uint32_t>(scalar_base(p.ks + row), 4 * c);
+      b.vs[t] = load_at<uint32_t>(scalar_base(p.vs + row), 4 * c);
     }
   }
 }
@@ -184,7 +218,7 @@ struct State {
 // Maximum, weights and O of one block.  `left`: keys of the sequence from the
 // block's first on (less than a block only in its last).
 template <int D, bool E4M3>
-__device__ __forceinline__ void take_block(const Block<D, E4M3> &b, State<Block<D, E4M3>> &st,
+__device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M3>> &st,
                                            const bf16x8 (&q)[Block<D, E4M3>::kSteps], float scale2,
                                            int left) {
   using B = Block<D, E4M3>;
@@ -216,7 +250,11 @@ __device__ __forceinline__ void take_block(const Block<D, E4M3> &b, State<Block<
     for (int t = 0; t < B::kTiles; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (16 * t + 4 * c + r >= left) s[t][r] = -INFINITY;
+        if (16 * t + 4 * c + r >= left) {
+          s[t][r] = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < B::kWords; ++w) b.v[t / 2][4 * (t % 2) + r][w] = 0;  // 0 * inf
+        }
   }
   if (b.bad) s[0][0] = __builtin_nanf("");
   float mx = s[0][0];
@@ -271,158 +309,255 @@ __device__ __forceinline__ void take_block(const Block<D, E4M3> &b, State<Block<
   }
 }
 
-// Partial results of split i of (sequence, query head) r, n splits a row:
-// o [rows][n][d] (not divided by l), then (m, l) [rows][n].
-struct Partials {
-  float *o;
-  f32x2 *ml;
+// What a workgroup leaves for the join, in the workspace: for its first (0) and
+// last (1) head, of up to kRows rows, O not divided by l [g][2][kRows][D] and (m, l)
+// [g][2][kRows]; and, of each head that starts in its run, where its partial
+// results lie if it ends past the run: `count` of them (else 0), the first in slot
+// `slot` of workgroup `g`, the others in slot 0 of the next ones.  These are
+// indexed by the head; where there are more heads than workgroups by the
+// workgroup, whose last head alone can end past its run.
+struct Open {
+  int row0, heads, count, first;  // first = 2 g + slot
 };
-__device__ __forceinline__ Partials partials_at(void *ws, size_t rows, int n, int d) {
+struct Partials {
+  Open *open;
+  f32x2 *ml;
+  float *o;
+};
+constexpr size_t kOpenBytes = sizeof(Open), kRowBytesMl = 2 * kRows * sizeof(f32x2);
+__device__ __forceinline__ Partials partials_at(void *ws, int opens, int groups) {
   Partials p;
-  p.o = static_cast<float *>(ws);
-  p.ml = reinterpret_cast<f32x2 *>(p.o + rows * n * d);
+  p.open = static_cast<Open *>(ws);
+  p.ml = reinterpret_cast<f32x2 *>(p.open + opens);
+  p.o = reinterpret_cast<float *>(p.ml + (size_t)groups * 2 * kRows);
   return p;
 }
 
+// Keys of a unit.
+template <typename B>
+constexpr int kUnit = kWaves * B::kKeys;
+
+template <typename B>
+__device__ __forceinline__ int units_of(int len, int max_len) {
+  return len <= 0 || len > max_len ? 0 : (len - 1) / kUnit<B> + 1;
+}
+
+__device__ __forceinline__ int wave_scan(int x) {  // inclusive
+  const int lane = threadIdx.x % 64;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// Workgroups per CU: what the registers allow.
+constexpr int per_cu(int d, bool e4m3) { return d == 64 || (d < 128 && !e4m3) ? 4 : 3; }
+
 template <int D, bool E4M3>
-__global__ __launch_bounds__(kThreads, 2) void decode_split_kernel(const DecodeArgs a,
-                                                                   const DecodeSplit sp) {
+__global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const DecodeArgs a,
+                                                                           int opens) {
   using B = Block<D, E4M3>;
-  const int rep = a.n_q / a.s.n_k, groups = (rep + kRows - 1) / kRows;
-  int at = blockIdx.x;
-  const int split = at % sp.splits;
-  at /= sp.splits;
-  const int grp = at % groups;
-  at /= groups;
-  const int kvh = at % a.s.n_k, seq = at / a.s.n_k;
-  const int h0 = kvh * rep + grp * kRows;  // first query head
-  const int heads = rep - grp * kRows < kRows ? rep - grp * kRows : kRows;
-  const int len = a.lens[seq], lo = split * sp.keys;
-  const size_t row0 = (size_t)seq * a.n_q + h0;
-  uint16_t *o = static_cast<uint16_t *>(a.o) + row0 * D;
-  if (len <= 0 || len > a.max_len) {  // no keys, or more than the call allows
-    if (split > 0) return;
-    for (int i = threadIdx.x; i < heads * D; i += kThreads) o[i] = len <= 0 ? 0 : 0x7FFF;
-    if (threadIdx.x < heads && a.lse)
-      a.lse[row0 + threadIdx.x] = len <= 0 ? -INFINITY : __builtin_nanf("");
+  const int rep = scalar(a.n_q / a.s.n_k), row_groups = (rep + kRows - 1) / kRows;
+  const int R = scalar(a.s.n_k * row_groups);  // heads, as dealt out, of a sequence
+  const int b = a.s.b, G = gridDim.x, g = blockIdx.x;
+  const int wave = scalar(threadIdx.x / 64);
+  const int lane = threadIdx.x % 64, m = lane % 16, c = lane / 16;
+  __shared__ float so[kWaves][kRows][D + 4], sm[kWaves][kRows], sl[kWaves][kRows];
+  __shared__ int sums[kWaves], found[2];
+
+  const Partials ps = partials_at(a.workspace, opens, G);
+  const bool joins = a.workspace != nullptr, by_head = joins && opens != G;
+
+  // Sequences without keys, or with more than the call allows, are shared out.
+  auto write_empty = [&]() {
+    for (int s = g; s < b; s += G) {
+      const int len = scalar_load(a.lens, s);
+      if (units_of<B>(len, a.max_len) > 0) continue;
+      uint16_t *o = static_cast<uint16_t *>(a.o) + (size_t)s * a.n_q * D;
+      for (int i = threadIdx.x; i < a.n_q * D; i += kThreads) o[i] = len <= 0 ? 0 : 0x7FFF;
+      if (a.lse)
+        for (int i = threadIdx.x; i < a.n_q; i += kThreads)
+          a.lse[(size_t)s * a.n_q + i] = len <= 0 ? -INFINITY : __builtin_nanf("");
+      if (by_head)
+        for (int i = threadIdx.x; i < R; i += kThreads) ps.open[(size_t)s * R + i].count = 0;
+    }
+  };
+
+  // All units, and this workgroup's run [begin, end).
+  const int n0 = (int)threadIdx.x < b ? units_of<B>(a.lens[threadIdx.x], a.max_len) : 0;
+  int mine = n0;
+  for (int s = threadIdx.x + kThreads; s < b; s += kThreads)
+    mine += units_of<B>(a.lens[s], a.max_len);
+  mine = wave_scan(mine);
+  if (lane == 63) sums[wave] = mine;
+  __syncthreads();
+  const int total = scalar(R * (sums[0] + sums[1] + sums[2] + sums[3]));
+  const int quota = scalar((total + G - 1) / G);
+  const long long first = (long long)g * quota;
+  if (first >= total) {
+    if (joins && !by_head && threadIdx.x == 0) ps.open[g].count = 0;
+    write_empty();
     return;
   }
-  if (lo >= len) return;
-  const int hi = len - lo < sp.keys ? len : lo + sp.keys;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int lane = threadIdx.x % 64, m = lane % 16, c = lane / 16;
+  const int begin = (int)first, end = total - begin < quota ? total : begin + quota;
+  // The sequence of unit `begin`: chunks of 256 sequences, each thread one.
+  int base = 0;
+  for (int s0 = 0;; s0 += kThreads) {
+    const int s = s0 + threadIdx.x;
+    int n = n0, x = mine;
+    if (b > kThreads) {  // else the sums above are those of the one chunk
+      __syncthreads();   // sums, read above or in the last turn
+      if (s0 > 0) n = s < b ? units_of<B>(a.lens[s], a.max_len) : 0;
+      x = wave_scan(n);
+      if (lane == 63) sums[wave] = x;
+      __syncthreads();
+    }
+    x += base;
+    for (int w = 0; w < wave; ++w) x += sums[w];
+    if (begin >= R * (x - n) && begin < R * x) found[0] = s, found[1] = begin - R * (x - n);
+    base += sums[0] + sums[1] + sums[2] + sums[3];
+    if (begin < R * base) break;  // some thread of this chunk has found it
+    if (s0 + kThreads >= b) return;  // not reached while lens stays as it is
+  }
+  __syncthreads();
+  int seq = scalar(found[0]);
+  int n = units_of<B>(scalar_load(a.lens, seq), a.max_len);  // units of a head of it
+  int head = scalar(found[1] / n), u = scalar(found[1] % n);
 
   Pages pg;
   pg.k = static_cast<const char *>(a.k_pages);
   pg.v = static_cast<const char *>(a.v_pages);
   pg.ks = a.k_scales;
   pg.vs = a.v_scales;
-  pg.table = a.table + (size_t)seq * a.s.max_pages;
   pg.page_log2 = a.s.page_log2;
   pg.n_pages = a.s.n_pages;
   pg.max_pages = a.s.max_pages;
   pg.n_k = a.s.n_k;
-  pg.kvh = kvh;
-
-  bf16x8 q[B::kSteps];
-  const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (long long)seq * a.q_row +
-                       (size_t)(h0 + m) * D;
-#pragma unroll
-  for (int s = 0; s < B::kSteps; ++s) {
-    const int e = E4M3 ? 64 * (s / 2) + 16 * c + 8 * (s % 2) : 32 * s + 8 * c;
-    u32x4 w = {0, 0, 0, 0};
-    if (m < heads && e < D) w = *reinterpret_cast<const u32x4 *>(qp + e);
-    q[s] = as_bf16x8(w);
-  }
   const float scale2 = a.scale * kLog2e;
+  Open open = {0, 0, 0, 0};
 
-  State<B> st;
-  st.m = -INFINITY;
-  st.l = 0.f;
+  for (int pos = begin; pos < end;) {
+    const int take = n - u < end - pos ? n - u : end - pos;  // units of this head
+    const int len = scalar_load(a.lens, seq);
+    const int lo = u * kUnit<B>;
+    const int hi = (u + take) * kUnit<B> < len ? (u + take) * kUnit<B> : len;
+    const int kvh = scalar(head / row_groups), grp = scalar(head % row_groups);
+    const int h0 = kvh * rep + grp * kRows;  // first query head
+    const int heads = rep - grp * kRows < kRows ? rep - grp * kRows : kRows;
+    pg.table = a.table + (size_t)seq * a.s.max_pages;
+    pg.kvh = kvh;
+
+    // Blocks lo + (4j + wave) * kKeys: the next one's loads are in flight while
+    // one is taken, and the one after's page numbers.
+    int t = lo + wave * B::kKeys;
+    Block<D, E4M3> x;
+    int ids[B::kTiles];
+    load_ids<B>(pg, t, hi, ids);
+    bf16x8 q[B::kSteps];
+    const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (long long)seq * a.q_row +
+                         (size_t)(h0 + m) * D;
 #pragma unroll
-  for (int i = 0; i < B::kCols; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < B::kSteps; ++s) {
+      const int e = E4M3 ? 64 * (s / 2) + 16 * c + 8 * (s % 2) : 32 * s + 8 * c;
+      u32x4 w = {0, 0, 0, 0};
+      if (m < heads && e < D) w = *reinterpret_cast<const u32x4 *>(qp + e);
+      q[s] = as_bf16x8(w);
+    }
+    State<B> st;
+    st.m = -INFINITY;
+    st.l = 0.f;
+#pragma unroll
+    for (int i = 0; i < B::kCols; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    while (t < hi) {
+      load_block<D, E4M3>(x, pg, t, hi, ids);
+      load_ids<B>(pg, t + kUnit<B>, hi, ids);
+      take_block<D, E4M3>(x, st, q, scale2, hi - t);
+      t += kUnit<B>;
+    }
+    st.l = column_sum(st.l);
 
-  // Blocks lo + (4j + wave) * kKeys: the next one's loads are in flight while
-  // one is taken, and the one after's page numbers.
-  constexpr int kStep = kWaves * B::kKeys;
-  int t = lo + wave * B::kKeys;
-  Block<D, E4M3> x, y;
-  int ids[B::kTiles];
-  load_ids<B>(pg, t, hi, ids);
-  load_block<D, E4M3>(x, pg, t, hi, ids);
-  load_ids<B>(pg, t + kStep, hi, ids);
-  while (t < hi) {
-    load_block<D, E4M3>(y, pg, t + kStep, hi, ids);
-    load_ids<B>(pg, t + 2 * kStep, hi, ids);
-    take_block<D, E4M3>(x, st, q, scale2, hi - t);
-    t += kStep;
-    if (t >= hi) break;
-    load_block<D, E4M3>(x, pg, t + kStep, hi, ids);
-    load_ids<B>(pg, t + 2 * kStep, hi, ids);
-    take_block<D, E4M3>(y, st, q, scale2, hi - t);
-    t += kStep;
+    // The four waves.
+    __syncthreads();  // the last head's
+    if (c == 0) sm[wave][m] = st.m, sl[wave][m] = st.l;
+    __syncthreads();
+    float M = sm[0][m];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm[w][m]);
+    const float f = fast_exp2(st.m - (M == -INFINITY ? 0.f : M));
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (B::kCols * (4 * c + r) < D) {
+#pragma unroll
+        for (int i = 0; i < B::kCols; i += 4)
+          *reinterpret_cast<f32x4 *>(&so[wave][m][B::kCols * (4 * c + r) + i]) =
+              f32x4{st.o[i][r] * f, st.o[i + 1][r] * f, st.o[i + 2][r] * f, st.o[i + 3][r] * f};
+      }
+    __syncthreads();
+    const size_t row0 = (size_t)seq * a.n_q + h0;
+    const bool whole = take == n;
+    const int slot = pos != begin;
+    if (u == 0) {
+      open = Open{(int)row0, heads, whole ? 0 : (pos + n - 1) / quota - g + 1, 2 * g + slot};
+      if (by_head && threadIdx.x == 0) ps.open[(size_t)seq * R + head] = open;
+    }
+    for (int i = threadIdx.x; i < heads * (D / 4); i += kThreads) {
+      const int h = i / (D / 4), e = i % (D / 4) * 4;
+      float mx = sm[0][h], L = 0.f;
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) mx = fmaxf(mx, sm[w][h]);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+      f32x4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        L += fast_exp2(sm[w][h] - ref) * sl[w][h];
+        O += *reinterpret_cast<const f32x4 *>(&so[w][h][e]);
+      }
+      if (whole) {
+        O *= 1.f / L;
+        *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.o) + (row0 + h) * D + e) =
+            u32x2{pack_bf16x2(O.x, O.y), pack_bf16x2(O.z, O.w)};
+        if (e == 0 && a.lse) a.lse[row0 + h] = (mx + fast_log2(L)) * kLn2;
+      } else {
+        const size_t p = ((size_t)g * 2 + slot) * kRows + h;
+        *reinterpret_cast<f32x4 *>(ps.o + p * D + e) = O;
+        if (e == 0) ps.ml[p] = f32x2{mx, L};
+      }
+    }
+    pos += take;
+    if (pos < end) {  // the next head, of the next sequence that has keys
+      u = 0;
+      if (++head == R) {
+        head = 0;
+        n = 0;
+        while (n == 0 && ++seq < b) n = units_of<B>(scalar_load(a.lens, seq), a.max_len);
+        if (n == 0) break;  // not reached while lens stays as it is
+      }
+    }
   }
-  st.l = column_sum(st.l);
-
-  // The four waves.
-  __shared__ float so[kWaves][kRows][D + 4], sm[kWaves][kRows], sl[kWaves][kRows];
-  if (c == 0) sm[wave][m] = st.m, sl[wave][m] = st.l;
-  __syncthreads();
-  float M = sm[0][m];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm[w][m]);
-  const float f = fast_exp2(st.m - (M == -INFINITY ? 0.f : M));
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (B::kCols * (4 * c + r) < D) {
-#pragma unroll
-      for (int i = 0; i < B::kCols; i += 4)
-        *reinterpret_cast<f32x4 *>(&so[wave][m][B::kCols * (4 * c + r) + i]) =
-            f32x4{st.o[i][r] * f, st.o[i + 1][r] * f, st.o[i + 2][r] * f, st.o[i + 3][r] * f};
-    }
-  __syncthreads();
-  const bool whole = len <= sp.keys;  // the sequence's only split
-  const Partials ps = partials_at(a.workspace, (size_t)a.s.b * a.n_q, sp.splits, D);
-  for (int i = threadIdx.x; i < heads * (D / 4); i += kThreads) {
-    const int h = i / (D / 4), e = i % (D / 4) * 4;
-    float mx = sm[0][h], L = 0.f;
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) mx = fmaxf(mx, sm[w][h]);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    f32x4 O = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      L += fast_exp2(sm[w][h] - ref) * sl[w][h];
-      O += *reinterpret_cast<const f32x4 *>(&so[w][h][e]);
-    }
-    if (whole) {
-      O *= 1.f / L;
-      *reinterpret_cast<u32x2 *>(o + h * D + e) = u32x2{pack_bf16x2(O.x, O.y), pack_bf16x2(O.z, O.w)};
-      if (e == 0 && a.lse) a.lse[row0 + h] = (mx + fast_log2(L)) * kLn2;
-    } else {
-      const size_t p = (row0 + h) * sp.splits + split;
-      *reinterpret_cast<f32x4 *>(ps.o + p * D + e) = O;
-      if (e == 0) ps.ml[p] = f32x2{mx, L};
-    }
-  }
+  if (joins && !by_head && threadIdx.x == 0) ps.open[g] = open;
+  write_empty();
 }
 
-// One (sequence, query head) with several splits: its splits in turn over 8
-// groups of 32 threads, 4 elements of d a thread.
-template <int D>
-__global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs a,
-                                                               const DecodeSplit sp) {
-  const int r = blockIdx.x;
-  const int len = a.lens[r / a.n_q];
-  if (len <= sp.keys || len > a.max_len) return;  // written by the split itself
-  const int n = (len + sp.keys - 1) / sp.keys;
-  const Partials p = partials_at(a.workspace, gridDim.x, sp.splits, D);
-  const f32x2 *ml = p.ml + (size_t)r * sp.splits;
-  const float *po = p.o + (size_t)r * sp.splits * D;
-  const int g = threadIdx.x / 32, e = threadIdx.x % 32 * 4;
-  __shared__ float so[8][D + 4], sl[8], sm[kWaves];
+// One row of one head with several partial results: these in turn over 8 C groups of
+// 32 / C threads, 4 elements of d a thread; C workgroups share the row's elements.
+template <int D, int C>
+__global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs a, int opens,
+                                                               int groups) {
+  constexpr int L = 32 / C, R = kThreads / L;
+  const Partials p = partials_at(a.workspace, opens, groups);
+  const Open open = p.open[blockIdx.x];
+  const int h = blockIdx.y;
+  if (h >= open.heads || open.count == 0) return;
+  const int n = open.count;
+  auto at = [&](int i) {
+    return (size_t)(i ? (open.first | 1) - 1 + 2 * i : open.first) * kRows + h;
+  };
+  const int g = threadIdx.x / L, col = blockIdx.z * (4 * L) + threadIdx.x % L * 4;
+  __shared__ float so[R][4 * L + 4], sl[R], sm[kWaves];
   float M = -INFINITY;
-  for (int i = threadIdx.x; i < n; i += kThreads) M = fmaxf(M, ml[i].x);
+  for (int i = threadIdx.x; i < n; i += kThreads) M = fmaxf(M, p.ml[at(i)].x);
 #pragma unroll
   for (int x = 32; x; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
   if (threadIdx.x % 64 == 0) sm[threadIdx.x / 64] = M;
@@ -431,63 +566,81 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs 
   for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm[w]);
   const float ref = M == -INFINITY ? 0.f : M;
   f32x4 O = {0.f, 0.f, 0.f, 0.f};
-  float L = 0.f;
+  float l = 0.f;
 #pragma unroll 4
-  for (int i = g; i < n; i += 8) {
-    const f32x2 x = ml[i];
+  for (int i = g; i < n; i += R) {
+    const f32x2 x = p.ml[at(i)];
     const float f = fast_exp2(x.x - ref);
-    L += f * x.y;
-    if (e < D) O += f * *reinterpret_cast<const f32x4 *>(po + (size_t)i * D + e);
+    l += f * x.y;
+    if (col < D) O += f * *reinterpret_cast<const f32x4 *>(p.o + at(i) * D + col);
   }
-  if (e < D) *reinterpret_cast<f32x4 *>(&so[g][e]) = O;
-  if (e == 0) sl[g] = L;
+  *reinterpret_cast<f32x4 *>(&so[g][threadIdx.x % L * 4]) = O;
+  if (threadIdx.x % L == 0) sl[g] = l;
   __syncthreads();
-  if (threadIdx.x < D / 2) {
-    const int x = threadIdx.x * 2;
+  const int e = blockIdx.z * (4 * L) + threadIdx.x * 2;
+  if (threadIdx.x < 2 * L && e < D) {
     float A = 0.f, Bb = 0.f;
-    L = 0.f;
+    l = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) A += so[i][x], Bb += so[i][x + 1], L += sl[i];
-    const float inv = 1.f / L;
-    static_cast<uint32_t *>(a.o)[(size_t)r * (D / 2) + threadIdx.x] = pack_bf16x2(A * inv, Bb * inv);
-    if (threadIdx.x == 0 && a.lse) a.lse[r] = (M + fast_log2(L)) * kLn2;
+    for (int i = 0; i < R; ++i) {
+      A += so[i][threadIdx.x * 2];
+      Bb += so[i][threadIdx.x * 2 + 1];
+      l += sl[i];
+    }
+    const float inv = 1.f / l;
+    const size_t r = (size_t)open.row0 + h;
+    static_cast<uint32_t *>(a.o)[(r * D + e) / 2] = pack_bf16x2(A * inv, Bb * inv);
+    if (e == 0 && a.lse) a.lse[r] = (M + fast_log2(l)) * kLn2;
   }
+}
+
+struct Shape {
+  int groups, opens;  // workgroups, and descriptors for the join
+  size_t bytes;       // of workspace, 0 where no head is shared by two workgroups
+};
+Shape shape_of(int b, int n_q, int n_k, int d, int max_len, bool e4m3) {
+  const int rep = n_q / n_k, most = kCus * per_cu(d, e4m3);
+  const long long heads = (long long)b * n_k * ((rep + kRows - 1) / kRows);
+  const int unit = e4m3 ? 256 : 128;
+  const long long units = heads * (((long long)max_len + unit - 1) / unit);
+  Shape s;
+  s.groups = (int)(units < most ? units : most);
+  s.opens = (int)(heads < s.groups ? heads : s.groups);
+  s.bytes = max_len <= unit ? 0
+                            : s.opens * kOpenBytes +
+                                  s.groups * (kRowBytesMl + 2 * kRows * d * sizeof(float));
+  return s;
+}
+
+template <int D, bool E4M3>
+hipError_t decode_typed(const DecodeArgs &a, hipStream_t stream) {
+  const Shape s = shape_of(a.s.b, a.n_q, a.s.n_k, D, a.max_len, E4M3);
+  hipLaunchKernelGGL((decode_kernel<D, E4M3>), dim3(s.groups), dim3(kThreads), 0, stream, a,
+                     s.opens);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.workspace) return e;
+  const int rep = a.n_q / a.s.n_k, rows = rep < kRows ? rep : kRows;
+  if (s.groups >= 16 * s.opens)
+    hipLaunchKernelGGL((decode_join_kernel<D, 8>), dim3(s.opens, rows, 8), dim3(kThreads), 0,
+                       stream, a, s.opens, s.groups);
+  else
+    hipLaunchKernelGGL((decode_join_kernel<D, 1>), dim3(s.opens, rows), dim3(kThreads), 0, stream,
+                       a, s.opens, s.groups);
+  return hipGetLastError();
 }
 
 template <int D>
 hipError_t decode_dim(const DecodeArgs &a, hipStream_t stream) {
-  const DecodeSplit sp = decode_split(a.s.b, a.n_q, a.s.n_k, a.max_len);
-  const int rep = a.n_q / a.s.n_k;
-  const unsigned blocks =
-      (unsigned)a.s.b * a.s.n_k * ((rep + kRows - 1) / kRows) * (unsigned)sp.splits;
-  if (a.s.e4m3)
-    hipLaunchKernelGGL((decode_split_kernel<D, true>), dim3(blocks), dim3(kThreads), 0, stream, a,
-                       sp);
-  else
-    hipLaunchKernelGGL((decode_split_kernel<D, false>), dim3(blocks), dim3(kThreads), 0, stream, a,
-                       sp);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || sp.splits == 1) return e;
-  hipLaunchKernelGGL((decode_join_kernel<D>), dim3((unsigned)a.s.b * a.n_q), dim3(kThreads), 0,
-                     stream, a, sp);
-  return hipGetLastError();
+  return a.s.e4m3 ? decode_typed<D, true>(a, stream) : decode_typed<D, false>(a, stream);
 }
 
 }  // namespace
 
-DecodeSplit decode_split(int b, int n_q, int n_k, int max_len) {
-  const int rep = n_q / n_k;
-  const long long rows = (long long)b * n_k * ((rep + kRows - 1) / kRows);
-  const long long want = (4096 + rows - 1) / rows;  // splits
-  DecodeSplit sp;
-  sp.keys = (int)((max_len + want * 256 - 1) / (want * 256)) * 256;
-  sp.splits = (max_len + sp.keys - 1) / sp.keys;
-  return sp;
-}
-
+// Enough for either type of cache.
 size_t decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_len) {
-  const DecodeSplit sp = decode_split(b, n_q, n_k, max_len);
-  return sp.splits == 1 ? 0 : (size_t)b * n_q * sp.splits * (d + 2) * sizeof(float);
+  const size_t x = shape_of(b, n_q, n_k, d, max_len, false).bytes;
+  const size_t y = shape_of(b, n_q, n_k, d, max_len, true).bytes;
+  return x > y ? x : y;
 }
 
 hipError_t launch_attn_decode(const DecodeArgs &a, hipStream_t stream) {

@@ -81,15 +81,9 @@ struct DecodeArgs {
   float *lse;
   int n_q, max_len;
   float scale;
-  void *workspace;
+  void *workspace;  // NULL where no head is shared by two workgroups
 };
 
-// How the sequences of a call are split: keys per split (a multiple of 64) and
-// the splits of the longest.
-struct DecodeSplit {
-  int keys, splits;
-};
-DecodeSplit decode_split(int b, int n_q, int n_k, int max_len);
 size_t decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_len);
 
 hipError_t launch_attn_decode(const DecodeArgs &a, hipStream_t stream);
