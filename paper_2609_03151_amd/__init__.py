@@ -449,81 +449,116 @@ def attn_bwd_sharded(q_shards, k_shards, v_shards, o_shards, lse, do_shards, dq_
 
 
 # --------------------------------------- operators around attention
-# Their tensors have to lie on one device; a call whose device is not the
-# current one makes it current for the launch.
-def _call(name: str, t: torch.Tensor, *args):
-    dev = t.get_device()
-    fn = getattr(lib(), name)
+# A call on a few tokens takes less time on the GPU than its arguments' checks
+# would as so many Python calls: one condition per tensor below, and a refusal's
+# wording found only once it is refused.  All tensors of a call lie on one
+# device, which is made current for the launch if it is not.
+_Tensor, _F32, _BF, _I32 = torch.Tensor, torch.float32, torch.bfloat16, torch.int32
+
+
+def _call(name: str, fn, dev: int, *args):
+    if dev < 0:
+        raise TypeError(f"{name}: tensors must be CUDA (HIP) tensors")
     if dev == torch._C._cuda_getDevice():
-        rc = fn(*args, _stream(t))
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, _stream(t))
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     if rc != 0:
         raise BaspError(rc, name)
 
 
-def _on(t: torch.Tensor, name: str, dtype, shape, like: torch.Tensor) -> int:
-    """Pointer of a contiguous tensor of this type and shape on ``like``'s device."""
-    p = _dev(t, name, dtype)
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.get_device() != like.get_device():
-        raise ValueError(f"{name} and the first tensor are on different devices")
-    return p
-
-
-def _rows(t: torch.Tensor, name: str, dtype, shape, like: torch.Tensor):
-    """(pointer, elements between tokens) of a [..., n, d] tensor whose tokens lie one stride apart
-    and whose heads lie side by side: contiguous, or columns of a wider contiguous tensor."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+def _device(t, name: str, dims: int) -> int:
+    """Device index of a call's first tensor, of this many dimensions; below zero for a host tensor,
+    which _call refuses."""
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dtype != dtype:
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
+    return t.get_device()
+
+
+def _refuse(t, name: str, dtype, shape, dev: int):
+    if dev >= 0 or not isinstance(t, _Tensor):
+        _dev(t, name, dtype)
+    elif t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.get_device() != like.get_device():
-        raise ValueError(f"{name} and the first tensor are on different devices")
-    n, d = shape[-2:]
+    raise ValueError(f"{name} is on device {t.get_device()}, the call's first tensor on {dev}")
+
+
+def _on(t, name: str, dtype, shape, dev: int) -> int:
+    """Pointer of a contiguous tensor of this type and shape on device ``dev``."""
+    if (isinstance(t, _Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == dev
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _refuse(t, name, dtype, shape, dev)
+
+
+def _opt(t, name: str, dtype, shape, dev: int):
+    return None if t is None else _on(t, name, dtype, shape, dev)
+
+
+def _rows(t, name: str, dtype, shape, dev: int):
+    """(pointer, elements between tokens) of a [..., n, d] tensor whose tokens lie one stride apart
+    and whose heads lie side by side: contiguous, or columns of a wider contiguous tensor."""
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.shape == shape
+            and t.get_device() == dev):
+        _refuse(t.contiguous() if isinstance(t, _Tensor) else t, name, dtype, shape, dev)
+    n, d = shape[-2], shape[-1]
     if t.is_contiguous():
         return t.data_ptr(), n * d
     st = t.stride()
     lead = [(s, z) for s, z in zip(st[:-2], shape[:-2]) if z > 1]  # outermost first
     row = lead[-1][0] if lead else n * d
-    ok = (d == 1 or st[-1] == 1) and (n == 1 or st[-2] == d) and row >= n * d
+    ok = st[-1] == 1 and (n == 1 or st[-2] == d) and row >= n * d
     want = row
     for s, z in reversed(lead):
         ok = ok and s == want
         want = s * z
-    if not ok and t.numel():
+    if not ok:
         raise ValueError(f"{name} must have its heads side by side and its tokens one stride apart")
     return t.data_ptr(), row
 
 
-def _opt(t, name: str, dtype, shape, like):
-    return None if t is None else _on(t, name, dtype, shape, like)
+def _space(workspace, need: int, like, dev: int):
+    """(tensor to keep, pointer, bytes) of a given workspace of any type, or of a new one."""
+    if workspace is None:
+        if need == 0:
+            return None, None, 0
+        workspace = like.new_empty(need, dtype=torch.uint8)
+        return workspace, workspace.data_ptr(), need
+    p = _on(workspace, "workspace", workspace.dtype, workspace.shape, dev)
+    return workspace, p, workspace.numel() * workspace.element_size()
 
 
 def _norm_args(q, k, q_weight, k_weight, cos, sin, positions):
-    if not isinstance(q, torch.Tensor) or q.dim() != 4:
-        raise ValueError("q must be [b, S, n_q, d]")
-    if not isinstance(k, torch.Tensor) or k.dim() != 4 or (k.shape[0], k.shape[1], k.shape[3]) != (
-            q.shape[0], q.shape[1], q.shape[3]):
-        raise ValueError("q and k disagree in shape")
+    """Device, sizes, (weights, tables, positions) pointers and the element type's code."""
+    dev = _device(q, "q", 4)
     b, S, n_q, d = q.shape
-    f32 = torch.float32
+    if not isinstance(k, _Tensor) or k.dim() != 4:
+        raise ValueError("k must be [b, S, n_k, d]")
+    kb, kS, n_k, kd = k.shape
+    if kb != b or kS != S or kd != d:
+        raise ValueError("q and k disagree in shape")
     if (cos is None) != (sin is None) or (q_weight is None) != (k_weight is None):
         raise ValueError("cos and sin, and q_weight and k_weight, go together")
-    if cos is not None and (not isinstance(cos, torch.Tensor) or cos.dim() != 2):
-        raise ValueError("cos and sin must be [positions, rot/2]")
-    table_rows, half = (0, 0) if cos is None else cos.shape
-    if half == 0:  # no columns: nothing is rotated
-        cos = sin = None
-    tail = (_opt(q_weight, "q_weight", f32, (d,), q), _opt(k_weight, "k_weight", f32, (d,), q))
-    turn = (_opt(cos, "cos", f32, (table_rows, half), q),
-            _opt(sin, "sin", f32, (table_rows, half), q),
-            _opt(positions, "positions", torch.int32, (b, S), q))
-    return (b, S, n_q, k.shape[2], d, 2 * half, table_rows), tail, turn
+    qw = kw = c = sn = None
+    if q_weight is not None:
+        w = (d,)
+        qw, kw = _on(q_weight, "q_weight", _F32, w, dev), _on(k_weight, "k_weight", _F32, w, dev)
+    rows = half = 0
+    if cos is not None:
+        if not isinstance(cos, _Tensor) or cos.dim() != 2:
+            raise ValueError("cos and sin must be [positions, rot/2]")
+        table = cos.shape
+        rows, half = table
+        c, sn = _on(cos, "cos", _F32, table, dev), _on(sin, "sin", _F32, table, dev)
+        if half == 0:  # no columns: nothing is rotated
+            c = sn = None
+    pos = None if positions is None else _on(positions, "positions", _I32, (b, S), dev)
+    return dev, (b, S, n_q, n_k, d, 2 * half, rows), (qw, kw), (c, sn, pos), _dtype_code(q)
 
 
 def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, eps: float = 1e-6, positions=None,
@@ -535,20 +570,22 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, eps: float = 1e-6, position
     (``rope_table`` makes them), or both None for no rotation.  A token's position is
     ``positions`` int32 [b, S] (negative: a row of padding, zeros out), or pos0 + its index.
     Returns (q_out, k_out) in q's type."""
-    (b, S, n_q, n_k, d, rot, rows), w, turn = _norm_args(q, k, q_weight, k_weight, cos, sin,
-                                                         positions)
-    dt = q.dtype
-    code = _dtype_code(q)
+    dev, dims, w, turn, code = _norm_args(q, k, q_weight, k_weight, cos, sin, positions)
+    dt, q_shape, k_shape, d = q.dtype, q.shape, k.shape, dims[4]
+    qp, q_row = _rows(q, "q", dt, q_shape, dev)
+    kp, k_row = _rows(k, "k", dt, k_shape, dev)
     if q_out is None:
-        q_out = torch.empty((b, S, n_q, d), dtype=dt, device=q.device)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        qop, qo_row = q_out.data_ptr(), dims[2] * d
+    else:
+        qop, qo_row = _rows(q_out, "q_out", dt, q_shape, dev)
     if k_out is None:
-        k_out = torch.empty((b, S, n_k, d), dtype=dt, device=q.device)
-    qp, q_row = _rows(q, "q", dt, q.shape, q)
-    kp, k_row = _rows(k, "k", dt, k.shape, q)
-    qop, qo_row = _rows(q_out, "q_out", dt, q.shape, q)
-    kop, ko_row = _rows(k_out, "k_out", dt, k.shape, q)
-    _call("basp_qk_norm_rope", q, qp, kp, qop, kop, *w, *turn, b, S, n_q, n_k, d, rot, rows, q_row,
-          k_row, qo_row, ko_row, eps, pos0, interleaved, code)
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+        kop, ko_row = k_out.data_ptr(), dims[3] * d
+    else:
+        kop, ko_row = _rows(k_out, "k_out", dt, k_shape, dev)
+    _call("basp_qk_norm_rope", (_lib or lib()).basp_qk_norm_rope, dev, qp, kp, qop, kop, *w, *turn,
+          *dims, q_row, k_row, qo_row, ko_row, eps, pos0, interleaved, code)
     return q_out, k_out
 
 
@@ -562,44 +599,41 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, eps: fl
     """Backward of qk_norm_rope at its inputs ``q``, ``k``: from the gradients of its outputs (fp32
     or bf16, contiguous) to (dq, dk, dq_weight, dk_weight): dq, dk in the gradients' type (``dq``
     may be ``dq_out`` itself, ``dk`` ``dk_out``), the weights' in fp32 (None without weights)."""
-    (b, S, n_q, n_k, d, rot, rows), w, turn = _norm_args(q, k, q_weight, k_weight, cos, sin,
-                                                         positions)
-    code = _dtype_code(q)
+    dev, dims, w, turn, code = _norm_args(q, k, q_weight, k_weight, cos, sin, positions)
+    b, S, n_q, n_k, d = dims[:5]
+    q_shape, k_shape = q.shape, k.shape
+    qp, q_row = _rows(q, "q", q.dtype, q_shape, dev)
+    kp, k_row = _rows(k, "k", q.dtype, k_shape, dev)
+    if not isinstance(dq_out, _Tensor):
+        raise TypeError("dq_out must be a CUDA (HIP) tensor")
     gt, gcode = dq_out.dtype, _dtype_code(dq_out)
+    gq, gk = _on(dq_out, "dq_out", gt, q_shape, dev), _on(dk_out, "dk_out", gt, k_shape, dev)
     if dq is None:
-        dq = torch.empty((b, S, n_q, d), dtype=gt, device=q.device)
+        dq = torch.empty_like(dq_out)
     if dk is None:
-        dk = torch.empty((b, S, n_k, d), dtype=gt, device=q.device)
+        dk = torch.empty_like(dk_out)
+    L = _lib or lib()
+    dqw = dkw = ws = ws_n = None
     if q_weight is None:
-        dq_weight = dk_weight = workspace = None
+        dq_weight = dk_weight = None
+        ws_n = 0
     else:
         if dq_weight is None:
-            dq_weight = torch.empty(d, dtype=torch.float32, device=q.device)
+            dq_weight = torch.empty_like(q_weight)
         if dk_weight is None:
-            dk_weight = torch.empty(d, dtype=torch.float32, device=q.device)
+            dk_weight = torch.empty_like(k_weight)
         if b * S == 0:
             dq_weight.zero_()
             dk_weight.zero_()
-        if workspace is None:
-            need = qk_norm_rope_bwd_workspace_bytes(b, S, n_q, n_k, d)
-            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
-    qp, q_row = _rows(q, "q", q.dtype, q.shape, q)
-    kp, k_row = _rows(k, "k", q.dtype, k.shape, q)
-    f32 = torch.float32
-    _call("basp_qk_norm_rope_bwd", q, qp, kp, _on(dq_out, "dq_out", gt, q.shape, q),
-          _on(dk_out, "dk_out", gt, k.shape, q), _on(dq, "dq", gt, q.shape, q),
-          _on(dk, "dk", gt, k.shape, q), *w, _opt(dq_weight, "dq_weight", f32, (d,), q),
-          _opt(dk_weight, "dk_weight", f32, (d,), q), *turn, *_space(workspace, q), b, S, n_q,
-          n_k, d, rot, rows, q_row, k_row, eps, pos0, interleaved, code, gcode)
+        dqw = _on(dq_weight, "dq_weight", _F32, (d,), dev)
+        dkw = _on(dk_weight, "dk_weight", _F32, (d,), dev)
+        need = 0 if workspace is not None else L.basp_qk_norm_rope_bwd_workspace_bytes(
+            b, S, n_q, n_k, d)
+        workspace, ws, ws_n = _space(workspace, need, q, dev)
+    _call("basp_qk_norm_rope_bwd", L.basp_qk_norm_rope_bwd, dev, qp, kp, gq, gk,
+          _on(dq, "dq", gt, q_shape, dev), _on(dk, "dk", gt, k_shape, dev), *w, dqw, dkw, *turn, ws,
+          ws_n, *dims, q_row, k_row, eps, pos0, interleaved, code, gcode)
     return dq, dk, dq_weight, dk_weight
-
-
-def _space(workspace, like):
-    """(pointer, bytes) of a workspace tensor of any type, or of none."""
-    if workspace is None:
-        return None, 0
-    return (_on(workspace, "workspace", None, workspace.shape, like),
-            workspace.numel() * workspace.element_size())
 
 
 def rope_table(n: int, rot: int, base: float = 10000.0, device="cuda"):
@@ -611,29 +645,36 @@ def rope_table(n: int, rot: int, base: float = 10000.0, device="cuda"):
 
 
 # --------------------------------------------------------- key-value cache
-def _pages(k_pages, v_pages, k_scales, v_scales, table, like):
+_CACHE_TYPES = {torch.bfloat16: BASP_BF16, torch.float8_e4m3fn: BASP_E4M3}
+
+
+def _pages(k_pages, v_pages, k_scales, v_scales, table, b, dev: int):
     """((k_pages, v_pages, k_scales, v_scales, table) pointers, (n_k, d, page, n_pages, max_pages),
-    dtype code) of a paged cache."""
-    if not isinstance(k_pages, torch.Tensor) or k_pages.dim() != 4:
+    dtype code) of a paged cache whose table has b rows."""
+    if not isinstance(k_pages, _Tensor) or k_pages.dim() != 4:
         raise ValueError("k_pages must be [n_pages, n_k, page, d]")
-    n_pages, n_k, page, d = shape = k_pages.shape
+    shape = k_pages.shape
+    n_pages, n_k, page, d = shape
     dt = k_pages.dtype
-    if dt == torch.bfloat16:
-        code = BASP_BF16
-    elif dt == torch.float8_e4m3fn:
-        code = BASP_E4M3
-    else:
+    code = _CACHE_TYPES.get(dt)
+    if code is None:
         raise TypeError(f"unsupported dtype {dt}")
-    if (k_scales is None) != (dt == torch.bfloat16) or (v_scales is None) != (k_scales is None):
-        raise ValueError("an 8-bit cache has k_scales and v_scales, a bf16 cache neither")
-    if not isinstance(table, torch.Tensor) or table.dim() != 2:
-        raise ValueError("block_table must be [b, max_pages]")
-    u8 = torch.uint8
-    ptrs = (_on(k_pages, "k_pages", dt, shape, like), _on(v_pages, "v_pages", dt, shape, like),
-            _opt(k_scales, "k_scales", u8, shape[:3], like),
-            _opt(v_scales, "v_scales", u8, shape[:3], like),
-            _on(table, "block_table", torch.int32, table.shape, like))
-    return ptrs, (n_k, d, page, n_pages, table.shape[1]), code
+    if not isinstance(table, _Tensor) or table.dim() != 2 or table.shape[0] != b:
+        raise ValueError(f"block_table must be [{b}, max_pages]")
+    if code == BASP_BF16:
+        if k_scales is not None or v_scales is not None:
+            raise ValueError("a bf16 cache has no scales")
+        ks = vs = None
+    else:
+        if k_scales is None or v_scales is None:
+            raise ValueError("an 8-bit cache has k_scales and v_scales")
+        u8, s_shape = torch.uint8, (n_pages, n_k, page)
+        ks = _on(k_scales, "k_scales", u8, s_shape, dev)
+        vs = _on(v_scales, "v_scales", u8, s_shape, dev)
+    t_shape = table.shape
+    return ((_on(k_pages, "k_pages", dt, shape, dev), _on(v_pages, "v_pages", dt, shape, dev), ks, vs,
+             _on(table, "block_table", _I32, t_shape, dev)),
+            (n_k, d, page, n_pages, t_shape[1]), code)
 
 
 def kv_write(k, v, k_pages, v_pages, block_table, start, count=None, k_scales=None,
@@ -642,33 +683,36 @@ def kv_write(k, v, k_pages, v_pages, block_table, start, count=None, k_scales=No
     per sequence into the pages [n_pages, n_k, page, d] of a cache, bf16 or e4m3 (then with
     scale bytes [n_pages, n_k, page]): token t of sequence s at position start[s] + t, for
     t < count[s] (count None: all T).  Sequences with a negative start are skipped."""
-    if not isinstance(k, torch.Tensor) or k.dim() != 4:
-        raise ValueError("k must be [b, T, n_k, d]")
-    b, T = k.shape[:2]
-    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, k)
-    if k.shape[2:] != (dims[0], dims[1]) or block_table.shape[0] != b:
-        raise ValueError("k, the pages and block_table disagree in shape")
-    kp, k_row = _rows(k, "k", torch.bfloat16, k.shape, k)
-    vp, v_row = _rows(v, "v", torch.bfloat16, k.shape, k)
-    _call("basp_kv_write", k, kp, vp, *ptrs, _on(start, "start", torch.int32, (b,), k),
-          _opt(count, "count", torch.int32, (b,), k), b, T, *dims, k_row, v_row, code)
+    dev = _device(k, "k", 4)
+    shape = k.shape
+    b, T, n_k, d = shape
+    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, b, dev)
+    if dims[0] != n_k or dims[1] != d:
+        raise ValueError("k and the pages disagree in shape")
+    kp, k_row = _rows(k, "k", _BF, shape, dev)
+    vp, v_row = _rows(v, "v", _BF, shape, dev)
+    _call("basp_kv_write", (_lib or lib()).basp_kv_write, dev, kp, vp, *ptrs,
+          _on(start, "start", _I32, (b,), dev),
+          None if count is None else _on(count, "count", _I32, (b,), dev), b, T, *dims, k_row,
+          v_row, code)
 
 
 def kv_read(k_pages, v_pages, block_table, T: int, start=None, count=None, k_scales=None,
             v_scales=None, k=None, v=None):
     """Positions start[s] .. start[s] + count[s] - 1 of every sequence (start None: from 0, count None:
     T) out of a paged cache, as (k, v) [b, T, n_k, d] bf16; rows past count[s] are zeros."""
-    like = k_pages
-    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, like)
-    b, shape = block_table.shape[0], (block_table.shape[0], T, dims[0], dims[1])
-    bf = torch.bfloat16
+    dev = _device(block_table, "block_table", 2)
+    b = block_table.shape[0]
+    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, b, dev)
+    shape = (b, T, dims[0], dims[1])
     if k is None:
-        k = torch.empty(shape, dtype=bf, device=like.device)
+        k = block_table.new_empty(shape, dtype=_BF)
     if v is None:
-        v = torch.empty(shape, dtype=bf, device=like.device)
-    _call("basp_kv_read", like, *ptrs, _opt(start, "start", torch.int32, (b,), like),
-          _opt(count, "count", torch.int32, (b,), like), _on(k, "k", bf, shape, like),
-          _on(v, "v", bf, shape, like), b, T, *dims, code)
+        v = torch.empty_like(k)
+    _call("basp_kv_read", (_lib or lib()).basp_kv_read, dev, *ptrs,
+          None if start is None else _on(start, "start", _I32, (b,), dev),
+          None if count is None else _on(count, "count", _I32, (b,), dev),
+          _on(k, "k", _BF, shape, dev), _on(v, "v", _BF, shape, dev), b, T, *dims, code)
     return k, v
 
 
@@ -684,28 +728,27 @@ def attn_decode(q, k_pages, v_pages, block_table, lens, scale: float | None = No
     d], lse fp32 [b, n_q]).  A length of 0 gives zeros and -inf.  ``max_len``: the longest sequence
     expected (default: all the table holds).  Two calls that may overlap on the device, captured
     graphs among them, need a ``workspace`` each (default: one of its own per call)."""
-    if not isinstance(q, torch.Tensor) or q.dim() != 3:
-        raise ValueError("q must be [b, n_q, d]")
-    b, n_q, d = q.shape
-    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, q)
+    dev = _device(q, "q", 3)
+    shape = q.shape
+    b, n_q, d = shape
+    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, b, dev)
     n_k, dp, page, n_pages, max_pages = dims
-    if dp != d or block_table.shape[0] != b:
-        raise ValueError("q, the pages and block_table disagree in shape")
-    scale = d ** -0.5 if scale is None else scale
+    if dp != d:
+        raise ValueError("q and the pages disagree in shape")
+    if scale is None:
+        scale = d ** -0.5
     if max_len is None:
         max_len = max_pages * page
-    bf = torch.bfloat16
+    qp, q_row = _rows(q, "q", _BF, shape, dev)
     if out is None:
-        out = torch.empty((b, n_q, d), dtype=bf, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None:
-        lse = torch.empty((b, n_q), dtype=torch.float32, device=q.device)
-    if workspace is None:
-        need = attn_decode_workspace_bytes(b, n_q, n_k, d, max_len)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    qp, q_row = _rows(q, "q", bf, q.shape, q)
-    _call("basp_attn_decode", q, qp, *ptrs, _on(lens, "lens", torch.int32, (b,), q),
-          _on(out, "out", bf, q.shape, q), _on(lse, "lse", torch.float32, (b, n_q), q),
-          *_space(workspace, q), b, n_q, n_k, d, page, n_pages, max_pages, max_len, q_row,
-          float(scale), code)
+        lse = q.new_empty((b, n_q), dtype=_F32)
+    L = _lib or lib()
+    need = 0 if workspace is not None else L.basp_attn_decode_workspace_bytes(b, n_q, n_k, d,
+                                                                              max_len)
+    workspace, ws, ws_n = _space(workspace, need, q, dev)
+    _call("basp_attn_decode", L.basp_attn_decode, dev, qp, *ptrs, _on(lens, "lens", _I32, (b,), dev),
+          _on(out, "out", _BF, shape, dev), _on(lse, "lse", _F32, (b, n_q), dev), ws, ws_n, b, n_q,
+          n_k, d, page, n_pages, max_pages, max_len, q_row, float(scale), code)
     return out, lse
