@@ -411,7 +411,8 @@ int basp_attn_bwd_sharded(const void *const *q_shards,
  * Errors: NULL (a pointer, or one weight or table without the other), SHAPE
  * (negative size, rot as above, q_row < n_q*d, pos0 < 0, or pos0 + S >
  * table_rows without positions), UNSUPPORTED (d, dtype, eps negative or not
- * finite, b*S*n_q or b*S*n_k >= 2^29), ALIGN, HIP. */
+ * finite, b*S*n_q or b*S*n_k >= 2^29, b*S*(ceil(n_q/4) + ceil(n_k/4)) >= 2^27),
+ * ALIGN, HIP. */
 int basp_qk_norm_rope(const void *q, const void *k, void *qo, void *ko, const float *qw,
                       const float *kw, const float *cos, const float *sin,
                       const int *positions, int b, int S, int n_q, int n_k, int d, int rot,

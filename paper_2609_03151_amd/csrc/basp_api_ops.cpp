@@ -27,8 +27,8 @@ uint64_t rows_of(int b, int S, int n, int bits) {
 }
 
 // Shape rules of norm and rotation, forward and backward; pointers are looked
-// at by the callers.  A launch's threads are a 32-bit count, four of them a row
-// in the forward: up to 2^29 rows of each tensor.
+// at by the callers.  A launch's threads are a 32-bit count, 16 of them four heads
+// of a token in the forward.
 int check_norm(int b, int S, int n_q, int n_k, int d, int rot, int table_rows, long long q_row,
                long long k_row, float eps, int pos0, bool positions, int dtype, int grad_dtype) {
   if (b < 0 || S < 0 || n_q < 1 || n_k < 1 || d < 1) return BASP_ERR_SHAPE;
@@ -38,7 +38,8 @@ int check_norm(int b, int S, int n_q, int n_k, int d, int rot, int table_rows, l
     if (t != BASP_BF16 && t != BASP_F32) return BASP_ERR_UNSUPPORTED;
   if (!(eps >= 0.f) || !isfinite(eps)) return BASP_ERR_UNSUPPORTED;
   if ((uint64_t)b * (uint64_t)S != 0 &&
-      (rows_of(b, S, n_q, 29) == 0 || rows_of(b, S, n_k, 29) == 0))
+      (rows_of(b, S, n_q, 29) == 0 || rows_of(b, S, n_k, 29) == 0 ||
+       rows_of(b, S, (n_q - 1) / 4 + (n_k - 1) / 4 + 2, 27) == 0))
     return BASP_ERR_UNSUPPORTED;
   if (q_row < (long long)n_q * d || k_row < (long long)n_k * d) return BASP_ERR_SHAPE;
   if (rot > 0 && !positions && (long long)pos0 + S > table_rows) return BASP_ERR_SHAPE;

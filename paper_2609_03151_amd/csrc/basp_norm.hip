@@ -44,19 +44,31 @@ __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
-// Four elements in fp32.
-__device__ __forceinline__ f32x4 load4(const uint16_t *p) {
-  const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
+// Four elements in fp32.  NT: read with the non-temporal hint.
+__device__ __forceinline__ f32x4 widen(u32x2 v) {
   return f32x4{__builtin_bit_cast(float, v.x << 16), __builtin_bit_cast(float, v.x & 0xFFFF0000u),
                __builtin_bit_cast(float, v.y << 16), __builtin_bit_cast(float, v.y & 0xFFFF0000u)};
 }
 __device__ __forceinline__ f32x4 load4(const float *p) {
   return *reinterpret_cast<const f32x4 *>(p);
 }
-__device__ __forceinline__ void store4(uint16_t *p, f32x4 v) {
-  *reinterpret_cast<u32x2 *>(p) = u32x2{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
+template <bool NT>
+__device__ __forceinline__ f32x4 load4(const uint16_t *p) {
+  const u32x2 *q = reinterpret_cast<const u32x2 *>(p);
+  return widen(NT ? __builtin_nontemporal_load(q) : *q);
 }
-__device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
+template <bool NT>
+__device__ __forceinline__ f32x4 load4(const float *p) {
+  const f32x4 *q = reinterpret_cast<const f32x4 *>(p);
+  return NT ? __builtin_nontemporal_load(q) : *q;
+}
+__device__ __forceinline__ void store4(uint16_t *p, f32x4 v) {
+  __builtin_nontemporal_store(u32x2{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)},
+                              reinterpret_cast<u32x2 *>(p));
+}
+__device__ __forceinline__ void store4(float *p, f32x4 v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(p));
+}
 
 // The elements of a row that a lane holds: runs [a, a+4) and [b, b+4), and the
 // first of the four pairs (a column of the cos and sin tables), or turns =
@@ -124,9 +136,23 @@ constexpr int kLanes = D <= 64 ? 8 : 16;  // lanes per row
 template <int D>
 constexpr int kGroups = kThreads / kLanes<D>;  // rows a workgroup holds at once
 
-constexpr int kU = 4;  // rows in flight per group, forward
+// The other element of each pair, for both runs.
+template <bool INTER>
+__device__ __forceinline__ void partners(f32x4 a, f32x4 b, f32x4 &oa, f32x4 &ob) {
+  oa = INTER ? f32x4{a.y, a.x, a.w, a.z} : b;
+  ob = INTER ? f32x4{b.y, b.x, b.w, b.z} : a;
+}
 
-template <typename T, int D, bool INTER>
+// Forward.  A group of lanes takes up to kHeads consecutive heads of one token: its
+// indices, position and table values are found once for them, and the weights go
+// into the rotation's coefficients once,
+//   y_a = r (x_a (w_a c) - x_b (w_b s)),  y_b = r (x_b (w_b c) + x_a (w_a s)),
+// which leaves about 70 vector instructions a row: with 150 (all of this per row)
+// these took most of the time of a large call, 165 us for 128K tokens of 8 + 1
+// heads of 128 in bf16.
+constexpr int kHeads = 4;
+
+template <typename T, int D, bool INTER, bool NT>
 __global__ __launch_bounds__(kThreads) void norm_rope_kernel(const NormArgs a, uint32_t q_blocks) {
   constexpr int L = kLanes<D>, R = kGroups<D>;
   const bool is_k = blockIdx.x >= q_blocks;
@@ -134,48 +160,71 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(const NormArgs a, u
   const uint32_t blk = blockIdx.x - (is_k ? q_blocks : 0);
   const int m = threadIdx.x % L;
   const LaneCols lc = lane_cols<INTER>(m, a.rot);
-  const bool on = 8 * m < D;
+  const uint32_t unit = blk * R + threadIdx.x / L;
+  const bool on = 8 * m < D && unit < s.units;
+  const uint32_t token = s.by_chunks.div(unit), h0 = (unit - token * s.chunks) * kHeads;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f}, one = {1.f, 1.f, 1.f, 1.f};
-  f32x4 wa = one, wb = one;
-  if (s.w && on) wa = load4(s.w + lc.a), wb = load4(s.w + lc.b);
-  const uint32_t row0 = blk * (R * kU) + threadIdx.x / L;
-  f32x4 xa[kU], xb[kU], c[kU], sn[kU];
-  RowAt at[kU];
+  int heads = 0, pos = 0;
+  f32x4 xa[kHeads], xb[kHeads];
+  if (on) {
+    heads = s.n - h0 < kHeads ? s.n - h0 : kHeads;
+    const T *x = static_cast<const T *>(s.x) + (long long)token * s.x_row + (size_t)h0 * D;
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const uint32_t row = row0 + u * R;
-    xa[u] = xb[u] = zero;
-    c[u] = one, sn[u] = zero;
-    at[u].pos = -1;
-    if (row < s.rows && on) {
-      at[u] = row_at(a, s, row);
-      const T *x = static_cast<const T *>(s.x) + (long long)at[u].token * s.x_row +
-                   (size_t)at[u].head * D;
-      xa[u] = load4(x + lc.a);
-      xb[u] = load4(x + lc.b);
-      if (lc.turns && at[u].pos >= 0 && at[u].pos < a.table_rows) {
-        const size_t t = (size_t)at[u].pos * (a.rot / 2) + lc.pair;
-        c[u] = load4(a.cos + t);
-        sn[u] = load4(a.sin + t);
+    for (int h = 0; h < kHeads; ++h) {
+      xa[h] = xb[h] = zero;
+      if (h < heads) {
+        xa[h] = load4<NT>(x + h * D + lc.a);
+        xb[h] = load4<NT>(x + h * D + lc.b);
       }
     }
+    pos = a.positions ? a.positions[token] : a.pos0 + (int)(token - a.by_S.div(token) * a.S);
+  }
+  f32x4 ca = one, cb = one, sa = zero, sb = zero;  // y_a = x_a ca + (its partner) sa
+  if (s.w && on) ca = load4(s.w + lc.a), cb = load4(s.w + lc.b);
+  const bool turned = a.rot > 0;
+  if (lc.turns && on) {
+    f32x4 c = one * __builtin_nanf(""), sn = c, wa, wb;
+    if (pos >= 0 && pos < a.table_rows) {
+      const size_t t = (size_t)pos * (a.rot / 2) + lc.pair;
+      c = load4(a.cos + t);
+      sn = load4(a.sin + t);
+    }
+    partners<INTER>(ca, cb, wa, wb);
+    if (INTER) {
+      sa = wa * f32x4{-sn.x, sn.x, -sn.y, sn.y};
+      sb = wb * f32x4{-sn.z, sn.z, -sn.w, sn.w};
+      ca *= f32x4{c.x, c.x, c.y, c.y};
+      cb *= f32x4{c.z, c.z, c.w, c.w};
+    } else {
+      sa = wa * -sn;
+      sb = wb * sn;
+      ca *= c;
+      cb *= c;
+    }
+  } else if (turned && pos >= a.table_rows) {
+    ca = cb = one * __builtin_nanf("");
   }
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const uint32_t row = row0 + u * R;
-    if (s.w) {
-      const float ss = group_sum<L>(dot8(xa[u], xb[u], xa[u], xb[u]));
-      const float r = rsqrtf(ss * (1.f / D) + a.eps);
-      xa[u] *= r * wa;
-      xb[u] *= r * wb;
+  for (int h = 0; h < kHeads; ++h) {
+    f32x4 ya = xa[h] * ca, yb = xb[h] * cb;
+    if (turned) {
+      f32x4 oa, ob;
+      partners<INTER>(xa[h], xb[h], oa, ob);
+      if (a.rot < D && !lc.turns) oa = ob = zero;
+      ya += oa * sa;
+      yb += ob * sb;
     }
-    if (lc.turns) turn<INTER>(xa[u], xb[u], c[u], sn[u]);
-    if (at[u].pos < 0) xa[u] = xb[u] = zero;
-    if (a.rot > 0 && at[u].pos >= a.table_rows) xa[u] = xb[u] = one * __builtin_nanf("");
-    if (row < s.rows && on) {
-      T *y = static_cast<T *>(s.y) + (long long)at[u].token * s.y_row + (size_t)at[u].head * D;
-      store4(y + lc.a, xa[u]);
-      store4(y + lc.b, xb[u]);
+    if (s.w) {
+      const float r =
+          rsqrtf(group_sum<L>(dot8(xa[h], xb[h], xa[h], xb[h])) * (1.f / D) + a.eps);
+      ya *= r;
+      yb *= r;
+    }
+    if (h < heads) {
+      if (pos < 0) ya = yb = zero;
+      T *y = static_cast<T *>(s.y) + (long long)token * s.y_row + (size_t)(h0 + h) * D;
+      store4(y + lc.a, ya);
+      store4(y + lc.b, yb);
     }
   }
 }
@@ -184,7 +233,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(const NormArgs a, u
 // partial sums stay in its eight registers over all rows of its workgroup
 // (rows blk*R.., a grid stride apart); the workgroup's groups are then added
 // in LDS in a fixed order and written as one row of `partials`.
-template <typename TX, typename TG, int D, bool INTER>
+template <typename TX, typename TG, int D, bool INTER, bool NT>
 __global__ __launch_bounds__(kThreads) void norm_rope_bwd_kernel(const NormArgs a,
                                                                  float *partials,
                                                                  uint32_t q_blocks) {
@@ -210,13 +259,13 @@ __global__ __launch_bounds__(kThreads) void norm_rope_bwd_kernel(const NormArgs 
       at = row_at(a, s, (uint32_t)row);
       if (at.pos >= 0) {
         const TG *dy = static_cast<const TG *>(s.dy) + row * D;
-        za = load4(dy + lc.a);
-        zb = load4(dy + lc.b);
+        za = load4<NT>(dy + lc.a);
+        zb = load4<NT>(dy + lc.b);
         if (s.w) {
           const TX *x = static_cast<const TX *>(s.x) + (long long)at.token * s.x_row +
                         (size_t)at.head * D;
-          xa = load4(x + lc.a);
-          xb = load4(x + lc.b);
+          xa = load4<NT>(x + lc.a);
+          xb = load4<NT>(x + lc.b);
         }
         if (lc.turns && at.pos < a.table_rows) {
           const size_t t = (size_t)at.pos * (a.rot / 2) + lc.pair;
@@ -248,8 +297,8 @@ __global__ __launch_bounds__(kThreads) void norm_rope_bwd_kernel(const NormArgs 
   __shared__ float part[R][D];
   if (on) {
     float *p = part[threadIdx.x / L];
-    store4(p + lc.a, dwa);
-    store4(p + lc.b, dwb);
+    *reinterpret_cast<f32x4 *>(p + lc.a) = dwa;
+    *reinterpret_cast<f32x4 *>(p + lc.b) = dwb;
   }
   __syncthreads();
   for (int e = threadIdx.x; e < D; e += kThreads) {
@@ -282,39 +331,54 @@ __global__ __launch_bounds__(kThreads) void norm_dw_kernel(const NormArgs a, con
   }
 }
 
-template <typename T, int D>
-hipError_t fwd_typed(const NormArgs &a, bool interleaved, hipStream_t stream) {
-  const uint64_t per = kGroups<D> * kU;
-  const uint64_t qb = (a.side[0].rows + per - 1) / per, kb = (a.side[1].rows + per - 1) / per;
+// Whether a call's inputs are read with the non-temporal hint: where what it
+// moves (`bytes`) does not stay in the 256 MB of the last-level cache anyway.  128K
+// tokens of 8 + 1 heads of 128 in bf16 (604 MB): 130 -> 120 us, their backward 301 ->
+// 269; but 4K tokens of 8 + 2 heads (21 MB, the inputs still cached) 6.6 -> 7.1,
+// backward 16.2 -> 17.6.  Results are stored with the hint always (137 -> 130, 4K
+// tokens 7.6 -> 6.6).
+bool streams(const NormArgs &a, int d, int bytes_per_element) {
+  return ((uint64_t)a.side[0].rows + a.side[1].rows) * d * bytes_per_element > 192ull << 20;
+}
+
+template <typename T, int D, bool INTER>
+hipError_t fwd_typed(const NormArgs &a, bool nt, hipStream_t stream) {
+  const uint64_t per = kGroups<D>;
+  const uint64_t qb = (a.side[0].units + per - 1) / per, kb = (a.side[1].units + per - 1) / per;
   const dim3 grid((unsigned)(qb + kb));
-  if (interleaved)
-    hipLaunchKernelGGL((norm_rope_kernel<T, D, true>), grid, dim3(kThreads), 0, stream, a,
+  if (nt)
+    hipLaunchKernelGGL((norm_rope_kernel<T, D, INTER, true>), grid, dim3(kThreads), 0, stream, a,
                        (uint32_t)qb);
   else
-    hipLaunchKernelGGL((norm_rope_kernel<T, D, false>), grid, dim3(kThreads), 0, stream, a,
+    hipLaunchKernelGGL((norm_rope_kernel<T, D, INTER, false>), grid, dim3(kThreads), 0, stream, a,
                        (uint32_t)qb);
   return hipGetLastError();
 }
 
+template <typename T, int D>
+hipError_t fwd_order(const NormArgs &a, bool interleaved, bool nt, hipStream_t stream) {
+  return interleaved ? fwd_typed<T, D, true>(a, nt, stream) : fwd_typed<T, D, false>(a, nt, stream);
+}
+
 template <typename T>
-hipError_t fwd_dim(const NormArgs &a, int d, bool interleaved, hipStream_t stream) {
+hipError_t fwd_dim(const NormArgs &a, int d, bool interleaved, bool nt, hipStream_t stream) {
   switch (d) {
-    case 64: return fwd_typed<T, 64>(a, interleaved, stream);
-    case 80: return fwd_typed<T, 80>(a, interleaved, stream);
-    case 96: return fwd_typed<T, 96>(a, interleaved, stream);
-    default: return fwd_typed<T, 128>(a, interleaved, stream);
+    case 64: return fwd_order<T, 64>(a, interleaved, nt, stream);
+    case 80: return fwd_order<T, 80>(a, interleaved, nt, stream);
+    case 96: return fwd_order<T, 96>(a, interleaved, nt, stream);
+    default: return fwd_order<T, 128>(a, interleaved, nt, stream);
   }
 }
 
-template <typename TX, typename TG, int D>
-hipError_t bwd_typed(const NormArgs &a, float *partials, bool interleaved, hipStream_t stream) {
+template <typename TX, typename TG, int D, bool INTER>
+hipError_t bwd_typed(const NormArgs &a, float *partials, bool nt, hipStream_t stream) {
   const uint32_t qb = norm_bwd_blocks(a.side[0].rows, D), kb = norm_bwd_blocks(a.side[1].rows, D);
-  if (interleaved)
-    hipLaunchKernelGGL((norm_rope_bwd_kernel<TX, TG, D, true>), dim3(qb + kb), dim3(kThreads), 0,
-                       stream, a, partials, qb);
+  if (nt)
+    hipLaunchKernelGGL((norm_rope_bwd_kernel<TX, TG, D, INTER, true>), dim3(qb + kb), dim3(kThreads),
+                       0, stream, a, partials, qb);
   else
-    hipLaunchKernelGGL((norm_rope_bwd_kernel<TX, TG, D, false>), dim3(qb + kb), dim3(kThreads), 0,
-                       stream, a, partials, qb);
+    hipLaunchKernelGGL((norm_rope_bwd_kernel<TX, TG, D, INTER, false>), dim3(qb + kb),
+                       dim3(kThreads), 0, stream, a, partials, qb);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.side[0].w) return e;
   hipLaunchKernelGGL((norm_dw_kernel<D>), dim3(D / 16, 2), dim3(kThreads), 0, stream, a, partials,
@@ -322,23 +386,35 @@ hipError_t bwd_typed(const NormArgs &a, float *partials, bool interleaved, hipSt
   return hipGetLastError();
 }
 
+template <typename TX, typename TG, int D>
+hipError_t bwd_order(const NormArgs &a, float *partials, bool interleaved, bool nt,
+                     hipStream_t stream) {
+  return interleaved ? bwd_typed<TX, TG, D, true>(a, partials, nt, stream)
+                     : bwd_typed<TX, TG, D, false>(a, partials, nt, stream);
+}
+
 template <typename TX, typename TG>
-hipError_t bwd_dim(const NormArgs &a, float *partials, int d, bool interleaved,
+hipError_t bwd_dim(const NormArgs &a, float *partials, int d, bool interleaved, bool nt,
                    hipStream_t stream) {
   switch (d) {
-    case 64: return bwd_typed<TX, TG, 64>(a, partials, interleaved, stream);
-    case 80: return bwd_typed<TX, TG, 80>(a, partials, interleaved, stream);
-    case 96: return bwd_typed<TX, TG, 96>(a, partials, interleaved, stream);
-    default: return bwd_typed<TX, TG, 128>(a, partials, interleaved, stream);
+    case 64: return bwd_order<TX, TG, 64>(a, partials, interleaved, nt, stream);
+    case 80: return bwd_order<TX, TG, 80>(a, partials, interleaved, nt, stream);
+    case 96: return bwd_order<TX, TG, 96>(a, partials, interleaved, nt, stream);
+    default: return bwd_order<TX, TG, 128>(a, partials, interleaved, nt, stream);
   }
 }
 
 }  // namespace
 
-hipError_t launch_norm_rope(const NormArgs &a, int d, bool interleaved, bool f32,
-                            hipStream_t stream) {
-  return f32 ? fwd_dim<float>(a, d, interleaved, stream)
-             : fwd_dim<uint16_t>(a, d, interleaved, stream);
+hipError_t launch_norm_rope(NormArgs a, int d, bool interleaved, bool f32, hipStream_t stream) {
+  for (NormSide &s : a.side) {
+    s.chunks = (s.n + kHeads - 1) / kHeads;
+    s.by_chunks = FastDiv::make(s.chunks);
+    s.units = s.rows / s.n * s.chunks;
+  }
+  const bool nt = streams(a, d, f32 ? 8 : 4);
+  return f32 ? fwd_dim<float>(a, d, interleaved, nt, stream)
+             : fwd_dim<uint16_t>(a, d, interleaved, nt, stream);
 }
 
 int norm_bwd_blocks(uint32_t rows, int d) {
@@ -349,11 +425,12 @@ int norm_bwd_blocks(uint32_t rows, int d) {
 
 hipError_t launch_norm_rope_bwd(const NormArgs &a, float *partials, int d, bool interleaved,
                                 bool f32, bool grad_f32, hipStream_t stream) {
+  const bool nt = streams(a, d, (f32 ? 4 : 2) + (grad_f32 ? 8 : 4));
   if (f32)
-    return grad_f32 ? bwd_dim<float, float>(a, partials, d, interleaved, stream)
-                    : bwd_dim<float, uint16_t>(a, partials, d, interleaved, stream);
-  return grad_f32 ? bwd_dim<uint16_t, float>(a, partials, d, interleaved, stream)
-                  : bwd_dim<uint16_t, uint16_t>(a, partials, d, interleaved, stream);
+    return grad_f32 ? bwd_dim<float, float>(a, partials, d, interleaved, nt, stream)
+                    : bwd_dim<float, uint16_t>(a, partials, d, interleaved, nt, stream);
+  return grad_f32 ? bwd_dim<uint16_t, float>(a, partials, d, interleaved, nt, stream)
+                  : bwd_dim<uint16_t, uint16_t>(a, partials, d, interleaved, nt, stream);
 }
 
 }  // namespace basp

@@ -22,6 +22,8 @@ struct NormSide {
   uint32_t rows;     // tokens * n
   FastDiv by_n;      // division by n
   uint32_t n;
+  uint32_t units, chunks;  // forward: (token, chunk of heads), chunks per token
+  FastDiv by_chunks;
   long long x_row, y_row;
 };
 
@@ -35,8 +37,7 @@ struct NormArgs {
   float eps;
 };
 
-hipError_t launch_norm_rope(const NormArgs &a, int d, bool interleaved, bool f32,
-                            hipStream_t stream);
+hipError_t launch_norm_rope(NormArgs a, int d, bool interleaved, bool f32, hipStream_t stream);
 
 // Workgroups of the backward for a tensor of `rows` rows of d elements; each
 // writes one partial sum of dw.
