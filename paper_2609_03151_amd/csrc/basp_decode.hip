@@ -131,6 +131,14 @@ template <typename T>
 __device__ __forceinline__ T load_at(gptr base, uint32_t off) {
   return *(const __attribute__((address_space(1))) T *)(base + off);
 }
+// The same with the non-temporal hint: for V, whose rows a load reads whole.  K's
+// loads read half a cache line each, and with the hint the line is fetched twice
+// (64 ragged sequences of up to 32K tokens: none 198 us, V 178, both 269 in an
+// earlier form; K by way of LDS in whole rows, both with the hint, 178).
+template <typename T>
+__device__ __forceinline__ T load_once(gptr base, uint32_t off) {
+  return __builtin_nontemporal_load((const __attribute__((address_space(1))) T *)(base + off));
+}
 
 // An entry of the block table or of lens: a load through the scalar cache, which
 // the counter that the pages' loads are waited by does not see (nothing writes
@@ -191,13 +199,13 @@ __device__ __forceinline__ void load_block(Block<D, E4M3> &b, const Pages &p, in
       const int r = 4 * c + e;
       const uint32_t o = (uint32_t)(r < last ? r : last) * B::kRowBytes + vc;
       if constexpr (B::kWords == 4) {
-        const u32x4 x = load_at<u32x4>(vb, o);
+        const u32x4 x = load_once<u32x4>(vb, o);
         v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
       } else if constexpr (B::kWords == 2) {
-        const u32x2 x = load_at<u32x2>(vb, o);
+        const u32x2 x = load_once<u32x2>(vb, o);
         v[0] = x.x, v[1] = x.y;
       } else {
-        v[0] = load_at<uint32_t>(vb, o);
+        v[0] = load_once<uint32_t>(vb, o);
       }
     }
     if constexpr (E4M3) {
@@ -365,7 +373,7 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
   const int wave = scalar(threadIdx.x / 64);
   const int lane = threadIdx.x % 64, m = lane % 16, c = lane / 16;
   __shared__ float so[kWaves][kRows][D + 4], sm[kWaves][kRows], sl[kWaves][kRows];
-  __shared__ int sums[kWaves], found[2];
+  __shared__ int sums[kWaves], found[3];
 
   const Partials ps = partials_at(a.workspace, opens, G);
   const bool joins = a.workspace != nullptr, by_head = joins && opens != G;
@@ -386,7 +394,8 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
   };
 
   // All units, and this workgroup's run [begin, end).
-  const int n0 = (int)threadIdx.x < b ? units_of<B>(a.lens[threadIdx.x], a.max_len) : 0;
+  const int len0 = (int)threadIdx.x < b ? a.lens[threadIdx.x] : 0;
+  const int n0 = units_of<B>(len0, a.max_len);
   int mine = n0;
   for (int s = threadIdx.x + kThreads; s < b; s += kThreads)
     mine += units_of<B>(a.lens[s], a.max_len);
@@ -406,24 +415,25 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
   int base = 0;
   for (int s0 = 0;; s0 += kThreads) {
     const int s = s0 + threadIdx.x;
-    int n = n0, x = mine;
+    int len = len0, n = n0, x = mine;
     if (b > kThreads) {  // else the sums above are those of the one chunk
       __syncthreads();   // sums, read above or in the last turn
-      if (s0 > 0) n = s < b ? units_of<B>(a.lens[s], a.max_len) : 0;
+      if (s0 > 0) len = s < b ? a.lens[s] : 0, n = units_of<B>(len, a.max_len);
       x = wave_scan(n);
       if (lane == 63) sums[wave] = x;
       __syncthreads();
     }
     x += base;
     for (int w = 0; w < wave; ++w) x += sums[w];
-    if (begin >= R * (x - n) && begin < R * x) found[0] = s, found[1] = begin - R * (x - n);
+    if (begin >= R * (x - n) && begin < R * x)
+      found[0] = s, found[1] = begin - R * (x - n), found[2] = len;
     base += sums[0] + sums[1] + sums[2] + sums[3];
     if (begin < R * base) break;  // some thread of this chunk has found it
     if (s0 + kThreads >= b) return;  // not reached while lens stays as it is
   }
   __syncthreads();
   int seq = scalar(found[0]);
-  int n = units_of<B>(scalar_load(a.lens, seq), a.max_len);  // units of a head of it
+  int len = scalar(found[2]), n = units_of<B>(len, a.max_len);  // n: units of a head of it
   int head = scalar(found[1] / n), u = scalar(found[1] % n);
 
   Pages pg;
@@ -440,7 +450,6 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
 
   for (int pos = begin; pos < end;) {
     const int take = n - u < end - pos ? n - u : end - pos;  // units of this head
-    const int len = scalar_load(a.lens, seq);
     const int lo = u * kUnit<B>;
     const int hi = (u + take) * kUnit<B> < len ? (u + take) * kUnit<B> : len;
     const int kvh = scalar(head / row_groups), grp = scalar(head % row_groups);
@@ -531,7 +540,10 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
       if (++head == R) {
         head = 0;
         n = 0;
-        while (n == 0 && ++seq < b) n = units_of<B>(scalar_load(a.lens, seq), a.max_len);
+        while (n == 0 && ++seq < b) {
+          len = scalar_load(a.lens, seq);
+          n = units_of<B>(len, a.max_len);
+        }
         if (n == 0) break;  // not reached while lens stays as it is
       }
     }
@@ -541,11 +553,12 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
 }
 
 // One row of one head with several partial results: these in turn over 8 C groups of
-// 32 / C threads, 4 elements of d a thread; C workgroups share the row's elements.
+// 32 / C threads, 4 elements of d a thread, each group with a running maximum; C
+// workgroups share the row's elements.
 template <int D, int C>
 __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs a, int opens,
                                                                int groups) {
-  constexpr int L = 32 / C, R = kThreads / L;
+  constexpr int L = 32 / C, R = kThreads / L, kAtOnce = 4;
   const Partials p = partials_at(a.workspace, opens, groups);
   const Open open = p.open[blockIdx.x];
   const int h = blockIdx.y;
@@ -555,37 +568,63 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs 
     return (size_t)(i ? (open.first | 1) - 1 + 2 * i : open.first) * kRows + h;
   };
   const int g = threadIdx.x / L, col = blockIdx.z * (4 * L) + threadIdx.x % L * 4;
-  __shared__ float so[R][4 * L + 4], sl[R], sm[kWaves];
-  float M = -INFINITY;
-  for (int i = threadIdx.x; i < n; i += kThreads) M = fmaxf(M, p.ml[at(i)].x);
-#pragma unroll
-  for (int x = 32; x; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
-  if (threadIdx.x % 64 == 0) sm[threadIdx.x / 64] = M;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sm[w]);
-  const float ref = M == -INFINITY ? 0.f : M;
+  __shared__ float so[kWaves][4 * L + 4], sm[kWaves], sl[kWaves];
   f32x4 O = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-#pragma unroll 4
-  for (int i = g; i < n; i += R) {
-    const f32x2 x = p.ml[at(i)];
-    const float f = fast_exp2(x.x - ref);
-    l += f * x.y;
-    if (col < D) O += f * *reinterpret_cast<const f32x4 *>(p.o + at(i) * D + col);
+  float M = -INFINITY, l = 0.f;
+  for (int i0 = g; i0 < n; i0 += kAtOnce * R) {
+    f32x2 x[kAtOnce];
+    f32x4 o[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int i = i0 + u * R < n ? i0 + u * R : i0;  // again the first: dropped below
+      x[u] = p.ml[at(i)];
+      o[u] = *reinterpret_cast<const f32x4 *>(p.o + at(i) * D + (col < D ? col : 0));
+    }
+    float mx = fmaxf(M, x[0].x);
+#pragma unroll
+    for (int u = 1; u < kAtOnce; ++u) mx = fmaxf(mx, x[u].x);
+    const float ref = mx == -INFINITY ? 0.f : mx, f = fast_exp2(M - ref);
+    M = mx;
+    l *= f;
+    O *= f;
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+      if (i0 + u * R < n) {
+        const float w = fast_exp2(x[u].x - ref);
+        l += w * x[u].y;
+        O += w * o[u];
+      }
   }
-  *reinterpret_cast<f32x4 *>(&so[g][threadIdx.x % L * 4]) = O;
-  if (threadIdx.x % L == 0) sl[g] = l;
+  // the groups of a wave, then the waves
+  float mx = M;
+#pragma unroll
+  for (int x = 32; x >= L; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
+  const float f = fast_exp2(M - (mx == -INFINITY ? 0.f : mx));
+  l *= f;
+  O *= f;
+#pragma unroll
+  for (int x = 32; x >= L; x >>= 1) {
+    l += __shfl_xor(l, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) O[i] += __shfl_xor(O[i], x);
+  }
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  if (lane < L) *reinterpret_cast<f32x4 *>(&so[wave][4 * lane]) = O;
+  if (lane == 0) sm[wave] = mx, sl[wave] = l;
   __syncthreads();
   const int e = blockIdx.z * (4 * L) + threadIdx.x * 2;
   if (threadIdx.x < 2 * L && e < D) {
+    M = sm[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm[w]);
     float A = 0.f, Bb = 0.f;
     l = 0.f;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      A += so[i][threadIdx.x * 2];
-      Bb += so[i][threadIdx.x * 2 + 1];
-      l += sl[i];
+    for (int w = 0; w < kWaves; ++w) {
+      const float fw = fast_exp2(sm[w] - (M == -INFINITY ? 0.f : M));
+      A += fw * so[w][threadIdx.x * 2];
+      Bb += fw * so[w][threadIdx.x * 2 + 1];
+      l += fw * sl[w];
     }
     const float inv = 1.f / l;
     const size_t r = (size_t)open.row0 + h;
