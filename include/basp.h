@@ -481,7 +481,7 @@ int basp_qk_norm_rope_bwd(const void *q, const void *k, const void *dqo, const v
  * A sequence with start[s] < 0 is skipped, and so are tokens whose position is
  * past the table or whose page number is outside [0, n_pages); every other byte of
  * the pages and scales stays as it was.  Also SHAPE when k_row < n_k*d, and
- * UNSUPPORTED when b*T*n_k >= 2^28. */
+ * UNSUPPORTED when b*T*n_k >= 2^27. */
 int basp_kv_write(const void *k, const void *v, void *k_pages, void *v_pages,
                   unsigned char *k_scales, unsigned char *v_scales, const int *block_table,
                   const int *start, const int *count, int b, int T, int n_k, int d, int page,
@@ -492,7 +492,7 @@ int basp_kv_write(const void *k, const void *v, void *k_pages, void *v_pages,
  * (start NULL: 0, count NULL: T) into k and v (bf16, [b, T, n_k, d], contiguous,
  * 16-byte aligned).  Rows t >= count[s], and all rows of a sequence with
  * start[s] < 0, are zeros; rows past the table or on a page number outside
- * [0, n_pages) are NaN.  UNSUPPORTED when b*T*n_k >= 2^28. */
+ * [0, n_pages) are NaN.  UNSUPPORTED when b*T*n_k >= 2^27. */
 int basp_kv_read(const void *k_pages, const void *v_pages, const unsigned char *k_scales,
                  const unsigned char *v_scales, const int *block_table, const int *start,
                  const int *count, void *k, void *v, int b, int T, int n_k, int d, int page,

@@ -610,8 +610,14 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, eps: fl
     gq, gk = _on(dq_out, "dq_out", gt, q_shape, dev), _on(dk_out, "dk_out", gt, k_shape, dev)
     if dq is None:
         dq = torch.empty_like(dq_out)
+        dqp = dq.data_ptr()
+    else:
+        dqp = _on(dq, "dq", gt, q_shape, dev)
     if dk is None:
         dk = torch.empty_like(dk_out)
+        dkp = dk.data_ptr()
+    else:
+        dkp = _on(dk, "dk", gt, k_shape, dev)
     L = _lib or lib()
     dqw = dkw = ws = ws_n = None
     if q_weight is None:
@@ -620,19 +626,22 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, eps: fl
     else:
         if dq_weight is None:
             dq_weight = torch.empty_like(q_weight)
+            dqw = dq_weight.data_ptr()
+        else:
+            dqw = _on(dq_weight, "dq_weight", _F32, (d,), dev)
         if dk_weight is None:
             dk_weight = torch.empty_like(k_weight)
+            dkw = dk_weight.data_ptr()
+        else:
+            dkw = _on(dk_weight, "dk_weight", _F32, (d,), dev)
         if b * S == 0:
             dq_weight.zero_()
             dk_weight.zero_()
-        dqw = _on(dq_weight, "dq_weight", _F32, (d,), dev)
-        dkw = _on(dk_weight, "dk_weight", _F32, (d,), dev)
         need = 0 if workspace is not None else L.basp_qk_norm_rope_bwd_workspace_bytes(
             b, S, n_q, n_k, d)
         workspace, ws, ws_n = _space(workspace, need, q, dev)
-    _call("basp_qk_norm_rope_bwd", L.basp_qk_norm_rope_bwd, dev, qp, kp, gq, gk,
-          _on(dq, "dq", gt, q_shape, dev), _on(dk, "dk", gt, k_shape, dev), *w, dqw, dkw, *turn, ws,
-          ws_n, *dims, q_row, k_row, eps, pos0, interleaved, code, gcode)
+    _call("basp_qk_norm_rope_bwd", L.basp_qk_norm_rope_bwd, dev, qp, kp, gq, gk, dqp, dkp, *w, dqw,
+          dkw, *turn, ws, ws_n, *dims, q_row, k_row, eps, pos0, interleaved, code, gcode)
     return dq, dk, dq_weight, dk_weight
 
 
@@ -707,12 +716,18 @@ def kv_read(k_pages, v_pages, block_table, T: int, start=None, count=None, k_sca
     shape = (b, T, dims[0], dims[1])
     if k is None:
         k = block_table.new_empty(shape, dtype=_BF)
+        kp = k.data_ptr()
+    else:
+        kp = _on(k, "k", _BF, shape, dev)
     if v is None:
-        v = torch.empty_like(k)
+        v = block_table.new_empty(shape, dtype=_BF)
+        vp = v.data_ptr()
+    else:
+        vp = _on(v, "v", _BF, shape, dev)
     _call("basp_kv_read", (_lib or lib()).basp_kv_read, dev, *ptrs,
           None if start is None else _on(start, "start", _I32, (b,), dev),
-          None if count is None else _on(count, "count", _I32, (b,), dev),
-          _on(k, "k", _BF, shape, dev), _on(v, "v", _BF, shape, dev), b, T, *dims, code)
+          None if count is None else _on(count, "count", _I32, (b,), dev), kp, vp, b, T, *dims,
+          code)
     return k, v
 
 
@@ -742,13 +757,18 @@ def attn_decode(q, k_pages, v_pages, block_table, lens, scale: float | None = No
     qp, q_row = _rows(q, "q", _BF, shape, dev)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        op = out.data_ptr()
+    else:
+        op = _on(out, "out", _BF, shape, dev)
     if lse is None:
         lse = q.new_empty((b, n_q), dtype=_F32)
+        lp = lse.data_ptr()
+    else:
+        lp = _on(lse, "lse", _F32, (b, n_q), dev)
     L = _lib or lib()
     need = 0 if workspace is not None else L.basp_attn_decode_workspace_bytes(b, n_q, n_k, d,
                                                                               max_len)
     workspace, ws, ws_n = _space(workspace, need, q, dev)
     _call("basp_attn_decode", L.basp_attn_decode, dev, qp, *ptrs, _on(lens, "lens", _I32, (b,), dev),
-          _on(out, "out", _BF, shape, dev), _on(lse, "lse", _F32, (b, n_q), dev), ws, ws_n, b, n_q,
-          n_k, d, page, n_pages, max_pages, max_len, q_row, float(scale), code)
+          op, lp, ws, ws_n, b, n_q, n_k, d, page, n_pages, max_pages, max_len, q_row, scale, code)
     return out, lse

@@ -202,8 +202,8 @@ int run_cache(bool write, const void *k, const void *v, const void *k_pages, con
   if (rc) return rc;
   if (k_row < (long long)n_k * d || v_row < (long long)n_k * d) return BASP_ERR_SHAPE;
   if ((uint64_t)b * (uint64_t)T == 0) return BASP_OK;  // empty: no pointer is inspected
-  // A launch's threads are a 32-bit count, eight of them a (token, head).
-  const uint64_t rows = rows_of(b, T, n_k, 28);
+  // A launch's threads are a 32-bit count, 16 of them a (token, head).
+  const uint64_t rows = rows_of(b, T, n_k, 27);
   if (rows == 0) return BASP_ERR_UNSUPPORTED;
   if (!k || !v || (write && !start)) return BASP_ERR_NULL;
   rc = check_pages(k_pages, v_pages, k_scales, v_scales, table, cache_dtype);

@@ -13,6 +13,11 @@
 //
 // Both kernels are bound by HBM: one group of 16 lanes (8 at d = 64) per token
 // and head moves its K and its V row, eight elements a lane (16 bytes of bf16).
+// Two such pairs of rows per group are slower (a call of 16K rows: 17.2 us
+// against 16.1 for write and read), four more so.  What is read back is stored with
+// the non-temporal hint (256K tokens of 2 heads in bf16, both calls: 171 us
+// without, 149 with), pages are not (157 with: the 8- and 16-byte stores of a row
+// come together in the cache).
 #include "basp_device.hpp"
 #include "basp_ops.hpp"
 
@@ -21,7 +26,6 @@ namespace basp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kU = 2;  // (token, head) pairs in flight per group
 
 template <int D>
 constexpr int kLanes = D <= 64 ? 8 : 16;
@@ -90,54 +94,46 @@ __device__ __forceinline__ bool find_row(const CacheArgs &a, uint32_t s, long lo
 
 template <int D, bool E4M3>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(const CacheArgs a) {
-  constexpr int L = kLanes<D>, R = kThreads / L;
+  constexpr int L = kLanes<D>;
   const int m = threadIdx.x % L;
-  const uint32_t i0 = blockIdx.x * (R * kU) + threadIdx.x / L;
-  u32x4 x[kU][2];
-  size_t row[kU];
-  bool live[kU];
+  const uint32_t i = blockIdx.x * (kThreads / L) + threadIdx.x / L;  // (token, head)
+  u32x4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  size_t row = 0;
+  bool live = false;
+  if (i < a.rows) {
+    const uint32_t token = a.by_n.div(i), h = i - token * a.s.n_k;
+    const uint32_t s = a.by_T.div(token), t = token - s * a.T;
+    const int start = a.start[s];
+    if (start >= 0 && (!a.count || (int)t < a.count[s]))
+      live = find_row(a, s, (long long)start + t, h, row);
+    live = live && 8 * m < D;
+    if (live)
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const uint32_t i = i0 + u * R;
-    live[u] = false;
-    x[u][0] = x[u][1] = u32x4{0, 0, 0, 0};
-    if (i < a.rows) {
-      const uint32_t token = a.by_n.div(i), h = i - token * a.s.n_k;
-      const uint32_t s = a.by_T.div(token), t = token - s * a.T;
-      const int start = a.start[s];
-      if (start >= 0 && (!a.count || (int)t < a.count[s]))
-        live[u] = find_row(a, s, (long long)start + t, h, row[u]);
-      if (live[u] && 8 * m < D)
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-          x[u][w] = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.x[w]) +
-                                                     (long long)token * a.x_row[w] +
-                                                     (size_t)h * D + 8 * m);
-    }
+      for (int w = 0; w < 2; ++w)
+        x[w] = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.x[w]) +
+                                                (long long)token * a.x_row[w] + (size_t)h * D +
+                                                8 * m);
   }
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      u32x4 v = x[u][w];
-      if constexpr (E4M3) {
-        uint32_t mag = mag2(v.x);
-        mag = mag2(v.y) > mag ? mag2(v.y) : mag;
-        mag = mag2(v.z) > mag ? mag2(v.z) : mag;
-        mag = mag2(v.w) > mag ? mag2(v.w) : mag;
-        const uint32_t byte = scale_byte(group_max<L>(mag));
-        if (byte == 247)  // e = 120, the largest
-          v = u32x4{below_top(v.x), below_top(v.y), below_top(v.z), below_top(v.w)};
-        const float f = pow2_of_byte(254 - byte);  // 2^-e
-        const u32x2 q = {(uint32_t)pack_e4m3<true>(v.y, f, pack_e4m3<false>(v.x, f, 0)),
-                         (uint32_t)pack_e4m3<true>(v.w, f, pack_e4m3<false>(v.z, f, 0))};
-        if (live[u] && 8 * m < D) {
-          *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.pages[w]) + row[u] * D + 8 * m) = q;
-          if (m == 0) a.scales[w][row[u]] = (uint8_t)byte;
-        }
-      } else if (live[u] && 8 * m < D) {
-        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.pages[w]) + row[u] * D + 8 * m) = v;
+  for (int w = 0; w < 2; ++w) {
+    u32x4 v = x[w];
+    if constexpr (E4M3) {
+      uint32_t mag = mag2(v.x);
+      mag = mag2(v.y) > mag ? mag2(v.y) : mag;
+      mag = mag2(v.z) > mag ? mag2(v.z) : mag;
+      mag = mag2(v.w) > mag ? mag2(v.w) : mag;
+      const uint32_t byte = scale_byte(group_max<L>(mag));
+      if (byte == 247)  // e = 120, the largest
+        v = u32x4{below_top(v.x), below_top(v.y), below_top(v.z), below_top(v.w)};
+      const float f = pow2_of_byte(254 - byte);  // 2^-e
+      const u32x2 q = {(uint32_t)pack_e4m3<true>(v.y, f, pack_e4m3<false>(v.x, f, 0)),
+                       (uint32_t)pack_e4m3<true>(v.w, f, pack_e4m3<false>(v.z, f, 0))};
+      if (live) {
+        *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.pages[w]) + row * D + 8 * m) = q;
+        if (m == 0) a.scales[w][row] = (uint8_t)byte;
       }
+    } else if (live) {
+      *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.pages[w]) + row * D + 8 * m) = v;
     }
   }
 }
@@ -152,60 +148,48 @@ __device__ __forceinline__ uint32_t unpack_e4m3(uint32_t w, float f) {
 
 template <int D, bool E4M3>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(const CacheArgs a) {
-  constexpr int L = kLanes<D>, R = kThreads / L;
+  constexpr int L = kLanes<D>;
   const int m = threadIdx.x % L;
-  const uint32_t i0 = blockIdx.x * (R * kU) + threadIdx.x / L;
-  u32x4 x[kU][2];
-  float f[kU][2];
+  const uint32_t i = blockIdx.x * (kThreads / L) + threadIdx.x / L;  // (token, head)
+  if (i >= a.rows || 8 * m >= D) return;
+  u32x4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+  float f[2] = {1.f, 1.f};
+  const uint32_t token = a.by_n.div(i), h = i - token * a.s.n_k;
+  const uint32_t s = a.by_T.div(token), t = token - s * a.T;
+  const int start = a.start ? a.start[s] : 0;
+  if (start >= 0 && (!a.count || (int)t < a.count[s])) {
+    size_t row;
+    if (find_row(a, s, (long long)start + t, h, row)) {
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const uint32_t i = i0 + u * R;
-    x[u][0] = x[u][1] = u32x4{0, 0, 0, 0};
-    f[u][0] = f[u][1] = 1.f;
-    if (i < a.rows && 8 * m < D) {
-      const uint32_t token = a.by_n.div(i), h = i - token * a.s.n_k;
-      const uint32_t s = a.by_T.div(token), t = token - s * a.T;
-      const int start = a.start ? a.start[s] : 0;
-      if (start >= 0 && (!a.count || (int)t < a.count[s])) {
-        size_t row;
-        if (find_row(a, s, (long long)start + t, h, row)) {
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            if constexpr (E4M3) {
-              const u32x2 q = *reinterpret_cast<const u32x2 *>(
-                  static_cast<const uint8_t *>(a.pages[w]) + row * D + 8 * m);
-              x[u][w].x = q.x, x[u][w].y = q.y;
-              f[u][w] = pow2_of_byte(a.scales[w][row]);
-            } else {
-              x[u][w] = *reinterpret_cast<const u32x4 *>(
-                  static_cast<const uint16_t *>(a.pages[w]) + row * D + 8 * m);
-            }
-          }
-        } else {  // NaN: bf16 0x7FFF, and as e4m3 bytes
-          x[u][0] = x[u][1] = u32x4{0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu};
+      for (int w = 0; w < 2; ++w) {
+        if constexpr (E4M3) {
+          const u32x2 q = *reinterpret_cast<const u32x2 *>(
+              static_cast<const uint8_t *>(a.pages[w]) + row * D + 8 * m);
+          x[w].x = q.x, x[w].y = q.y;
+          f[w] = pow2_of_byte(a.scales[w][row]);
+        } else {
+          x[w] = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.pages[w]) +
+                                                  row * D + 8 * m);
         }
       }
+    } else {  // NaN: bf16 0x7FFF, and as e4m3 bytes
+      x[0] = x[1] = u32x4{0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu};
     }
   }
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const uint32_t i = i0 + u * R;
-    if (i < a.rows && 8 * m < D) {
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        u32x4 v = x[u][w];
-        if constexpr (E4M3)
-          v = u32x4{unpack_e4m3<false>(v.x, f[u][w]), unpack_e4m3<true>(v.x, f[u][w]),
-                    unpack_e4m3<false>(v.y, f[u][w]), unpack_e4m3<true>(v.y, f[u][w])};
-        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.x[w]) + (size_t)i * D + 8 * m) = v;
-      }
-    }
+  for (int w = 0; w < 2; ++w) {
+    u32x4 v = x[w];
+    if constexpr (E4M3)
+      v = u32x4{unpack_e4m3<false>(v.x, f[w]), unpack_e4m3<true>(v.x, f[w]),
+                unpack_e4m3<false>(v.y, f[w]), unpack_e4m3<true>(v.y, f[w])};
+    __builtin_nontemporal_store(
+        v, reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.x[w]) + (size_t)i * D + 8 * m));
   }
 }
 
 template <int D>
 hipError_t write_dim(const CacheArgs &a, hipStream_t stream) {
-  const uint32_t per = kThreads / kLanes<D> * kU;
+  const uint32_t per = kThreads / kLanes<D>;
   const dim3 grid((unsigned)(((uint64_t)a.rows + per - 1) / per));
   if (a.s.e4m3)
     hipLaunchKernelGGL((kv_write_kernel<D, true>), grid, dim3(kThreads), 0, stream, a);
@@ -216,7 +200,7 @@ hipError_t write_dim(const CacheArgs &a, hipStream_t stream) {
 
 template <int D>
 hipError_t read_dim(const CacheArgs &a, hipStream_t stream) {
-  const uint32_t per = kThreads / kLanes<D> * kU;
+  const uint32_t per = kThreads / kLanes<D>;
   const dim3 grid((unsigned)(((uint64_t)a.rows + per - 1) / per));
   if (a.s.e4m3)
     hipLaunchKernelGGL((kv_read_kernel<D, true>), grid, dim3(kThreads), 0, stream, a);
