@@ -468,6 +468,11 @@ def _call(name: str, fn, dev: int, *args):
         raise BaspError(rc, name)
 
 
+def _int(x: int) -> int:
+    """A size as a C int: -1, which the library refuses, for one that does not fit."""
+    return x if -1 < x < 1 << 31 else -1
+
+
 def _device(t, name: str, dims: int) -> int:
     """Device index of a call's first tensor, of this many dimensions; below zero for a host tensor,
     which _call refuses."""
@@ -585,7 +590,7 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, eps: float = 1e-6, position
     else:
         kop, ko_row = _rows(k_out, "k_out", dt, k_shape, dev)
     _call("basp_qk_norm_rope", (_lib or lib()).basp_qk_norm_rope, dev, qp, kp, qop, kop, *w, *turn,
-          *dims, q_row, k_row, qo_row, ko_row, eps, pos0, interleaved, code)
+          *dims, q_row, k_row, qo_row, ko_row, eps, _int(pos0), interleaved, code)
     return q_out, k_out
 
 
@@ -641,7 +646,7 @@ def qk_norm_rope_bwd(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, eps: fl
             b, S, n_q, n_k, d)
         workspace, ws, ws_n = _space(workspace, need, q, dev)
     _call("basp_qk_norm_rope_bwd", L.basp_qk_norm_rope_bwd, dev, qp, kp, gq, gk, dqp, dkp, *w, dqw,
-          dkw, *turn, ws, ws_n, *dims, q_row, k_row, eps, pos0, interleaved, code, gcode)
+          dkw, *turn, ws, ws_n, *dims, q_row, k_row, eps, _int(pos0), interleaved, code, gcode)
     return dq, dk, dq_weight, dk_weight
 
 
@@ -752,8 +757,7 @@ def attn_decode(q, k_pages, v_pages, block_table, lens, scale: float | None = No
         raise ValueError("q and the pages disagree in shape")
     if scale is None:
         scale = d ** -0.5
-    if max_len is None:
-        max_len = max_pages * page
+    max_len = _int(max_pages * page if max_len is None else max_len)
     qp, q_row = _rows(q, "q", _BF, shape, dev)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)

@@ -27,20 +27,48 @@ unpack pass: attention reads the shard buffers in place and writes O, dQ,
 dK, dV straight into the send buffers (bit for bit the same results); with a
 shared kv head, dK and dV go to one send block per member (`dk_send`,
 `dv_send`), each the member's partial gradient for that member's tokens.
+
+With a `QkNormRope` the share's Q and K are normalised per head and rotated
+between the pack and attention, and the backward goes through both:
+
+  forward:  pack(Q, K, V) -> qk_norm_rope -> attn_fwd -> unpack(O)
+  backward: pack(dO) -> attn_bwd -> qk_norm_rope_bwd -> unpack(dQ, dK, dV)
+
+`dq_weight`, `dk_weight` are then the rank's parts of the weights' gradients
+(those of its heads), to be summed over the group.  Attention on the shard
+buffers in place has no such step: there the owner of a shard calls
+qk_norm_rope on it before the exchange.
+
+After a forward `fill_cache` puts the prompt's K and V into a paged cache, and
+`decode` takes the share on by one token per sequence.
 """
 from __future__ import annotations
+
+from dataclasses import dataclass
 
 import torch
 
 from . import (attn_bwd, attn_bwd_sharded, attn_bwd_sharded_workspace_bytes,
                attn_bwd_workspace_bytes, attn_fwd,
-               attn_fwd_sharded, heads_per_member, pack, pack_qkv, unpack, unpack_add,
-               unpack_grads)
+               attn_fwd_sharded, heads_per_member, pack, pack_qkv, qk_norm_rope, qk_norm_rope_bwd,
+               qk_norm_rope_bwd_workspace_bytes, unpack, unpack_add, unpack_grads)
+
+
+@dataclass
+class QkNormRope:
+    """Norm weights (fp32 [d], both None: no norm) and position tables (`rope_table`, both None: no
+    rotation) of a layer's queries and keys."""
+    q_weight: torch.Tensor | None
+    k_weight: torch.Tensor | None
+    cos: torch.Tensor | None
+    sin: torch.Tensor | None
+    eps: float = 1e-6
+    interleaved: bool = False
 
 
 class RankShare:
     def __init__(self, q_shards, k_shards, v_shards, do_shards, G: int, rank: int,
-                 scale: float | None = None):
+                 scale: float | None = None, norm_rope: QkNormRope | None = None):
         self.G, self.rank = G, rank
         self.q_shards, self.k_shards, self.v_shards = q_shards, k_shards, v_shards
         self.do_shards = do_shards
@@ -75,12 +103,28 @@ class RankShare:
             self.dv_send = [torch.zeros((b, Sg, 1, d), dtype=f32, device=dev) for _ in range(G)]
         ws = max(attn_bwd_workspace_bytes(b, S, H, H_kv, d, G),
                  attn_bwd_sharded_workspace_bytes(b, S, H, H_kv, d, G))
+        # norm and rotation: what the pack gives, kept for the backward; the
+        # weights' gradients (this rank's heads' part)
+        self.norm_rope = norm_rope
+        self.q_in, self.k_in = self.q, self.k
+        self.dq_weight = self.dk_weight = None
+        if norm_rope is not None:
+            self.q_in, self.k_in = torch.empty_like(self.q), torch.empty_like(self.k)
+            if norm_rope.q_weight is not None:
+                self.dq_weight = torch.empty_like(norm_rope.q_weight)
+                self.dk_weight = torch.empty_like(norm_rope.k_weight)
+                ws = max(ws, qk_norm_rope_bwd_workspace_bytes(b, S, self.Hl, self.Hkl, d))
         self.workspace = torch.empty(max(ws, 16), dtype=torch.uint8, device=dev)
 
     # individual steps, so that callers can time them
     def pack_qkv(self):
-        pack_qkv(self.q_shards, self.k_shards, self.v_shards, self.rank, q=self.q, k=self.k,
+        pack_qkv(self.q_shards, self.k_shards, self.v_shards, self.rank, q=self.q_in, k=self.k_in,
                  v=self.v)
+
+    def qk_norm_rope(self):
+        n = self.norm_rope
+        qk_norm_rope(self.q_in, self.k_in, n.q_weight, n.k_weight, n.cos, n.sin, eps=n.eps,
+                     interleaved=n.interleaved, q_out=self.q, k_out=self.k)
 
     def attn_fwd(self):
         attn_fwd(self.q, self.k, self.v, G=self.G, scale=self.scale, out=self.o, lse=self.lse,
@@ -96,6 +140,14 @@ class RankShare:
         attn_bwd(self.q, self.k, self.v, self.o, self.lse, self.do, G=self.G, scale=self.scale,
                  dq=self.dq, dk=self.dk, dv=self.dv, workspace=self.workspace, H_kv=self.H_kv)
 
+    def qk_norm_rope_bwd(self):
+        """dq, dk in place: from the gradients of attention's Q and K to those of the packed ones."""
+        n = self.norm_rope
+        qk_norm_rope_bwd(self.q_in, self.k_in, self.dq, self.dk, n.q_weight, n.k_weight, n.cos, n.sin,
+                         eps=n.eps, interleaved=n.interleaved, dq=self.dq, dk=self.dk,
+                         dq_weight=self.dq_weight, dk_weight=self.dk_weight,
+                         workspace=self.workspace)
+
     def _unpack_kv_grad(self, local, shards):
         (unpack_add if self.shared_kv else unpack)(local, shards, self.rank)
 
@@ -105,24 +157,56 @@ class RankShare:
 
     def forward(self):
         self.pack_qkv()
+        if self.norm_rope is not None:
+            self.qk_norm_rope()
         self.attn_fwd()
         self.unpack_o()
 
     def backward(self):
         self.pack_do()
         self.attn_bwd()
+        if self.norm_rope is not None:
+            self.qk_norm_rope_bwd()
         self.unpack_grads()
 
     def step(self):
         self.forward()
         self.backward()
 
+    # generation after the prompt
+    def fill_cache(self, cache, block_table):
+        """K and V of the last forward into a `PagedKV`, sequence s's tokens from position 0 on in the
+        pages that row s of the block table lists."""
+        start = torch.zeros(self.b, dtype=torch.int32, device=self.k.device)
+        cache.write(self.k, self.v, block_table, start)
+
+    def decode(self, cache, q, k, v, block_table, lens, max_len: int | None = None, workspace=None):
+        """One new token per sequence: q [n, 1, H/G, d] and k, v [n, 1, Hkl, d], the rank's heads of
+        its projections, at position lens[s] - 1.  Norm and rotation if the share has them, the
+        token's K and V into the cache, and attention over the lens[s] tokens: returns (O [n,
+        H/G, d], LSE [n, H/G]).  A length of 0 is a slot without a sequence."""
+        at = lens - 1
+        n = self.norm_rope
+        if n is not None:
+            q, k = qk_norm_rope(q, k, n.q_weight, n.k_weight, n.cos, n.sin, eps=n.eps,
+                                interleaved=n.interleaved, positions=at.view(-1, 1))
+        cache.write(k, v, block_table, at)
+        return cache.attend(q[:, 0], block_table, lens, scale=self.scale, max_len=max_len,
+                            workspace=workspace)
+
     # attention on the shard buffers in place
+    def _check_in_place(self):
+        if self.norm_rope is not None:
+            raise ValueError("attention in place takes normalised, rotated shards: call qk_norm_rope "
+                             "on them before the exchange")
+
     def forward_sharded(self):
+        self._check_in_place()
         attn_fwd_sharded(self.q_shards, self.k_shards, self.v_shards, self.o_shards, self.rank,
                          scale=self.scale, lse=self.lse)
 
     def backward_sharded(self):
+        self._check_in_place()
         dk, dv = ((self.dk_send, self.dv_send) if self.shared_kv
                   else (self.dk_shards, self.dv_shards))
         attn_bwd_sharded(self.q_shards, self.k_shards, self.v_shards, self.o_shards, self.lse,
@@ -154,8 +238,8 @@ class RankShare:
         # an added gradient is read on both sides and written once
         kv_grad = (lambda t: 3 * t.numel() * t.element_size()) if self.shared_kv else two
         return [
-            ("pack_q", lambda: pack(self.q_shards, self.rank, out=self.q), two(self.q)),
-            ("pack_k", lambda: pack(self.k_shards, self.rank, out=self.k), two(self.k)),
+            ("pack_q", lambda: pack(self.q_shards, self.rank, out=self.q_in), two(self.q)),
+            ("pack_k", lambda: pack(self.k_shards, self.rank, out=self.k_in), two(self.k)),
             ("pack_v", lambda: pack(self.v_shards, self.rank, out=self.v), two(self.v)),
             ("unpack_o", lambda: unpack(self.o, self.o_shards, self.rank), two(self.o)),
             ("pack_do", lambda: pack(self.do_shards, self.rank, out=self.do), two(self.do)),
