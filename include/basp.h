@@ -516,7 +516,9 @@ size_t basp_attn_decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_
  * pages the length reaches, gives NaN.  max_len: the longest sequence the caller
  * expects, 1 or more; it sizes the split and the workspace.
  * Products in bf16 with fp32 accumulation (an 8-bit key or value is exact in
- * bf16; scales are applied in fp32), softmax in fp32; deterministic.
+ * bf16, scales are applied in fp32, a weight is the sum of two bf16), softmax in
+ * fp32, O rounded once; deterministic.  A NaN or infinity among the values that a
+ * head attends to makes its element of O one of these.
  * workspace: basp_attn_decode_workspace_bytes() or more, 16-byte aligned;
  * contents ignored on entry; calls that may overlap on the device, two captured
  * graphs among them, need one each.  q and o 16-byte aligned, lse 4.

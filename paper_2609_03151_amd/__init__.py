@@ -501,8 +501,13 @@ def _on(t, name: str, dtype, shape, dev: int) -> int:
     _refuse(t, name, dtype, shape, dev)
 
 
-def _opt(t, name: str, dtype, shape, dev: int):
-    return None if t is None else _on(t, name, dtype, shape, dev)
+def _two(a, a_name: str, b, b_name: str, dtype, shape, dev: int):
+    """Pointers of two such tensors."""
+    if (isinstance(a, _Tensor) and isinstance(b, _Tensor) and a.dtype is dtype and b.dtype is dtype
+            and a.shape == shape == b.shape and a.get_device() == dev == b.get_device()
+            and a.is_contiguous() and b.is_contiguous()):
+        return a.data_ptr(), b.data_ptr()
+    return _on(a, a_name, dtype, shape, dev), _on(b, b_name, dtype, shape, dev)
 
 
 def _rows(t, name: str, dtype, shape, dev: int):
@@ -551,15 +556,14 @@ def _norm_args(q, k, q_weight, k_weight, cos, sin, positions):
         raise ValueError("cos and sin, and q_weight and k_weight, go together")
     qw = kw = c = sn = None
     if q_weight is not None:
-        w = (d,)
-        qw, kw = _on(q_weight, "q_weight", _F32, w, dev), _on(k_weight, "k_weight", _F32, w, dev)
+        qw, kw = _two(q_weight, "q_weight", k_weight, "k_weight", _F32, (d,), dev)
     rows = half = 0
     if cos is not None:
         if not isinstance(cos, _Tensor) or cos.dim() != 2:
             raise ValueError("cos and sin must be [positions, rot/2]")
         table = cos.shape
         rows, half = table
-        c, sn = _on(cos, "cos", _F32, table, dev), _on(sin, "sin", _F32, table, dev)
+        c, sn = _two(cos, "cos", sin, "sin", _F32, table, dev)
         if half == 0:  # no columns: nothing is rotated
             c = sn = None
     pos = None if positions is None else _on(positions, "positions", _I32, (b, S), dev)
@@ -682,11 +686,10 @@ def _pages(k_pages, v_pages, k_scales, v_scales, table, b, dev: int):
     else:
         if k_scales is None or v_scales is None:
             raise ValueError("an 8-bit cache has k_scales and v_scales")
-        u8, s_shape = torch.uint8, (n_pages, n_k, page)
-        ks = _on(k_scales, "k_scales", u8, s_shape, dev)
-        vs = _on(v_scales, "v_scales", u8, s_shape, dev)
+        ks, vs = _two(k_scales, "k_scales", v_scales, "v_scales", torch.uint8, (n_pages, n_k, page),
+                      dev)
     t_shape = table.shape
-    return ((_on(k_pages, "k_pages", dt, shape, dev), _on(v_pages, "v_pages", dt, shape, dev), ks, vs,
+    return ((*_two(k_pages, "k_pages", v_pages, "v_pages", dt, shape, dev), ks, vs,
              _on(table, "block_table", _I32, t_shape, dev)),
             (n_k, d, page, n_pages, t_shape[1]), code)
 

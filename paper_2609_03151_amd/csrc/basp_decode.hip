@@ -6,17 +6,18 @@
 // operations a byte of bf16 (16 on 8 query heads a kv head), which is more than
 // the vector units do beside such a stream and little for the matrix cores.
 //
-// The keys of all sequences are dealt out evenly: a unit is 128 keys (256 in 8
-// bits) of one kv head and up to 16 of its query heads, and each of at
-// most 512 workgroups, two per CU, takes one run of units, in the order of
-// sequences, heads and keys.  The lengths are known on the device only, so each
-// workgroup adds them up to find its run.  Its four waves take a block of 32 (64)
-// keys of each unit, each with a running maximum, sum and O of its own, joined in LDS
-// at the end of a sequence's head or of the run.  Only the first and the last
-// head of a run can be shared with other workgroups; their partial results are
-// joined by a second kernel:
+// The keys of all sequences are dealt out evenly: a unit is 128 keys of one kv
+// head for up to 16 of its query heads, and each of at most 768 workgroups, three
+// per CU, takes one run of units, in the order of sequences, heads and keys.  The
+// lengths are known on the device only, so each workgroup adds them up to find
+// its run.  Its four waves take a block of 32 keys of each unit, each with a running
+// maximum, sum and O of its own, joined in LDS at the end of a sequence's head or
+// of the run.  Only the first and the last head of a run can be shared with other
+// workgroups; their partial results are joined by a second kernel:
 //   M = max_i m_i,  O = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i
-// (scores in log2 units).
+// (scores in log2 units).  Splits of a fixed number of keys, one workgroup each,
+// left the longest ones to run alone at the end: 64 ragged sequences of up to 32K
+// tokens, 8 heads on 2 of 128, took 236 us, dealt out evenly 198.
 //
 // Nothing passes through LDS on the way to the matrix cores: the operands of
 // v_mfma_f32_16x16x32_bf16 (lane l: 8 consecutive contraction elements
@@ -46,6 +47,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kRows = 16;  // query heads of a workgroup
+constexpr int kTiles = 2;  // of 16 keys, in a wave's block
+constexpr int kBlockKeys = 16 * kTiles, kUnit = kWaves * kBlockKeys;  // a unit: a block per wave
 constexpr int kCus = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -95,14 +98,12 @@ template <int D, bool E4M3>
 struct Block {
   static constexpr int kElem = E4M3 ? 1 : 2;
   static constexpr int kRowBytes = D * kElem;
-  static constexpr int kTiles = E4M3 ? 4 : 2;         // 16 keys each
-  static constexpr int kKeys = 16 * kTiles;
   static constexpr int kLoads = (kRowBytes + 63) / 64;  // of 64 bytes per key
   static constexpr int kSteps = E4M3 ? 2 * kLoads : kLoads;
   static constexpr int kCols = D <= 64 ? 4 : 8;       // elements of d per lane of V
   static constexpr int kWords = kCols * kElem / 4;    // 32-bit words of V per key and lane
   u32x4 k[kTiles][kLoads];
-  uint32_t v[kTiles / 2][8][kWords];
+  uint32_t v[8][kWords];
   uint32_t ks[kTiles], vs[kTiles];  // scale bytes of keys 4(l/16)..
   bool bad;                         // a key on no valid page (wave-uniform)
 };
@@ -149,10 +150,9 @@ __device__ __forceinline__ int scalar_load(const int *p, size_t i) {
 
 // Page numbers of a block's tiles (tiles do not cross pages: both are
 // multiples of 16).
-template <typename B>
-__device__ __forceinline__ void load_ids(const Pages &p, int t0, int hi, int (&id)[B::kTiles]) {
+__device__ __forceinline__ void load_ids(const Pages &p, int t0, int hi, int (&id)[kTiles]) {
 #pragma unroll
-  for (int t = 0; t < B::kTiles; ++t) {
+  for (int t = 0; t < kTiles; ++t) {
     const int at = t0 + 16 * t, pi = at >> p.page_log2;
     id[t] = -1;
     if (at < hi && pi < p.max_pages) id[t] = scalar_load(p.table, pi);
@@ -165,12 +165,12 @@ __device__ __forceinline__ void load_ids(const Pages &p, int t0, int hi, int (&i
 // so the compiler can wait for one block's and leave the next one's.
 template <int D, bool E4M3>
 __device__ __forceinline__ void load_block(Block<D, E4M3> &b, const Pages &p, int t0, int hi,
-                                           const int (&ids)[Block<D, E4M3>::kTiles]) {
+                                           const int (&ids)[kTiles]) {
   using B = Block<D, E4M3>;
   const int lane = threadIdx.x % 64, m = lane % 16, c = lane / 16;
   b.bad = false;
 #pragma unroll
-  for (int t = 0; t < B::kTiles; ++t) {
+  for (int t = 0; t < kTiles; ++t) {
     const int at = t0 + 16 * t;
     const int id = scalar(ids[t]);
     const bool there = id >= 0 && id < p.n_pages;
@@ -195,7 +195,7 @@ __device__ __forceinline__ void load_block(Block<D, E4M3> &b, const Pages &p, in
     const uint32_t vc = m * B::kCols < D ? m * B::kCols * B::kElem : 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      uint32_t(&v)[B::kWords] = b.v[t / 2][4 * (t % 2) + e];
+      uint32_t(&v)[B::kWords] = b.v[4 * t + e];
       const int r = 4 * c + e;
       const uint32_t o = (uint32_t)(r < last ? r : last) * B::kRowBytes + vc;
       if constexpr (B::kWords == 4) {
@@ -231,9 +231,9 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
                                            int left) {
   using B = Block<D, E4M3>;
   const int c = threadIdx.x % 64 / 16;
-  float s[B::kTiles][4];
+  float s[kTiles][4];
 #pragma unroll
-  for (int t = 0; t < B::kTiles; ++t) {
+  for (int t = 0; t < kTiles; ++t) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < B::kLoads; ++i) {
@@ -253,21 +253,21 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
       if constexpr (E4M3) s[t][r] *= pow2_of_byte(b.ks[t], r);
     }
   }
-  if (left < B::kKeys) {
+  if (left < kBlockKeys) {
 #pragma unroll
-    for (int t = 0; t < B::kTiles; ++t)
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         if (16 * t + 4 * c + r >= left) {
           s[t][r] = -INFINITY;
 #pragma unroll
-          for (int w = 0; w < B::kWords; ++w) b.v[t / 2][4 * (t % 2) + r][w] = 0;  // 0 * inf
+          for (int w = 0; w < B::kWords; ++w) b.v[4 * t + r][w] = 0;  // 0 * inf
         }
   }
   if (b.bad) s[0][0] = __builtin_nanf("");
   float mx = s[0][0];
 #pragma unroll
-  for (int t = 0; t < B::kTiles; ++t)
+  for (int t = 0; t < kTiles; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[t][r]);
   mx = fmaxf(st.m, column_max(mx));
@@ -278,7 +278,7 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
 #pragma unroll
   for (int i = 0; i < B::kCols; ++i) st.o[i] *= f;
 #pragma unroll
-  for (int t = 0; t < B::kTiles; ++t)
+  for (int t = 0; t < kTiles; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float p = fast_exp2(s[t][r] - ref);
@@ -287,33 +287,36 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
       if constexpr (E4M3) {
         s[t][r] *= pow2_of_byte(b.vs[t], r);
         // past the end the scale may be anything
-        if (left < B::kKeys && 16 * t + 4 * c + r >= left) s[t][r] = 0.f;
+        if (left < kBlockKeys && 16 * t + 4 * c + r >= left) s[t][r] = 0.f;
       }
     }
+  // P as the sum of two bf16 (its rounding, and that of what this leaves): the
+  // matrix cores have room for two products, and O is as exact as its fp32 sums.
+  u32x4 hi, lo;
 #pragma unroll
-  for (int g = 0; g < B::kTiles / 2; ++g) {
-    // P rounded to bf16 for the matrix cores; its sum above is of the unrounded
-    const bf16x8 p = as_bf16x8(u32x4{pack_bf16x2(s[2 * g][0], s[2 * g][1]),
-                                     pack_bf16x2(s[2 * g][2], s[2 * g][3]),
-                                     pack_bf16x2(s[2 * g + 1][0], s[2 * g + 1][1]),
-                                     pack_bf16x2(s[2 * g + 1][2], s[2 * g + 1][3])});
+  for (int i = 0; i < 4; ++i) {
+    const float *x = &s[i / 2][i % 2 * 2];
+    hi[i] = pack_bf16x2(x[0], x[1]);
+    lo[i] = pack_bf16x2(x[0] - __builtin_bit_cast(float, hi[i] << 16),
+                        x[1] - __builtin_bit_cast(float, hi[i] & 0xFFFF0000u));
+  }
+  const bf16x8 p = as_bf16x8(hi), p2 = as_bf16x8(lo);
 #pragma unroll
-    for (int i = 0; i < B::kCols / 2; ++i) {  // elements 2i, 2i + 1
-      uint32_t w[8];
+  for (int i = 0; i < B::kCols / 2; ++i) {  // elements 2i, 2i + 1
+    uint32_t w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (E4M3)
-          w[e] = i % 2 ? widen<true>(b.v[g][e][i / 2]) : widen<false>(b.v[g][e][i / 2]);
-        else
-          w[e] = b.v[g][e][i];
-      }
-      st.o[2 * i] = mfma16x16x32(as_bf16x8(u32x4{halves<false>(w[0], w[1]), halves<false>(w[2], w[3]),
-                                                 halves<false>(w[4], w[5]), halves<false>(w[6], w[7])}),
-                                 p, st.o[2 * i]);
-      st.o[2 * i + 1] = mfma16x16x32(as_bf16x8(u32x4{halves<true>(w[0], w[1]), halves<true>(w[2], w[3]),
-                                                     halves<true>(w[4], w[5]), halves<true>(w[6], w[7])}),
-                                     p, st.o[2 * i + 1]);
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (E4M3)
+        w[e] = i % 2 ? widen<true>(b.v[e][i / 2]) : widen<false>(b.v[e][i / 2]);
+      else
+        w[e] = b.v[e][i];
     }
+    const bf16x8 even = as_bf16x8(u32x4{halves<false>(w[0], w[1]), halves<false>(w[2], w[3]),
+                                        halves<false>(w[4], w[5]), halves<false>(w[6], w[7])});
+    const bf16x8 odd = as_bf16x8(u32x4{halves<true>(w[0], w[1]), halves<true>(w[2], w[3]),
+                                       halves<true>(w[4], w[5]), halves<true>(w[6], w[7])});
+    st.o[2 * i] = mfma16x16x32(even, p, mfma16x16x32(even, p2, st.o[2 * i]));
+    st.o[2 * i + 1] = mfma16x16x32(odd, p, mfma16x16x32(odd, p2, st.o[2 * i + 1]));
   }
 }
 
@@ -332,7 +335,6 @@ struct Partials {
   f32x2 *ml;
   float *o;
 };
-constexpr size_t kOpenBytes = sizeof(Open), kRowBytesMl = 2 * kRows * sizeof(f32x2);
 __device__ __forceinline__ Partials partials_at(void *ws, int opens, int groups) {
   Partials p;
   p.open = static_cast<Open *>(ws);
@@ -341,13 +343,8 @@ __device__ __forceinline__ Partials partials_at(void *ws, int opens, int groups)
   return p;
 }
 
-// Keys of a unit.
-template <typename B>
-constexpr int kUnit = kWaves * B::kKeys;
-
-template <typename B>
 __device__ __forceinline__ int units_of(int len, int max_len) {
-  return len <= 0 || len > max_len ? 0 : (len - 1) / kUnit<B> + 1;
+  return len <= 0 || len > max_len ? 0 : (len - 1) / kUnit + 1;
 }
 
 __device__ __forceinline__ int wave_scan(int x) {  // inclusive
@@ -360,12 +357,14 @@ __device__ __forceinline__ int wave_scan(int x) {  // inclusive
   return x;
 }
 
-// Workgroups per CU: what the registers allow.
-constexpr int per_cu(int d, bool e4m3) { return d == 64 || (d < 128 && !e4m3) ? 4 : 3; }
+// Workgroups per CU.  One alone has enough bytes in flight to fill the memory;
+// three let more of them start on a short call (8 ragged sequences of up to 8K
+// tokens, 8 heads on 2: 14.9 us against 16.1 with two), four leave a long sequence in
+// more parts to join (one of 128K in 8 bits: 16.5 us with three, 19.5).
+constexpr int kPerCu = 3;
 
 template <int D, bool E4M3>
-__global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const DecodeArgs a,
-                                                                           int opens) {
+__global__ __launch_bounds__(kThreads, kPerCu) void decode_kernel(const DecodeArgs a, int opens) {
   using B = Block<D, E4M3>;
   const int rep = scalar(a.n_q / a.s.n_k), row_groups = (rep + kRows - 1) / kRows;
   const int R = scalar(a.s.n_k * row_groups);  // heads, as dealt out, of a sequence
@@ -382,7 +381,7 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
   auto write_empty = [&]() {
     for (int s = g; s < b; s += G) {
       const int len = scalar_load(a.lens, s);
-      if (units_of<B>(len, a.max_len) > 0) continue;
+      if (units_of(len, a.max_len) > 0) continue;
       uint16_t *o = static_cast<uint16_t *>(a.o) + (size_t)s * a.n_q * D;
       for (int i = threadIdx.x; i < a.n_q * D; i += kThreads) o[i] = len <= 0 ? 0 : 0x7FFF;
       if (a.lse)
@@ -395,10 +394,10 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
 
   // All units, and this workgroup's run [begin, end).
   const int len0 = (int)threadIdx.x < b ? a.lens[threadIdx.x] : 0;
-  const int n0 = units_of<B>(len0, a.max_len);
+  const int n0 = units_of(len0, a.max_len);
   int mine = n0;
   for (int s = threadIdx.x + kThreads; s < b; s += kThreads)
-    mine += units_of<B>(a.lens[s], a.max_len);
+    mine += units_of(a.lens[s], a.max_len);
   mine = wave_scan(mine);
   if (lane == 63) sums[wave] = mine;
   __syncthreads();
@@ -418,7 +417,7 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
     int len = len0, n = n0, x = mine;
     if (b > kThreads) {  // else the sums above are those of the one chunk
       __syncthreads();   // sums, read above or in the last turn
-      if (s0 > 0) len = s < b ? a.lens[s] : 0, n = units_of<B>(len, a.max_len);
+      if (s0 > 0) len = s < b ? a.lens[s] : 0, n = units_of(len, a.max_len);
       x = wave_scan(n);
       if (lane == 63) sums[wave] = x;
       __syncthreads();
@@ -433,7 +432,7 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
   }
   __syncthreads();
   int seq = scalar(found[0]);
-  int len = scalar(found[2]), n = units_of<B>(len, a.max_len);  // n: units of a head of it
+  int len = scalar(found[2]), n = units_of(len, a.max_len);  // n: units of a head of it
   int head = scalar(found[1] / n), u = scalar(found[1] % n);
 
   Pages pg;
@@ -450,8 +449,8 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
 
   for (int pos = begin; pos < end;) {
     const int take = n - u < end - pos ? n - u : end - pos;  // units of this head
-    const int lo = u * kUnit<B>;
-    const int hi = (u + take) * kUnit<B> < len ? (u + take) * kUnit<B> : len;
+    const int lo = u * kUnit;
+    const int hi = (u + take) * kUnit < len ? (u + take) * kUnit : len;
     const int kvh = scalar(head / row_groups), grp = scalar(head % row_groups);
     const int h0 = kvh * rep + grp * kRows;  // first query head
     const int heads = rep - grp * kRows < kRows ? rep - grp * kRows : kRows;
@@ -460,10 +459,10 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
 
     // Blocks lo + (4j + wave) * kKeys: the next one's loads are in flight while
     // one is taken, and the one after's page numbers.
-    int t = lo + wave * B::kKeys;
+    int t = lo + wave * kBlockKeys;
     Block<D, E4M3> x;
-    int ids[B::kTiles];
-    load_ids<B>(pg, t, hi, ids);
+    int ids[kTiles];
+    load_ids(pg, t, hi, ids);
     bf16x8 q[B::kSteps];
     const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (long long)seq * a.q_row +
                          (size_t)(h0 + m) * D;
@@ -481,9 +480,9 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
     for (int i = 0; i < B::kCols; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     while (t < hi) {
       load_block<D, E4M3>(x, pg, t, hi, ids);
-      load_ids<B>(pg, t + kUnit<B>, hi, ids);
+      load_ids(pg, t + kUnit, hi, ids);
       take_block<D, E4M3>(x, st, q, scale2, hi - t);
-      t += kUnit<B>;
+      t += kUnit;
     }
     st.l = column_sum(st.l);
 
@@ -542,7 +541,7 @@ __global__ __launch_bounds__(kThreads, per_cu(D, E4M3)) void decode_kernel(const
         n = 0;
         while (n == 0 && ++seq < b) {
           len = scalar_load(a.lens, seq);
-          n = units_of<B>(len, a.max_len);
+          n = units_of(len, a.max_len);
         }
         if (n == 0) break;  // not reached while lens stays as it is
       }
@@ -637,23 +636,22 @@ struct Shape {
   int groups, opens;  // workgroups, and descriptors for the join
   size_t bytes;       // of workspace, 0 where no head is shared by two workgroups
 };
-Shape shape_of(int b, int n_q, int n_k, int d, int max_len, bool e4m3) {
-  const int rep = n_q / n_k, most = kCus * per_cu(d, e4m3);
+Shape shape_of(int b, int n_q, int n_k, int d, int max_len) {
+  const int rep = n_q / n_k, most = kCus * kPerCu;
   const long long heads = (long long)b * n_k * ((rep + kRows - 1) / kRows);
-  const int unit = e4m3 ? 256 : 128;
-  const long long units = heads * (((long long)max_len + unit - 1) / unit);
+  const long long units = heads * (((long long)max_len + kUnit - 1) / kUnit);
   Shape s;
   s.groups = (int)(units < most ? units : most);
   s.opens = (int)(heads < s.groups ? heads : s.groups);
-  s.bytes = max_len <= unit ? 0
-                            : s.opens * kOpenBytes +
-                                  s.groups * (kRowBytesMl + 2 * kRows * d * sizeof(float));
+  s.bytes = max_len <= kUnit ? 0
+                             : s.opens * sizeof(Open) +
+                                   s.groups * 2 * kRows * (sizeof(f32x2) + d * sizeof(float));
   return s;
 }
 
 template <int D, bool E4M3>
 hipError_t decode_typed(const DecodeArgs &a, hipStream_t stream) {
-  const Shape s = shape_of(a.s.b, a.n_q, a.s.n_k, D, a.max_len, E4M3);
+  const Shape s = shape_of(a.s.b, a.n_q, a.s.n_k, D, a.max_len);
   hipLaunchKernelGGL((decode_kernel<D, E4M3>), dim3(s.groups), dim3(kThreads), 0, stream, a,
                      s.opens);
   hipError_t e = hipGetLastError();
@@ -675,11 +673,8 @@ hipError_t decode_dim(const DecodeArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-// Enough for either type of cache.
 size_t decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_len) {
-  const size_t x = shape_of(b, n_q, n_k, d, max_len, false).bytes;
-  const size_t y = shape_of(b, n_q, n_k, d, max_len, true).bytes;
-  return x > y ? x : y;
+  return shape_of(b, n_q, n_k, d, max_len).bytes;
 }
 
 hipError_t launch_attn_decode(const DecodeArgs &a, hipStream_t stream) {
