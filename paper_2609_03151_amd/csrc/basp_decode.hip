@@ -161,8 +161,7 @@ __device__ __forceinline__ void load_ids(const Pages &p, int t0, int hi, int (&i
 
 // Loads of the block from key t0 on.  Keys from `hi` on read the last row before
 // it instead (take_block drops them), tiles with no key before `hi` or on no valid
-// page the first row of page 0: the loads in flight are the same in every turn,
-// so the compiler can wait for one block's and leave the next one's.
+// page the first row of page 0.
 template <int D, bool E4M3>
 __device__ __forceinline__ void load_block(Block<D, E4M3> &b, const Pages &p, int t0, int hi,
                                            const int (&ids)[kTiles]) {
@@ -184,7 +183,7 @@ __device__ __forceinline__ void load_block(Block<D, E4M3> &b, const Pages &p, in
     const uint32_t kr = (uint32_t)(m < last ? m : last) * B::kRowBytes;
 #pragma unroll
     for (int s = 0; s < B::kLoads; ++s) {
-      // past a row's end (d = 80, 96; Q is zero there): its first bytes
+      // past a row's end (d = 80, 96): its first bytes, which take_block drops
       const uint32_t col = 64 * s + 16 * c;
       if constexpr (B::kRowBytes % 64 == 0)
         b.k[t][s] = load_at<u32x4>(kb, kr + 16 * c + 64 * s);
@@ -237,7 +236,8 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < B::kLoads; ++i) {
-      const u32x4 k = b.k[t][i];
+      u32x4 k = b.k[t][i];
+      if (64 * i + 64 > B::kRowBytes && 64 * i + 16 * c >= B::kRowBytes) k = u32x4{0, 0, 0, 0};
       if constexpr (E4M3) {
         acc = mfma16x16x32(as_bf16x8(u32x4{widen<false>(k.x), widen<true>(k.x), widen<false>(k.y),
                                            widen<true>(k.y)}), q[2 * i], acc);
@@ -457,8 +457,9 @@ __global__ __launch_bounds__(kThreads, kPerCu) void decode_kernel(const DecodeAr
     pg.table = a.table + (size_t)seq * a.s.max_pages;
     pg.kvh = kvh;
 
-    // Blocks lo + (4j + wave) * kKeys: the next one's loads are in flight while
-    // one is taken, and the one after's page numbers.
+    // Blocks lo + (4j + wave) * kBlockKeys, one in flight per wave, the next one's
+    // page numbers with it.  (A second block in flight in registers of its own
+    // leaves two waves per SIMD, and the time as it is.)
     int t = lo + wave * kBlockKeys;
     Block<D, E4M3> x;
     int ids[kTiles];

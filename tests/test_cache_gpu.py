@@ -267,6 +267,24 @@ def test_decode_nan_and_infinity(e4m3):
         check("lse", lse[0], rl, bl, F32)
 
 
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+def test_decode_keys_of_minus_infinity(d):
+    """A key whose first, or last, elements are minus infinity against a positive query is taken
+    out: its score is minus infinity, whatever the row's padding to whole operands reads."""
+    kp, vp, table, _ = _filled([150], 1, 16, d, False)
+    q = _randn(1, 3, d, seed=3).abs() + 0.5
+    out = (3, 40, 149)
+    for i, t in enumerate(out):
+        col = slice(0, 8) if i % 2 else slice(d - 4, d)
+        kp[int(table[0, t // 16]), 0, t % 16, col] = -math.inf
+    K, V = gather_ref(kp, None, table[0], 150), gather_ref(vp, None, table[0], 150)
+    keep = [i for i in range(150) if i not in out]
+    o, lse = basp.attn_decode(q, kp, vp, table, _ints([150]))
+    ro, bo, rl, bl = decode_ref(q[0], K[keep].contiguous(), V[keep].contiguous(), d ** -0.5)
+    check("o", o[0], ro, bo, BF16)
+    check("lse", lse[0], rl, bl, F32)
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_decode_bad_pages_and_lengths(e4m3):
     lens = [100, 100, 100, 40, 200, -7]
