@@ -265,7 +265,7 @@ int basp_kv_read(const void *k_pages, const void *v_pages, const unsigned char *
 
 size_t basp_attn_decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_len) {
   if (b < 1 || check_decode(b, n_q, n_k, d, max_len) != BASP_OK) return 0;
-  return basp::decode_workspace_bytes(b, n_q, n_k, d, max_len);
+  return basp::decode_cut(b, n_q, n_k, d, max_len).bytes;
 }
 
 int basp_attn_decode(const void *q, const void *k_pages, const void *v_pages,
@@ -285,7 +285,7 @@ int basp_attn_decode(const void *q, const void *k_pages, const void *v_pages,
   if (rc) return rc;
   if (!aligned(q, 16) || !aligned(o, 16) || !aligned(lse, 4) || !aligned(lens, 4) || q_row % 8 != 0)
     return BASP_ERR_ALIGN;
-  const size_t need = basp::decode_workspace_bytes(b, n_q, n_k, d, max_len);
+  const size_t need = basp::decode_cut(b, n_q, n_k, d, max_len).bytes;
   if (workspace_bytes < need) return BASP_ERR_WORKSPACE;
   if (need > 0 && !workspace) return BASP_ERR_NULL;
   if (!aligned(workspace, 16)) return BASP_ERR_ALIGN;

@@ -7,8 +7,8 @@
 // the vector units do beside such a stream and little for the matrix cores.
 //
 // The keys of all sequences are dealt out evenly: a unit is 128 keys of one kv
-// head for up to 16 of its query heads, and each of at most 768 workgroups, three
-// per CU, takes one run of units, in the order of sequences, heads and keys.  The
+// head for up to 16 of its query heads (32 where it has more than 16), and each of at
+// most 768 workgroups takes one run of units, in the order of sequences, heads and keys.  The
 // lengths are known on the device only, so each workgroup adds them up to find
 // its run.  Its four waves take a block of 32 keys of each unit, each with a running
 // maximum, sum and O of its own, joined in LDS at the end of a sequence's head or
@@ -46,10 +46,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kRows = 16;  // query heads of a workgroup
 constexpr int kTiles = 2;  // of 16 keys, in a wave's block
 constexpr int kBlockKeys = 16 * kTiles, kUnit = kWaves * kBlockKeys;  // a unit: a block per wave
-constexpr int kCus = 256;
+static_assert(kUnit == kDecodeUnit, "the host's cut");
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -214,20 +213,22 @@ __device__ __forceinline__ void load_block(Block<D, E4M3> &b, const Pages &p, in
   }
 }
 
-// One lane's state: query head l%16, its reference exponent, its part of the
-// sum (keys of its quarter of the lanes), and O in kCols accumulators.
+// One lane's state for query head l%16 of each 16 rows: its reference exponent, its
+// part of the sum (keys of its quarter of the lanes), and O in kCols
+// accumulators; and Q, the operand of the scores.
 template <typename B>
 struct State {
   float m, l;
   f32x4 o[B::kCols];
+  bf16x8 q[B::kSteps];
 };
 
-// Maximum, weights and O of one block.  `left`: keys of the sequence from the
-// block's first on (less than a block only in its last).
+// Scores of a block for 16 query heads, their maximum, and the weights (as the sum
+// of two bf16, operands of the product with V): updates st.m and st.l and scales
+// st.o to the new reference.
 template <int D, bool E4M3>
-__device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M3>> &st,
-                                           const bf16x8 (&q)[Block<D, E4M3>::kSteps], float scale2,
-                                           int left) {
+__device__ __forceinline__ void weights(const Block<D, E4M3> &b, State<Block<D, E4M3>> &st,
+                                        float scale2, int left, bf16x8 &p, bf16x8 &p2) {
   using B = Block<D, E4M3>;
   const int c = threadIdx.x % 64 / 16;
   float s[kTiles][4];
@@ -240,11 +241,11 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
       if (64 * i + 64 > B::kRowBytes && 64 * i + 16 * c >= B::kRowBytes) k = u32x4{0, 0, 0, 0};
       if constexpr (E4M3) {
         acc = mfma16x16x32(as_bf16x8(u32x4{widen<false>(k.x), widen<true>(k.x), widen<false>(k.y),
-                                           widen<true>(k.y)}), q[2 * i], acc);
+                                           widen<true>(k.y)}), st.q[2 * i], acc);
         acc = mfma16x16x32(as_bf16x8(u32x4{widen<false>(k.z), widen<true>(k.z), widen<false>(k.w),
-                                           widen<true>(k.w)}), q[2 * i + 1], acc);
+                                           widen<true>(k.w)}), st.q[2 * i + 1], acc);
       } else {
-        acc = mfma16x16x32(as_bf16x8(k), q[i], acc);
+        acc = mfma16x16x32(as_bf16x8(k), st.q[i], acc);
       }
     }
 #pragma unroll
@@ -258,11 +259,7 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (16 * t + 4 * c + r >= left) {
-          s[t][r] = -INFINITY;
-#pragma unroll
-          for (int w = 0; w < B::kWords; ++w) b.v[4 * t + r][w] = 0;  // 0 * inf
-        }
+        if (16 * t + 4 * c + r >= left) s[t][r] = -INFINITY;
   }
   if (b.bad) s[0][0] = __builtin_nanf("");
   float mx = s[0][0];
@@ -281,17 +278,17 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
   for (int t = 0; t < kTiles; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float p = fast_exp2(s[t][r] - ref);
-      st.l += p;
-      s[t][r] = p;
+      const float w = fast_exp2(s[t][r] - ref);
+      st.l += w;
+      s[t][r] = w;
       if constexpr (E4M3) {
         s[t][r] *= pow2_of_byte(b.vs[t], r);
         // past the end the scale may be anything
         if (left < kBlockKeys && 16 * t + 4 * c + r >= left) s[t][r] = 0.f;
       }
     }
-  // P as the sum of two bf16 (its rounding, and that of what this leaves): the
-  // matrix cores have room for two products, and O is as exact as its fp32 sums.
+  // A weight as its rounding to bf16 and that of what this leaves: the matrix cores
+  // have room for two products, and O is as exact as its fp32 sums.
   u32x4 hi, lo;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -300,7 +297,26 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
     lo[i] = pack_bf16x2(x[0] - __builtin_bit_cast(float, hi[i] << 16),
                         x[1] - __builtin_bit_cast(float, hi[i] & 0xFFFF0000u));
   }
-  const bf16x8 p = as_bf16x8(hi), p2 = as_bf16x8(lo);
+  p = as_bf16x8(hi);
+  p2 = as_bf16x8(lo);
+}
+
+// One block.  `left`: keys of the sequence from the block's first on (less than a
+// block only in its last).
+template <int D, bool E4M3, int RG>
+__device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M3>> (&st)[RG],
+                                           float scale2, int left) {
+  using B = Block<D, E4M3>;
+  bf16x8 p[RG], p2[RG];
+#pragma unroll
+  for (int g = 0; g < RG; ++g) weights<D, E4M3>(b, st[g], scale2, left, p[g], p2[g]);
+  if (left < kBlockKeys) {  // weights of 0 there; V may be anything
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (16 * (e / 4) + 4 * (int)(threadIdx.x % 64 / 16) + e % 4 >= left)
+#pragma unroll
+        for (int w = 0; w < B::kWords; ++w) b.v[e][w] = 0;
+  }
 #pragma unroll
   for (int i = 0; i < B::kCols / 2; ++i) {  // elements 2i, 2i + 1
     uint32_t w[8];
@@ -315,31 +331,32 @@ __device__ __forceinline__ void take_block(Block<D, E4M3> &b, State<Block<D, E4M
                                         halves<false>(w[4], w[5]), halves<false>(w[6], w[7])});
     const bf16x8 odd = as_bf16x8(u32x4{halves<true>(w[0], w[1]), halves<true>(w[2], w[3]),
                                        halves<true>(w[4], w[5]), halves<true>(w[6], w[7])});
-    st.o[2 * i] = mfma16x16x32(even, p, mfma16x16x32(even, p2, st.o[2 * i]));
-    st.o[2 * i + 1] = mfma16x16x32(odd, p, mfma16x16x32(odd, p2, st.o[2 * i + 1]));
+#pragma unroll
+    for (int g = 0; g < RG; ++g) {
+      f32x4 *o = st[g].o;
+      o[2 * i] = mfma16x16x32(even, p[g], mfma16x16x32(even, p2[g], o[2 * i]));
+      o[2 * i + 1] = mfma16x16x32(odd, p[g], mfma16x16x32(odd, p2[g], o[2 * i + 1]));
+    }
   }
 }
 
 // What a workgroup leaves for the join, in the workspace: for its first (0) and
-// last (1) head, of up to kRows rows, O not divided by l [g][2][kRows][D] and (m, l)
-// [g][2][kRows]; and, of each head that starts in its run, where its partial
+// last (1) head, of up to `rows` rows, O not divided by l [g][2][rows][D] and (m, l)
+// [g][2][rows]; and, of each head that starts in its run, where its partial
 // results lie if it ends past the run: `count` of them (else 0), the first in slot
-// `slot` of workgroup `g`, the others in slot 0 of the next ones.  These are
-// indexed by the head; where there are more heads than workgroups by the
-// workgroup, whose last head alone can end past its run.
-struct Open {
-  int row0, heads, count, first;  // first = 2 g + slot
-};
+// first % 2 of workgroup first / 2, the others in slot 0 of the next ones.  These
+// descriptors are indexed by the head; where there are more heads than workgroups
+// by the workgroup, whose last head alone can end past its run.
 struct Partials {
-  Open *open;
+  DecodeOpen *open;
   f32x2 *ml;
   float *o;
 };
-__device__ __forceinline__ Partials partials_at(void *ws, int opens, int groups) {
+__device__ __forceinline__ Partials partials_at(void *ws, int opens, int groups, int rows) {
   Partials p;
-  p.open = static_cast<Open *>(ws);
+  p.open = static_cast<DecodeOpen *>(ws);
   p.ml = reinterpret_cast<f32x2 *>(p.open + opens);
-  p.o = reinterpret_cast<float *>(p.ml + (size_t)groups * 2 * kRows);
+  p.o = reinterpret_cast<float *>(p.ml + (size_t)groups * 2 * rows);
   return p;
 }
 
@@ -357,15 +374,14 @@ __device__ __forceinline__ int wave_scan(int x) {  // inclusive
   return x;
 }
 
-// Workgroups per CU.  One alone has enough bytes in flight to fill the memory;
-// three let more of them start on a short call (8 ragged sequences of up to 8K
-// tokens, 8 heads on 2: 14.9 us against 16.1 with two), four leave a long sequence in
-// more parts to join (one of 128K in 8 bits: 16.5 us with three, 19.5).
-constexpr int kPerCu = 3;
-
-template <int D, bool E4M3>
-__global__ __launch_bounds__(kThreads, kPerCu) void decode_kernel(const DecodeArgs a, int opens) {
+// RG: rows of 16 query heads that a workgroup serves, two where a kv head has more
+// than 16, so that K and V are read once for 32 (32 ragged sequences of up to 16K
+// tokens, 64 heads on 2: 85 us with 16 to a workgroup, 58 with 32).
+template <int D, bool E4M3, int RG>
+__global__ __launch_bounds__(kThreads, RG == 1 ? 3 : 2) void decode_kernel(const DecodeArgs a,
+                                                                          int opens) {
   using B = Block<D, E4M3>;
+  constexpr int kRows = 16 * RG;
   const int rep = scalar(a.n_q / a.s.n_k), row_groups = (rep + kRows - 1) / kRows;
   const int R = scalar(a.s.n_k * row_groups);  // heads, as dealt out, of a sequence
   const int b = a.s.b, G = gridDim.x, g = blockIdx.x;
@@ -374,7 +390,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void decode_kernel(const DecodeAr
   __shared__ float so[kWaves][kRows][D + 4], sm[kWaves][kRows], sl[kWaves][kRows];
   __shared__ int sums[kWaves], found[3];
 
-  const Partials ps = partials_at(a.workspace, opens, G);
+  const Partials ps = partials_at(a.workspace, opens, G, kRows);
   const bool joins = a.workspace != nullptr, by_head = joins && opens != G;
 
   // Sequences without keys, or with more than the call allows, are shared out.
@@ -445,7 +461,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void decode_kernel(const DecodeAr
   pg.max_pages = a.s.max_pages;
   pg.n_k = a.s.n_k;
   const float scale2 = a.scale * kLog2e;
-  Open open = {0, 0, 0, 0};
+  DecodeOpen open = {0, 0, 0, 0};
 
   for (int pos = begin; pos < end;) {
     const int take = n - u < end - pos ? n - u : end - pos;  // units of this head
@@ -464,51 +480,62 @@ __global__ __launch_bounds__(kThreads, kPerCu) void decode_kernel(const DecodeAr
     Block<D, E4M3> x;
     int ids[kTiles];
     load_ids(pg, t, hi, ids);
-    bf16x8 q[B::kSteps];
-    const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (long long)seq * a.q_row +
-                         (size_t)(h0 + m) * D;
+    State<B> st[RG];
 #pragma unroll
-    for (int s = 0; s < B::kSteps; ++s) {
-      const int e = E4M3 ? 64 * (s / 2) + 16 * c + 8 * (s % 2) : 32 * s + 8 * c;
-      u32x4 w = {0, 0, 0, 0};
-      if (m < heads && e < D) w = *reinterpret_cast<const u32x4 *>(qp + e);
-      q[s] = as_bf16x8(w);
+    for (int rg = 0; rg < RG; ++rg) {
+      const int h = 16 * rg + m;
+      const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (long long)seq * a.q_row +
+                           (size_t)(h0 + h) * D;
+#pragma unroll
+      for (int s = 0; s < B::kSteps; ++s) {
+        const int e = E4M3 ? 64 * (s / 2) + 16 * c + 8 * (s % 2) : 32 * s + 8 * c;
+        u32x4 w = {0, 0, 0, 0};
+        if (h < heads && e < D) w = *reinterpret_cast<const u32x4 *>(qp + e);
+        st[rg].q[s] = as_bf16x8(w);
+      }
+      st[rg].m = -INFINITY;
+      st[rg].l = 0.f;
+#pragma unroll
+      for (int i = 0; i < B::kCols; ++i) st[rg].o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    State<B> st;
-    st.m = -INFINITY;
-    st.l = 0.f;
-#pragma unroll
-    for (int i = 0; i < B::kCols; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     while (t < hi) {
       load_block<D, E4M3>(x, pg, t, hi, ids);
       load_ids(pg, t + kUnit, hi, ids);
-      take_block<D, E4M3>(x, st, q, scale2, hi - t);
+      take_block<D, E4M3, RG>(x, st, scale2, hi - t);
       t += kUnit;
     }
-    st.l = column_sum(st.l);
 
     // The four waves.
     __syncthreads();  // the last head's
-    if (c == 0) sm[wave][m] = st.m, sl[wave][m] = st.l;
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const float l = column_sum(st[rg].l);
+      if (c == 0) sm[wave][16 * rg + m] = st[rg].m, sl[wave][16 * rg + m] = l;
+    }
     __syncthreads();
-    float M = sm[0][m];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm[w][m]);
-    const float f = fast_exp2(st.m - (M == -INFINITY ? 0.f : M));
+    for (int rg = 0; rg < RG; ++rg) {
+      const int h = 16 * rg + m;
+      float M = sm[0][h];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (B::kCols * (4 * c + r) < D) {
+      for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm[w][h]);
+      const float f = fast_exp2(st[rg].m - (M == -INFINITY ? 0.f : M));
+      const f32x4 *acc = st[rg].o;
 #pragma unroll
-        for (int i = 0; i < B::kCols; i += 4)
-          *reinterpret_cast<f32x4 *>(&so[wave][m][B::kCols * (4 * c + r) + i]) =
-              f32x4{st.o[i][r] * f, st.o[i + 1][r] * f, st.o[i + 2][r] * f, st.o[i + 3][r] * f};
-      }
+      for (int r = 0; r < 4; ++r)
+        if (B::kCols * (4 * c + r) < D) {
+#pragma unroll
+          for (int i = 0; i < B::kCols; i += 4)
+            *reinterpret_cast<f32x4 *>(&so[wave][h][B::kCols * (4 * c + r) + i]) =
+                f32x4{acc[i][r] * f, acc[i + 1][r] * f, acc[i + 2][r] * f, acc[i + 3][r] * f};
+        }
+    }
     __syncthreads();
     const size_t row0 = (size_t)seq * a.n_q + h0;
     const bool whole = take == n;
     const int slot = pos != begin;
     if (u == 0) {
-      open = Open{(int)row0, heads, whole ? 0 : (pos + n - 1) / quota - g + 1, 2 * g + slot};
+      open = DecodeOpen{(int)row0, heads, whole ? 0 : (pos + n - 1) / quota - g + 1, 2 * g + slot};
       if (by_head && threadIdx.x == 0) ps.open[(size_t)seq * R + head] = open;
     }
     for (int i = threadIdx.x; i < heads * (D / 4); i += kThreads) {
@@ -557,15 +584,15 @@ __global__ __launch_bounds__(kThreads, kPerCu) void decode_kernel(const DecodeAr
 // workgroups share the row's elements.
 template <int D, int C>
 __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs a, int opens,
-                                                               int groups) {
+                                                               int groups, int rows) {
   constexpr int L = 32 / C, R = kThreads / L, kAtOnce = 4;
-  const Partials p = partials_at(a.workspace, opens, groups);
-  const Open open = p.open[blockIdx.x];
+  const Partials p = partials_at(a.workspace, opens, groups, rows);
+  const DecodeOpen open = p.open[blockIdx.x];
   const int h = blockIdx.y;
   if (h >= open.heads || open.count == 0) return;
   const int n = open.count;
   auto at = [&](int i) {
-    return (size_t)(i ? (open.first | 1) - 1 + 2 * i : open.first) * kRows + h;
+    return (size_t)(i ? (open.first | 1) - 1 + 2 * i : open.first) * rows + h;
   };
   const int g = threadIdx.x / L, col = blockIdx.z * (4 * L) + threadIdx.x % L * 4;
   __shared__ float so[kWaves][4 * L + 4], sm[kWaves], sl[kWaves];
@@ -633,37 +660,24 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs 
   }
 }
 
-struct Shape {
-  int groups, opens;  // workgroups, and descriptors for the join
-  size_t bytes;       // of workspace, 0 where no head is shared by two workgroups
-};
-Shape shape_of(int b, int n_q, int n_k, int d, int max_len) {
-  const int rep = n_q / n_k, most = kCus * kPerCu;
-  const long long heads = (long long)b * n_k * ((rep + kRows - 1) / kRows);
-  const long long units = heads * (((long long)max_len + kUnit - 1) / kUnit);
-  Shape s;
-  s.groups = (int)(units < most ? units : most);
-  s.opens = (int)(heads < s.groups ? heads : s.groups);
-  s.bytes = max_len <= kUnit ? 0
-                             : s.opens * sizeof(Open) +
-                                   s.groups * 2 * kRows * (sizeof(f32x2) + d * sizeof(float));
-  return s;
-}
-
 template <int D, bool E4M3>
 hipError_t decode_typed(const DecodeArgs &a, hipStream_t stream) {
-  const Shape s = shape_of(a.s.b, a.n_q, a.s.n_k, D, a.max_len);
-  hipLaunchKernelGGL((decode_kernel<D, E4M3>), dim3(s.groups), dim3(kThreads), 0, stream, a,
-                     s.opens);
+  const DecodeCut s = decode_cut(a.s.b, a.n_q, a.s.n_k, D, a.max_len);
+  if (s.rows == 16)
+    hipLaunchKernelGGL((decode_kernel<D, E4M3, 1>), dim3(s.groups), dim3(kThreads), 0, stream, a,
+                       s.opens);
+  else
+    hipLaunchKernelGGL((decode_kernel<D, E4M3, 2>), dim3(s.groups), dim3(kThreads), 0, stream, a,
+                       s.opens);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.workspace) return e;
-  const int rep = a.n_q / a.s.n_k, rows = rep < kRows ? rep : kRows;
+  const int rep = a.n_q / a.s.n_k, rows = rep < s.rows ? rep : s.rows;
   if (s.groups >= 16 * s.opens)
     hipLaunchKernelGGL((decode_join_kernel<D, 8>), dim3(s.opens, rows, 8), dim3(kThreads), 0,
-                       stream, a, s.opens, s.groups);
+                       stream, a, s.opens, s.groups, s.rows);
   else
     hipLaunchKernelGGL((decode_join_kernel<D, 1>), dim3(s.opens, rows), dim3(kThreads), 0, stream,
-                       a, s.opens, s.groups);
+                       a, s.opens, s.groups, s.rows);
   return hipGetLastError();
 }
 
@@ -673,10 +687,6 @@ hipError_t decode_dim(const DecodeArgs &a, hipStream_t stream) {
 }
 
 }  // namespace
-
-size_t decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_len) {
-  return shape_of(b, n_q, n_k, d, max_len).bytes;
-}
 
 hipError_t launch_attn_decode(const DecodeArgs &a, hipStream_t stream) {
   switch (a.s.d) {

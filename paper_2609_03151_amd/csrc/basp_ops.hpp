@@ -85,7 +85,46 @@ struct DecodeArgs {
   void *workspace;  // NULL where no head is shared by two workgroups
 };
 
-size_t decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_len);
+// How a call is cut.  A workgroup serves up to 16 query heads of a kv head at
+// once, 32 where a kv head has more than 16.
+constexpr int kDecodeUnit = 128;  // keys of a unit
+
+// For each head, as dealt out, or workgroup that may leave partial results: where
+// they lie.
+struct DecodeOpen {
+  int row0, heads, count, first;
+};
+
+struct DecodeCut {
+  int rows;        // query heads of a workgroup: 16 or 32
+  int row_groups;  // workgroups' worth of query heads per kv head
+  int groups;      // workgroups
+  int opens;       // DecodeOpen descriptors: the smaller of heads and workgroups
+  size_t bytes;    // workspace; 0 where no head is shared by two workgroups
+};
+
+// Workgroups: three per CU at most (two of 32 rows).  One per CU alone has enough
+// bytes in flight to fill the memory; three let more of them start on a short call
+// (8 ragged sequences of up to 8K tokens, 8 heads on 2: 14.9 us against 16.1 with
+// two), four leave a long sequence in more parts to join (one of 128K in 8 bits:
+// 16.5 us with three, 19.5 with four).
+inline DecodeCut decode_cut(int b, int n_q, int n_k, int d, int max_len) {
+  DecodeCut c;
+  const int rep = n_q / n_k;
+  c.rows = rep > 16 ? 32 : 16;
+  c.row_groups = (rep + c.rows - 1) / c.rows;
+  const long long most = 256 * (c.rows == 16 ? 3 : 2);
+  const long long heads = (long long)b * n_k * c.row_groups;
+  const long long units = heads * (((long long)max_len + kDecodeUnit - 1) / kDecodeUnit);
+  c.groups = (int)(units < most ? units : most);
+  c.opens = (int)(heads < c.groups ? heads : c.groups);
+  // per workgroup its first and its last head's rows: (m, l) and O
+  c.bytes = max_len <= kDecodeUnit
+                ? 0
+                : c.opens * sizeof(DecodeOpen) +
+                      (size_t)c.groups * 2 * c.rows * (2 + d) * sizeof(float);
+  return c;
+}
 
 hipError_t launch_attn_decode(const DecodeArgs &a, hipStream_t stream);
 

@@ -197,6 +197,17 @@ def test_decode_heads_and_dims(d, e4m3, n_q, n_k, page):
     _check_decode(_randn(len(lens), n_q, d, seed=9), kp, vp, table, lens, kw)
 
 
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("n_q,n_k,L", [(17, 1, 700), (32, 1, 129), (33, 1, 300), (64, 2, 2000),
+                                       (80, 1, 1000)])
+def test_decode_many_query_heads(d, e4m3, n_q, n_k, L):
+    """More than 16 query heads on a kv head: 32 to a workgroup, and several of these."""
+    lens = [L, 0, L // 3, 1]
+    kp, vp, table, kw = _filled(lens, n_k, 32, d, e4m3, seed=n_q)
+    _check_decode(_randn(4, n_q, d, seed=9), kp, vp, table, lens, kw)
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("b,L,n_q,n_k,d,page", [
     (1, 1, 8, 1, 128, 64), (1, 5000, 8, 1, 128, 64), (1, 70001, 8, 1, 128, 64),
