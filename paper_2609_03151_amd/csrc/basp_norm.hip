@@ -310,25 +310,26 @@ __global__ __launch_bounds__(kThreads) void norm_rope_bwd_kernel(const NormArgs 
 }
 
 // dw of one side: the sum of its workgroups' partial rows, 16 columns per
-// workgroup, 16 threads a column, each over every 16th row.
+// workgroup, four a thread, 64 threads each over every 64th row.
 template <int D>
 __global__ __launch_bounds__(kThreads) void norm_dw_kernel(const NormArgs a, const float *partials,
                                                            uint32_t q_blocks, uint32_t k_blocks) {
   const bool is_k = blockIdx.y;
   const uint32_t first = is_k ? q_blocks : 0, n = is_k ? k_blocks : q_blocks;
-  const int col = blockIdx.x * 16 + threadIdx.x % 16, lane = threadIdx.x / 16;
-  float t = 0.f;
+  const int col = blockIdx.x * 16 + threadIdx.x % 4 * 4, row = threadIdx.x / 4;
+  f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (uint32_t i = lane; i < n; i += 16) t += partials[(size_t)(first + i) * D + col];
-  __shared__ float part[16][16];
-  part[lane][threadIdx.x % 16] = t;
-  __syncthreads();
-  if (lane == 0) {
-    t = 0.f;
+  for (uint32_t i = row; i < n; i += 64)
+    t += *reinterpret_cast<const f32x4 *>(partials + (size_t)(first + i) * D + col);
+  __shared__ float part[64][17];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += part[i][threadIdx.x];
-    a.side[is_k].dw[col] = t;
-  }
+  for (int i = 0; i < 4; ++i) part[row][threadIdx.x % 4 * 4 + i] = t[i];
+  __syncthreads();
+  // 16 threads a column, four rows each, then the 16 by lane exchange
+  const int c = threadIdx.x / 16, r = threadIdx.x % 16;
+  float x = part[r][c] + part[r + 16][c] + (part[r + 32][c] + part[r + 48][c]);
+  x = group_sum<16>(x);
+  if (r == 0) a.side[is_k].dw[blockIdx.x * 16 + c] = x;
 }
 
 // Whether a call's inputs are read with the non-temporal hint: where what it
