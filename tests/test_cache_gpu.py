@@ -455,3 +455,33 @@ def test_captured_steps(e4m3):
         assert torch.equal(kp.view(torch.uint8), kp2.view(torch.uint8)), i
         for s, n in enumerate(here):
             now[s] = n if n else now[s]
+
+
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("b,n_q,L", [(1, 8, 3000), (7, 5, 300), (40, 20, 500)])
+def test_decode_and_read_write_nothing_else(d, e4m3, b, n_q, L):
+    """Outputs and workspace inside larger buffers: what lies around them stays, and a workspace of the
+    size reported is enough."""
+    lens = [L] + [(37 * i) % L for i in range(1, b)]
+    kp, vp, table, kw = _filled(lens, 1, 32, d, e4m3)
+
+    def inside(dtype, shape):
+        n = math.prod(shape)
+        buf = torch.full((n + 128,), 7.0, dtype=dtype, device="cuda")
+        return buf, buf[64:64 + n].view(shape)
+
+    need = basp.attn_decode_workspace_bytes(b, n_q, 1, d, L)
+    assert need % 4 == 0
+    ob, o = inside(BF16, (b, n_q, d))
+    lb, lse = inside(F32, (b, n_q))
+    wb, ws = inside(F32, (need // 4,))
+    kb, k = inside(BF16, (b, 33, 1, d))
+    vb, v = inside(BF16, (b, 33, 1, d))
+    q = _randn(b, n_q, d, seed=3)
+    basp.attn_decode(q, kp, vp, table, _ints(lens), max_len=L, out=o, lse=lse, workspace=ws, **kw)
+    basp.kv_read(kp, vp, table, 33, count=_ints([min(33, n) for n in lens]), k=k, v=v, **kw)
+    for buf in (ob, lb, wb, kb, vb):
+        assert (buf[:64] == 7).all() and (buf[-64:] == 7).all()
+    ro, rl = basp.attn_decode(q, kp, vp, table, _ints(lens), max_len=L, **kw)
+    assert torch.equal(o, ro) and torch.equal(lse, rl)

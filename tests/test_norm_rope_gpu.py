@@ -236,3 +236,45 @@ def test_captured_and_other_stream():
         want = both(None)
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(got, want)), i
+
+
+def test_norm_alone_with_positions():
+    """No rotation: positions only mark padding, however large they are."""
+    q, k, qw, kw, rn = _inputs(2, 9, 3, 1, 96, BF16)
+    pos = torch.arange(18, dtype=torch.int32, device="cuda").view(2, 9) * 10 ** 8
+    pos[1, 4] = -3
+    qo, ko = basp.qk_norm_rope(q, k, qw, kw, None, None, positions=pos)
+    for name, x, w, y in (("q", q, qw, qo), ("k", k, kw, ko)):
+        check(name, y, *norm_rope_ref(x, w, None, None, pos, 1e-6, 0, False), BF16)
+    dy = rn(*q.shape, t=F32), rn(*k.shape, t=F32)
+    dq, dk, dqw, dkw = basp.qk_norm_rope_bwd(q, k, *dy, qw, kw, None, None, positions=pos)
+    for name, x, g, w, dx, dw in (("dq", q, dy[0], qw, dq, dqw), ("dk", k, dy[1], kw, dk, dkw)):
+        rx, bx, rw, bw = norm_rope_bwd_ref(x, g, w, None, None, pos, 1e-6, 0, False)
+        check(name, dx, rx, bx, F32)
+        check(name + "_weight", dw, rw, bw, F32)
+
+
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+def test_writes_nothing_else(d):
+    """Outputs inside larger buffers: what lies around them stays."""
+    b, S, n_q, n_k = 3, 23, 5, 1
+    q, k, qw, kw, rn = _inputs(b, S, n_q, n_k, d, BF16)
+    cos, sin = basp.rope_table(S, d)
+    dy = rn(*q.shape, t=F32), rn(*k.shape, t=F32)
+
+    def inside(n, dtype, shape):
+        buf = torch.full((n + 128,), 7.0, dtype=dtype, device="cuda")
+        return buf, buf[64:64 + n].view(shape)
+
+    outs = {n: inside(t.numel(), dt, t.shape) for n, t, dt in (
+        ("q_out", q, BF16), ("k_out", k, BF16), ("dq", q, F32), ("dk", k, F32),
+        ("dq_weight", qw, F32), ("dk_weight", kw, F32))}
+    ws, space = inside(basp.qk_norm_rope_bwd_workspace_bytes(b, S, n_q, n_k, d) // 4, F32, (-1,))
+    view = lambda *names: {n: outs[n][1] for n in names}  # noqa: E731
+    basp.qk_norm_rope(q, k, qw, kw, cos, sin, **view("q_out", "k_out"))
+    basp.qk_norm_rope_bwd(q, k, *dy, qw, kw, cos, sin, workspace=space,
+                          **view("dq", "dk", "dq_weight", "dk_weight"))
+    for buf in [ws, *(x[0] for x in outs.values())]:
+        assert (buf[:64] == 7).all() and (buf[-64:] == 7).all()
+    want = basp.qk_norm_rope(q, k, qw, kw, cos, sin)
+    assert torch.equal(outs["q_out"][1], want[0]) and torch.equal(outs["k_out"][1], want[1])
