@@ -165,18 +165,18 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(const NormArgs a, u
   const uint32_t token = s.by_chunks.div(unit), h0 = (unit - token * s.chunks) * kHeads;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f}, one = {1.f, 1.f, 1.f, 1.f};
   int heads = 0, pos = 0;
-  f32x4 xa[kHeads], xb[kHeads];
+  f32x4 xa[kHeads], xb[kHeads];  // zero in lanes past a row's end, which its sum includes
+#pragma unroll
+  for (int h = 0; h < kHeads; ++h) xa[h] = xb[h] = zero;
   if (on) {
     heads = s.n - h0 < kHeads ? s.n - h0 : kHeads;
     const T *x = static_cast<const T *>(s.x) + (long long)token * s.x_row + (size_t)h0 * D;
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
-      xa[h] = xb[h] = zero;
+    for (int h = 0; h < kHeads; ++h)
       if (h < heads) {
         xa[h] = load4<NT>(x + h * D + lc.a);
         xb[h] = load4<NT>(x + h * D + lc.b);
       }
-    }
     pos = a.positions ? a.positions[token] : a.pos0 + (int)(token - a.by_S.div(token) * a.S);
   }
   f32x4 ca = one, cb = one, sa = zero, sb = zero;  // y_a = x_a ca + (its partner) sa

@@ -278,3 +278,17 @@ def test_writes_nothing_else(d):
         assert (buf[:64] == 7).all() and (buf[-64:] == 7).all()
     want = basp.qk_norm_rope(q, k, qw, kw, cos, sin)
     assert torch.equal(outs["q_out"][1], want[0]) and torch.equal(outs["k_out"][1], want[1])
+
+
+@pytest.mark.parametrize("d", [64, 80, 96, 128])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_reads_its_rows_alone(d, dtype):
+    """NaN around the heads that a call takes, in rows shorter than their lanes and head counts that
+    leave a group short, reaches neither outputs nor gradients."""
+    b, S, n_q, n_k = 2, 21, 5, 2
+    q, k, qw, kw, rn = _inputs(b, S, n_q, n_k, d, dtype, seed=d)
+    cos, sin = basp.rope_table(S, d)
+    buf = torch.full((b, S, n_q + n_k + 3, d), torch.nan, dtype=dtype, device="cuda")
+    buf[:, :, 1:1 + n_q], buf[:, :, 2 + n_q:2 + n_q + n_k] = q, k
+    _run_both(buf[:, :, 1:1 + n_q], buf[:, :, 2 + n_q:2 + n_q + n_k], qw, kw, cos, sin, None, 1e-6,
+              d, False, F32, rn)
