@@ -78,7 +78,7 @@ basp::NormArgs norm_args(const void *q, const void *k, const float *qw, const fl
   a.by_S = basp::FastDiv::make(a.S);
   a.rot = rot;
   a.table_rows = table_rows;
-  a.pos0 = pos0;
+  a.pos0 = rot > 0 ? pos0 : 0;  // else bounded by no table: pos0 + t may pass 2^31
   a.eps = eps;
   return a;
 }

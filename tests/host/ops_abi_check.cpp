@@ -104,6 +104,12 @@ int main() {
   CHECK(g_norm.side[0].rows == 84000 && g_norm.side[1].rows == 12000 && g_norm.rot == 48);
   CHECK(g_norm.side[0].x == p[0] && g_norm.side[1].y == p[3] && g_norm.side[1].y_row == 384);
   CHECK(g_norm.by_S.div(2999) == 2 && g_norm.side[1].by_n.div(11) == 2);
+  // Without rotation no table bounds pos0, and pos0 + t in 32 bits must not come out
+  // negative, the mark of padding.
+  CHECK(basp_qk_norm_rope(p[0], p[1], p[2], p[3], f[4], f[5], nullptr, nullptr, nullptr, 4, 3000, 7, 1,
+                          96, 0, 0, 1024, 96, 672, 96, 1e-6f, INT_MAX, 0, BASP_BF16,
+                          nullptr) == BASP_OK);
+  CHECK((long long)g_norm.pos0 + 3000 <= INT_MAX);
   unsigned char *sc[2] = {static_cast<unsigned char *>(p[4]), static_cast<unsigned char *>(p[5])};
   CHECK(basp_kv_write(p[0], p[1], p[2], p[3], sc[0], sc[1], table, ints, ints, 5, 33, 2, 128, 256, 77,
                       9, 1024, 512, BASP_E4M3, nullptr) == BASP_OK);

@@ -292,3 +292,12 @@ def test_reads_its_rows_alone(d, dtype):
     buf[:, :, 1:1 + n_q], buf[:, :, 2 + n_q:2 + n_q + n_k] = q, k
     _run_both(buf[:, :, 1:1 + n_q], buf[:, :, 2 + n_q:2 + n_q + n_k], qw, kw, cos, sin, None, 1e-6,
               d, False, F32, rn)
+
+
+def test_norm_alone_behind_any_position():
+    """No rotation: pos0 has no effect, however large."""
+    q, k, qw, kw, rn = _inputs(2, 9, 3, 1, 80, BF16)
+    dy = rn(*q.shape, t=F32), rn(*k.shape, t=F32)
+    both = [(*basp.qk_norm_rope(q, k, qw, kw, None, None, pos0=p),
+             *basp.qk_norm_rope_bwd(q, k, *dy, qw, kw, None, None, pos0=p)) for p in (0, 2 ** 31 - 1)]
+    assert all(torch.equal(x, y) for x, y in zip(*both)) and both[0][0].any()
