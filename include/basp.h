@@ -523,7 +523,7 @@ size_t basp_attn_decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_
  * contents ignored on entry; calls that may overlap on the device, two captured
  * graphs among them, need one each.  q and o 16-byte aligned, lse 4.
  * Also SHAPE when n_q % n_k != 0, UNSUPPORTED when scale is not finite and positive,
- * b*n_q >= 2^22, max_len > 2^30 or b*n_q*(max_len/128) >= 2^31, and WORKSPACE. */
+ * b*n_q >= 2^22, max_len > 2^30 or b*n_q*ceil(max_len/128) >= 2^30, and WORKSPACE. */
 int basp_attn_decode(const void *q, const void *k_pages, const void *v_pages,
                      const unsigned char *k_scales, const unsigned char *v_scales,
                      const int *block_table, const int *lens, void *o, float *lse,

@@ -231,12 +231,13 @@ int run_cache(bool write, const void *k, const void *v, const void *k_pages, con
 }
 
 // Shape rules of basp_attn_decode.  The kernel counts units of 128 keys or more
-// per (sequence, head), and keys up to a unit past a length, in 32 bits.
+// per (sequence, head), what it deals out by adding the workgroups less one, and keys
+// up to a unit past a length, in 32 bits.
 int check_decode(int b, int n_q, int n_k, int d, int max_len) {
   if (b < 0 || n_q < 1 || n_k < 1 || d < 1 || max_len < 1 || n_q % n_k != 0) return BASP_ERR_SHAPE;
   if (!head_dim(d) || (uint64_t)b * (uint64_t)n_q >= (1ull << 22) || max_len > (1 << 30))
     return BASP_ERR_UNSUPPORTED;
-  if ((uint64_t)b * (uint64_t)n_q * (((uint64_t)max_len + 127) / 128) >= (1ull << 31))
+  if ((uint64_t)b * (uint64_t)n_q * (((uint64_t)max_len + 127) / 128) >= (1ull << 30))
     return BASP_ERR_UNSUPPORTED;
   return BASP_OK;
 }

@@ -177,3 +177,11 @@ def test_rope_table():
     p, i = 199999, 3
     a = p * 500000.0 ** (-2 * i / 64)
     assert abs(cos[p, i].item() - math.cos(a)) < 1e-6 and abs(sin[p, i].item() - math.sin(a)) < 1e-6
+
+
+def test_attn_decode_counts_in_32_bits():
+    """Units of keys of all heads, and workgroups on top in the division that deals them out, are
+    32-bit counts on the device."""
+    f = basp.attn_decode_workspace_bytes
+    assert f(2 ** 22 - 1, 1, 1, 64, 65536) == 0 == f(2 ** 15, 1, 1, 64, 2 ** 22)
+    assert f(2 ** 15 - 1, 1, 1, 64, 2 ** 22) > 0
