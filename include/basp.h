@@ -405,6 +405,9 @@ int basp_attn_bwd_sharded(const void *const *q_shards,
  * positions: int32 [b, S], or NULL for pos0 + t (t the token's index in its
  * sequence).  A negative position marks a row of padding: its outputs are
  * zeros.  A position of table_rows or more gives NaN.
+ * All arithmetic is fp32, the sum of squares included: beyond its range (a row of
+ * magnitudes past 10^18; with eps = 0 also one of less than 10^-18) results follow
+ * from that sum's overflow to infinity or underflow to 0.
  * Alignment: q, k, qo, ko and their row strides to 4 elements; weights and
  * tables 16 bytes; positions 4.
  * Head dims 64, 80, 96 and 128; rot a multiple of 8, 0 <= rot <= d.

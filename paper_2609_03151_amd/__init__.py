@@ -586,7 +586,7 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, eps: float = 1e-6, position
     will do); weights fp32 [d], or both None for no norm; ``cos``, ``sin`` fp32 [positions, rot/2]
     (``rope_table`` makes them), or both None for no rotation.  A token's position is
     ``positions`` int32 [b, S] (negative: a row of padding, zeros out), or pos0 + its index.
-    Returns (q_out, k_out) in q's type."""
+    Returns (q_out, k_out) in q's type; ``q_out`` may be ``q`` itself, ``k_out`` ``k``."""
     dev, dims, w, turn, code = _norm_args(q, k, q_weight, k_weight, cos, sin, positions)
     dt, q_shape, k_shape, d = q.dtype, q.shape, k.shape, dims[4]
     qp, q_row = _rows(q, "q", dt, q_shape, dev)
