@@ -39,8 +39,8 @@ between the pack and attention, and the backward goes through both:
 buffers in place has no such step: there the owner of a shard calls
 qk_norm_rope on it before the exchange.
 
-After a forward `fill_cache` puts the prompt's K and V into a paged cache, and
-`decode` takes the share on by one token per sequence.
+After a forward, either one, `fill_cache` puts the prompt's K and V into a paged
+cache, and `decode` takes the share on by one token per sequence.
 """
 from __future__ import annotations
 
@@ -115,16 +115,20 @@ class RankShare:
                 self.dk_weight = torch.empty_like(norm_rope.k_weight)
                 ws = max(ws, qk_norm_rope_bwd_workspace_bytes(b, S, self.Hl, self.Hkl, d))
         self.workspace = torch.empty(max(ws, 16), dtype=torch.uint8, device=dev)
+        # where the last forward's K and V are: "local" (k, v), "shards", or in neither
+        self._kv = None
 
     # individual steps, so that callers can time them
     def pack_qkv(self):
         pack_qkv(self.q_shards, self.k_shards, self.v_shards, self.rank, q=self.q_in, k=self.k_in,
                  v=self.v)
+        self._kv = "local" if self.norm_rope is None else None
 
     def qk_norm_rope(self):
         n = self.norm_rope
         qk_norm_rope(self.q_in, self.k_in, n.q_weight, n.k_weight, n.cos, n.sin, eps=n.eps,
                      interleaved=n.interleaved, q_out=self.q, k_out=self.k)
+        self._kv = "local"
 
     def attn_fwd(self):
         attn_fwd(self.q, self.k, self.v, G=self.G, scale=self.scale, out=self.o, lse=self.lse,
@@ -159,6 +163,7 @@ class RankShare:
         self.pack_qkv()
         if self.norm_rope is not None:
             self.qk_norm_rope()
+        self._kv = "local"
         self.attn_fwd()
         self.unpack_o()
 
@@ -176,9 +181,20 @@ class RankShare:
     # generation after the prompt
     def fill_cache(self, cache, block_table):
         """K and V of the last forward into a `PagedKV`, sequence s's tokens from position 0 on in the
-        pages that row s of the block table lists."""
-        start = torch.zeros(self.b, dtype=torch.int32, device=self.k.device)
-        cache.write(self.k, self.v, block_table, start)
+        pages that row s of the block table lists.  After `forward_sharded` the rank's head is read
+        from the shard buffers, which must still hold that forward's K and V.  The last forward is
+        the one that Python called last: the replay of a captured one does not count."""
+        if self._kv is None:
+            raise RuntimeError("fill_cache takes K and V of a forward: call one first")
+        dev, i32 = self.k.device, torch.int32
+        if self._kv == "local":
+            cache.write(self.k, self.v, block_table, torch.zeros(self.b, dtype=i32, device=dev))
+            return
+        Sg, h = self.S // self.G, self.rank * self.H_kv // self.G
+        first = Sg * torch.arange(self.G, dtype=i32, device=dev)  # token of each shard
+        start = first[:, None].expand(self.G, self.b).contiguous()
+        for k, v, at in zip(self.k_shards, self.v_shards, start):
+            cache.write(k[:, :, h:h + self.Hkl], v[:, :, h:h + self.Hkl], block_table, at)
 
     def decode(self, cache, q, k, v, block_table, lens, max_len: int | None = None, workspace=None):
         """One new token per sequence: q [n, 1, H/G, d] and k, v [n, 1, Hkl, d], the rank's heads of
@@ -204,6 +220,7 @@ class RankShare:
         self._check_in_place()
         attn_fwd_sharded(self.q_shards, self.k_shards, self.v_shards, self.o_shards, self.rank,
                          scale=self.scale, lse=self.lse)
+        self._kv = "shards"
 
     def backward_sharded(self):
         self._check_in_place()
