@@ -575,7 +575,7 @@ def _norm_args(q, k, q_weight, k_weight, cos, sin, positions):
         if half == 0:  # no columns: nothing is rotated
             c = sn = None
     pos = None if positions is None else _on(positions, "positions", _I32, (b, S), dev)
-    return dev, (b, S, n_q, n_k, d, 2 * half, rows), (qw, kw), (c, sn, pos), _dtype_code(q)
+    return dev, (b, S, n_q, n_k, d, 2 * half, _int(rows)), (qw, kw), (c, sn, pos), _dtype_code(q)
 
 
 def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, eps: float = 1e-6, positions=None,
@@ -699,7 +699,7 @@ def _pages(k_pages, v_pages, k_scales, v_scales, table, b, dev: int):
     t_shape = table.shape
     return ((*_two(k_pages, "k_pages", v_pages, "v_pages", dt, shape, dev), ks, vs,
              _on(table, "block_table", _I32, t_shape, dev)),
-            (n_k, d, page, n_pages, t_shape[1]), code)
+            (n_k, d, page, n_pages, _int(t_shape[1])), code)
 
 
 def kv_write(k, v, k_pages, v_pages, block_table, start, count=None, k_scales=None,
