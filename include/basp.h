@@ -521,7 +521,12 @@ size_t basp_attn_decode_workspace_bytes(int b, int n_q, int n_k, int d, int max_
  * Products in bf16 with fp32 accumulation (an 8-bit key or value is exact in
  * bf16, scales are applied in fp32, a weight is the sum of two bf16), softmax in
  * fp32, O rounded once; deterministic.  A NaN or infinity among the values that a
- * head attends to makes its element of O one of these.
+ * head attends to makes its element of O one of these, and so may values whose
+ * magnitudes add up to 2^128 or more over the keys: O's sum, of weights of at most
+ * 1, is fp32 before it is divided.  A score of plus infinity or NaN makes its
+ * head's O and LSE NaN; minus infinity takes its key out, and where that leaves
+ * none O is NaN and LSE -inf.  lens and block_table must not change while the
+ * call runs.
  * workspace: basp_attn_decode_workspace_bytes() or more, 16-byte aligned;
  * contents ignored on entry; calls that may overlap on the device, two captured
  * graphs among them, need one each.  q and o 16-byte aligned, lse 4.
