@@ -7,7 +7,9 @@ exchange of cached tokens.  A sequence's tokens lie in pages of `page` tokens, l
 of a block table; which page a sequence gets is the caller's.
 
 In 8 bits (`torch.float8_e4m3fn`) a token of one head is stored as e4m3 values with one
-power-of-two scale, off by at most 2^-4 of each value, at half the bytes (129 for 256 at d = 128).
+power-of-two scale 2^e, at half the bytes (129 for 256 at d = 128).  A value is off by at most 2^-4 of
+itself, or by 2^-10 * 2^e if that is more: values below 2^-6 * 2^e keep fewer bits, and those below
+2^-10 * 2^e are stored as 0.  The row's largest is above 224 * 2^e (or e is -110, its least).
 """
 from __future__ import annotations
 

@@ -7,8 +7,8 @@
 // one scale byte e + 127: e is the least whole number (-110 or more) with
 // max finite |x| <= 448 * 2^e.  A power of two costs nothing in precision (an
 // e4m3 value keeps its four significant bits at any scale, so a finer scale would only
-// move which values fall below the least normal one, 2^-6 * 2^e, at 2^-15 of
-// the row's maximum or less) and makes every step but the rounding of v exact:
+// move which values fall below the least normal one, 2^-6 * 2^e: with the maximum in
+// (224, 448] * 2^e that is 2^-14.8 to 2^-13.8 of it) and makes every step but the rounding of v exact:
 // x * 2^-e, v * 2^e in bf16, and the scores and weights that attention multiplies.
 //
 // Both kernels are bound by HBM: one group of 16 lanes (8 at d = 64) per token
