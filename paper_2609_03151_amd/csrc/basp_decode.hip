@@ -2,17 +2,22 @@
 // key-value cache:
 //   O = sum_{j < len} softmax_j(scale q . k_j) v_j,  LSE = log sum_j exp(scale q . k_j).
 //
-// Bound by HBM: every key and value of the cache is read once, for 4 n_q/n_k
-// operations a byte of bf16 (16 on 8 query heads a kv head), which is more than
-// the vector units do beside such a stream and little for the matrix cores.
+// Bound by HBM: every key and value of the cache is read once, for n_q/n_k
+// operations a byte of bf16 and twice that in 8 bits (8 and 16 on 8 query heads a kv
+// head; the second product of the weights, which are two bf16, is half as much
+// again).  That is more than the vector units do beside such a stream and little for the
+// matrix cores.
 //
-// The keys of all sequences are dealt out evenly: a unit is 128 keys of one kv
+// The keys of all sequences are dealt out in runs: a unit is 128 keys of one kv
 // head for up to 16 of its query heads (32 where it has more than 16), and each of at
-// most 768 workgroups takes one run of units, in the order of sequences, heads and keys.  The
-// lengths are known on the device only, so each workgroup adds them up to find
-// its run.  Its four waves take a block of 32 keys of each unit, each with a running
-// maximum, sum and O of its own, joined in LDS at the end of a sequence's head or
-// of the run.  Only the first and the last head of a run can be shared with other
+// most 768 workgroups (512 of 32 heads) takes one run of units, in the order of sequences,
+// heads and keys.  All runs but the last are as long, ceil(units / workgroups): even
+// where there are many units, while 769 of them make runs of two, as 1536 do (one
+// head in bf16, 769, 1024, 1100, 1536, 1537, 2304, 2305 units: 18.7, 20.7, 23.6, 26.1,
+// 25.8, 33.7, 35.8 us).  The lengths are known on the device only, so each workgroup
+// adds them up to find its run.  Its four waves take a block of 32 keys of each unit,
+// each with a running maximum, sum and O of its own, joined in LDS at the end of a
+// sequence's head or of the run.  Only the first and the last head of a run can be shared with other
 // workgroups; their partial results are joined by a second kernel:
 //   M = max_i m_i,  O = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i
 // (scores in log2 units).  Splits of a fixed number of keys, one workgroup each,

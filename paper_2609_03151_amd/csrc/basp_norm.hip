@@ -336,7 +336,10 @@ __global__ __launch_bounds__(kThreads) void norm_dw_kernel(const NormArgs a, con
 // moves (`bytes`) does not stay in the 256 MB of the last-level cache anyway.  128K
 // tokens of 8 + 1 heads of 128 in bf16 (604 MB): 130 -> 120 us, their backward 301 ->
 // 269; but 4K tokens of 8 + 2 heads (21 MB, the inputs still cached) 6.6 -> 7.1,
-// backward 16.2 -> 17.6.  Results are stored with the hint always (137 -> 130, 4K
+// backward 16.2 -> 17.6.  The other types are alike (8 + 2 heads of 128, without -> with):
+// fp32 forward 100 MB 19.1 -> 20.6, 400 MB 73.3 -> 71.3, 1 GB 188 -> 174; backward of
+// fp32 with fp32 gradients 23.6 -> 25.5, 83.4 -> 79.5, 213 -> 195, of bf16 with bf16
+// gradients 24.9 -> 27.1, 86.3 -> 85.1, 218 -> 200.  Results are stored with the hint always (137 -> 130, 4K
 // tokens 7.6 -> 6.6).
 bool streams(const NormArgs &a, int d, int bytes_per_element) {
   return ((uint64_t)a.side[0].rows + a.side[1].rows) * d * bytes_per_element > 192ull << 20;
