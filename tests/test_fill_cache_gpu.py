@@ -35,3 +35,39 @@ def test_either_forward_fills_the_same_cache(dtype, b, S, H, H_kv, d, G, rank):
         h = rank * H_kv // G
         for x, shards in ((got[0][0], sh.k_shards), (got[0][1], sh.v_shards)):
             assert torch.equal(x, torch.cat(shards, 1)[:, :, h:h + sh.Hkl])
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_captured_prompt(in_place):
+    """A forward and the cache's filling in one graph, replayed on new shards, against eager ones."""
+    b, S, H, H_kv, d, G, rank, page = 2, 512, 8, 4, 128, 2, 1, 64
+    w = small_workload(b=b, S=S, H=H, H_kv=H_kv, d=d, G=G, rank=rank, seed=23)
+    dev = lambda x: [s.cuda() for s in shards_of(x, w)]  # noqa: E731
+    sh = RankShare(*(dev(t) for t in global_tensors(w)), G=G, rank=rank, scale=w.scale)
+    mp = S // page
+    table = torch.randperm(b * mp, generator=torch.Generator().manual_seed(2)).view(b, mp).to(I32).cuda()
+    one, two = (PagedKV(b * mp, sh.Hkl, d, page=page) for _ in range(2))
+
+    def prompt(cache):
+        (sh.forward_sharded if in_place else sh.forward)()
+        sh.fill_cache(cache, table)
+
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        prompt(one)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            prompt(one)
+    g = torch.Generator("cuda").manual_seed(9)
+    for i in range(4):
+        for t in (*sh.q_shards, *sh.k_shards, *sh.v_shards):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        prompt(two)
+        torch.cuda.synchronize()
+        assert torch.equal(one.k_pages, two.k_pages) and torch.equal(one.v_pages, two.v_pages), i
+        k, _ = two.read(table, S)
+        h = rank * H_kv // G
+        assert torch.equal(k, torch.cat(sh.k_shards, 1)[:, :, h:h + sh.Hkl]), i
