@@ -29,6 +29,8 @@
  *   basp_kv_write / basp_kv_read   the rank's K and V into the pages of a
  *                  key-value cache (bf16, or 8 bits with a scale), and back
  *   basp_attn_decode   attention of one new token per sequence over the pages
+ *   basp_attn_span_fwd / basp_attn_span_bwd   attention of packed documents,
+ *                  prefixes and padding, with capped and biased scores
  *
  * The exchange itself (RCCL) is not part of this library.
  *
@@ -538,6 +540,70 @@ int basp_attn_decode(const void *q, const void *k_pages, const void *v_pages,
                      void *workspace, size_t workspace_bytes, int b, int n_q, int n_k, int d,
                      int page, int n_pages, int max_pages, int max_len, long long q_row,
                      float scale, basp_dtype cache_dtype, void *stream);
+
+/* ------------------------------------------------ attention over spans
+ *
+ * Sequences that hold several documents, prefixes that all of a document sees, and
+ * padding: query i sees the keys lo <= j < hi of its span and no others.  Its scores
+ * may be capped and biased by distance:
+ *   s_ij = scale * q_i . k_j
+ *   u_ij = cap * tanh(s_ij / cap) - slope_h * |i - j|    (u = s without a cap)
+ *   P_ij = exp(u_ij) / sum_{lo_i <= j < hi_i} exp(u_ij), 0 outside the span
+ *   O_i = sum_j P_ij v_j,  LSE_i = log sum_j exp(u_ij)
+ * on the rank's head-sharded tensors (Sec. II-C), as basp_attn_fwd, of which this is
+ * the general form (spans [0, i + 1), no cap, no slopes).
+ *
+ * spans: int32 [b, S, 2], (lo, hi) of every row, cut to [0, S]; hi <= lo: the row sees
+ * nothing (padding), its O is 0, its LSE -inf and all its gradients 0.  NULL: causal.
+ * Spans are read on the device; whatever they hold, nothing outside the tensors is
+ * read.  slopes: fp32 [n_q], any finite numbers, constants of the model (no
+ * gradients), or NULL.  cap: 0 for none, else up to 1024.
+ * q [b, S, n_q, d], k and v [b, S, n_k, d] bf16, tokens q_row (k_row, v_row) elements
+ * apart, b*S of them in one run, so they may be columns of one projection's output;
+ * n_q a multiple of n_k, query head h takes kv head h / (n_q/n_k).
+ * Products in bf16 with fp32 accumulation (P and dS rounded to bf16 for their
+ * products), softmax in fp32; deterministic.  tanh is off by at most 2^-21, so a capped
+ * score by 2^-21 * cap; a bias and an LSE are fp32 numbers, off by 2^-24 of
+ * themselves: rows all of whose keys are far away, |slope * distance| past 2^12, see that in
+ * P.  A value, key, query or gradient outside every span that it would meet does not
+ * count, infinities and NaN too; inside one they make what they reach NaN: a value
+ * its element of O, a score of plus infinity or NaN its row.
+ * Conditions: d 64, 80, 96 or 128; scale finite and positive; 16-byte aligned q, k, v, o,
+ * d_o and gradients, strides multiples of 8; spans 8, lse and slopes 4.  Errors: NULL, SHAPE
+ * (negative size, n_q % n_k != 0, a row stride below n*d), UNSUPPORTED (d, scale, cap;
+ * (S + 256) * row stride * 2 >= 2^31 bytes for any of the tensors, b > 65535, or b*n_q
+ * times S rounded up to 64 >= 2^27),
+ * ALIGN, HIP; b == 0 or S == 0 enqueues nothing. */
+
+/* o [b, S, n_q, d] bf16 and lse [b, n_q, S] fp32 (natural logarithm), contiguous. */
+int basp_attn_span_fwd(const void *q, const void *k, const void *v, const int *spans,
+                       const float *slopes, void *o, float *lse, int b, int S, int n_q, int n_k,
+                       int d, long long q_row, long long k_row, long long v_row, float scale,
+                       float cap, void *stream);
+
+/* Bytes of device workspace basp_attn_span_bwd needs: LSE and D per row and head, the
+ * rows' spans, and partial sums of dK and dV.  0 for an invalid or empty shape. */
+size_t basp_attn_span_bwd_workspace_bytes(int b, int S, int n_q, int n_k, int d);
+
+/* Gradients of sum(O * dO), with D_i = dO_i . O_i and t_ij = tanh(s_ij / cap) (0 without
+ * a cap):
+ *   dS_ij = P_ij (dO_i . v_j - D_i) (1 - t_ij^2)
+ *   dQ_i = scale sum_j dS_ij k_j
+ *   dK_j = scale sum_h sum_i dS_ij q_i,  dV_j = sum_h sum_i P_ij dO_i
+ * (over the rows whose span holds j, and the query heads of j's kv head).  o, lse: what
+ * basp_attn_span_fwd gave for the same arguments; o, d_o [b, S, n_q, d] bf16,
+ * contiguous.  dq, dk, dv in grad_dtype (BF16, rounded once at the end, or F32),
+ * contiguous, fully overwritten; with a kv head shared by several members dk and dv are
+ * this member's part.  workspace: basp_attn_span_bwd_workspace_bytes(), 16-byte
+ * aligned, contents ignored on entry; calls that may overlap on the device, two
+ * captured graphs among them, need one each.  Also WORKSPACE, and UNSUPPORTED where the
+ * units of work pass 2^23 (a thousand heads of 128K tokens). */
+int basp_attn_span_bwd(const void *q, const void *k, const void *v, const int *spans,
+                       const float *slopes, const void *o, const float *lse, const void *d_o,
+                       void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
+                       int b, int S, int n_q, int n_k, int d, long long q_row, long long k_row,
+                       long long v_row, float scale, float cap, basp_dtype grad_dtype,
+                       void *stream);
 
 #ifdef __cplusplus
 }

@@ -36,7 +36,8 @@ EXPORTS = ("basp_status_str", "basp_group_of", "basp_validate", "basp_pack",
            "basp_attn_bwd_sharded",
            "basp_qk_norm_rope", "basp_qk_norm_rope_bwd",
            "basp_qk_norm_rope_bwd_workspace_bytes", "basp_kv_write", "basp_kv_read",
-           "basp_attn_decode", "basp_attn_decode_workspace_bytes")
+           "basp_attn_decode", "basp_attn_decode_workspace_bytes",
+           "basp_attn_span_fwd", "basp_attn_span_bwd", "basp_attn_span_bwd_workspace_bytes")
 # Bytes of the static device buffer basp_attn_bwd_noalloc works in.
 NOALLOC_SCRATCH_BYTES = 128 << 20
 
@@ -97,6 +98,10 @@ def lib() -> ctypes.CDLL:
     L.basp_attn_decode_workspace_bytes.argtypes = [i] * 5
     L.basp_attn_decode_workspace_bytes.restype = sz
     L.basp_attn_decode.argtypes = [vp] * 10 + [sz] + [i] * 8 + [ll, f, i, vp]
+    L.basp_attn_span_fwd.argtypes = [vp] * 7 + [i] * 5 + [ll] * 3 + [f] * 2 + [vp]
+    L.basp_attn_span_bwd_workspace_bytes.argtypes = [i] * 5
+    L.basp_attn_span_bwd_workspace_bytes.restype = sz
+    L.basp_attn_span_bwd.argtypes = [vp] * 12 + [sz] + [i] * 5 + [ll] * 3 + [f] * 2 + [i, vp]
     for name in ("basp_group_of", "basp_validate", "basp_pack", "basp_unpack",
                  "basp_a2a_pack", "basp_a2a_unpack", "basp_a2a_pack_bf16", "basp_attn_fwd",
                  "basp_attn_bwd",
@@ -787,3 +792,114 @@ def attn_decode(q, k_pages, v_pages, block_table, lens, scale: float | None = No
     _call("basp_attn_decode", L.basp_attn_decode, dev, qp, *ptrs, _on(lens, "lens", _I32, (b,), dev),
           op, lp, ws, ws_n, b, n_q, n_k, d, page, n_pages, max_pages, max_len, q_row, scale, code)
     return out, lse
+
+
+# -------------------------------------------------- attention over spans
+_GRAD_TYPES = {torch.bfloat16: BASP_BF16, torch.float32: BASP_F32}
+
+
+def attn_spans(documents, prefix=None):
+    """Spans int32 [b, S, 2] of packed sequences, for ``attn_span_fwd``: ``documents`` integers [b, S],
+    the number of the document that each token belongs to (a document is a run of equal numbers;
+    negative: padding, which sees nothing); ``prefix`` integers [b, S] or None: how many tokens at the
+    start of the token's document all of it sees.  A token sees its document up to itself, and its
+    prefix."""
+    if documents.dim() != 2 or (prefix is not None and prefix.shape != documents.shape):
+        raise ValueError("documents and prefix must be [b, S]")
+    b, S = documents.shape
+    at = torch.arange(S, device=documents.device).expand(b, S)
+    first = torch.ones_like(documents, dtype=torch.bool)
+    first[:, 1:] = documents[:, 1:] != documents[:, :-1]
+    lo = torch.where(first, at, 0).cummax(1).values
+    hi = at + 1
+    if prefix is not None:
+        last = torch.ones_like(first)
+        last[:, :-1] = first[:, 1:]
+        end = torch.where(last, at + 1, S).flip(1).cummin(1).values.flip(1)
+        hi = torch.maximum(hi, torch.minimum(lo + prefix, end))
+    pad = documents < 0
+    return torch.stack((lo.masked_fill(pad, 0), hi.masked_fill(pad, 0)), -1).to(torch.int32)
+
+
+def _span_args(q, k, v, spans, scale, cap, slopes):
+    """Device, (q, k, v, spans, slopes) pointers, (b, S, n_q, n_k, d), row strides, (scale, cap)."""
+    dev = _device(q, "q", 4)
+    q_shape = q.shape
+    b, S, n_q, d = q_shape
+    if not isinstance(k, _Tensor) or k.dim() != 4:
+        raise ValueError("k must be [b, S, n_k, d]")
+    k_shape = k.shape
+    kb, kS, n_k, kd = k_shape
+    if kb != b or kS != S or kd != d:
+        raise ValueError("q and k disagree in shape")
+    qp, q_row = _rows(q, "q", _BF, q_shape, dev)
+    kp, k_row = _rows(k, "k", _BF, k_shape, dev)
+    vp, v_row = _rows(v, "v", _BF, k_shape, dev)
+    sp = None if spans is None else _on(spans, "spans", _I32, (b, S, 2), dev)
+    lp = None if slopes is None else _on(slopes, "slopes", _F32, (n_q,), dev)
+    if scale is None:
+        scale = d ** -0.5
+    if cap is None:
+        cap = 0.0
+    elif not cap > 0:
+        raise ValueError("cap must be positive, or None")
+    return dev, (qp, kp, vp, sp, lp), (b, S, n_q, n_k, d), (q_row, k_row, v_row), (scale, cap)
+
+
+def attn_span_fwd(q, k, v, spans, scale: float | None = None, cap: float | None = None,
+                  slopes=None, out=None, lse=None):
+    """Attention of packed documents, prefixes and padding: query i sees keys lo <= j < hi of its
+    span (int32 [b, S, 2], ``attn_spans`` makes them; None: causal).  Scores scale q.k, capped to
+    cap tanh(s / cap) where there is a ``cap``, less slopes[h] |i - j| where there are ``slopes``
+    (fp32 [n_q]).  ``q`` [b, S, n_q, d], ``k``, ``v`` [b, S, n_k, d] bf16 (columns of a fused
+    projection's output will do).  Returns (o bf16 [b, S, n_q, d], lse fp32 [b, n_q, S]); a row
+    that sees nothing has zeros and -inf."""
+    dev, ptrs, dims, strides, rule = _span_args(q, k, v, spans, scale, cap, slopes)
+    b, S, n_q, _, _ = dims
+    if out is None:
+        out = _like(q)
+        op = out.data_ptr()
+    else:
+        op = _on(out, "out", _BF, q.shape, dev)
+    if lse is None:
+        lse = q.new_empty((b, n_q, S), dtype=_F32)
+        lp = lse.data_ptr()
+    else:
+        lp = _on(lse, "lse", _F32, (b, n_q, S), dev)
+    _call("basp_attn_span_fwd", (_lib or lib()).basp_attn_span_fwd, dev, *ptrs, op, lp, *dims,
+          *strides, *rule)
+    return out, lse
+
+
+def attn_span_bwd_workspace_bytes(b, S, n_q, n_k, d) -> int:
+    return int(lib().basp_attn_span_bwd_workspace_bytes(b, S, n_q, n_k, d))
+
+
+def attn_span_bwd(q, k, v, o, lse, d_o, spans, scale: float | None = None,
+                  cap: float | None = None, slopes=None, grad_dtype: torch.dtype = torch.float32,
+                  dq=None, dk=None, dv=None, workspace=None):
+    """Backward of attn_span_fwd at its inputs, from its outputs ``o`` and ``lse`` and the gradient
+    ``d_o`` of o (bf16, contiguous): (dq, dk, dv) in ``grad_dtype`` (fp32 or bf16), contiguous.  Two
+    calls that may overlap on the device, captured graphs among them, need a ``workspace`` each
+    (default: one of its own per call)."""
+    dev, ptrs, dims, strides, rule = _span_args(q, k, v, spans, scale, cap, slopes)
+    b, S, n_q, n_k, d = dims
+    o_ptr, do_ptr = _two(o, "o", d_o, "d_o", _BF, q.shape, dev)
+    lp = _on(lse, "lse", _F32, (b, n_q, S), dev)
+    code = _GRAD_TYPES.get(grad_dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {grad_dtype}")
+    grads, out = [], []
+    for t, name, shape in ((dq, "dq", q.shape), (dk, "dk", k.shape), (dv, "dv", k.shape)):
+        if t is None:
+            t = q.new_empty(shape, dtype=grad_dtype)
+            grads.append(t.data_ptr())
+        else:
+            grads.append(_on(t, name, grad_dtype, shape, dev))
+        out.append(t)
+    L = _lib or lib()
+    need = 0 if workspace is not None else L.basp_attn_span_bwd_workspace_bytes(*dims)
+    workspace, ws, ws_n = _space(workspace, need, q, dev)
+    _call("basp_attn_span_bwd", L.basp_attn_span_bwd, dev, *ptrs, o_ptr, lp, do_ptr, *grads, ws,
+          ws_n, *dims, *strides, *rule, code)
+    return tuple(out)

@@ -39,6 +39,7 @@ FILE_FLAGS = {
     "basp_attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1",
                           "-mllvm", "-pragma-unroll-threshold=1000000"],
 }
+FILE_FLAGS["basp_span_bwd.hip"] = FILE_FLAGS["basp_attn_bwd.hip"]
 
 
 def sources():

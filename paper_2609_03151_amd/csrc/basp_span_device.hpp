@@ -1,0 +1,94 @@
+// basp_span_device.hpp -- device side of the score rule of attention over spans.
+#pragma once
+
+#include "basp_device.hpp"
+#include "basp_span.hpp"
+
+namespace basp {
+
+// buf_load16_lds_async with the wait states that a resource may need which was read
+// back from a vector register's lanes just before (kernels with more scalar values than
+// registers keep some there): five between a vector instruction's write of a scalar
+// register and a memory instruction's use of it.  The compiler does not see into the
+// asm and adds none.
+__device__ __forceinline__ void copy16_to_lds(u32x4 rsrc, uint32_t off, uint32_t lds_addr) {
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+               :
+               : "v"(off), "s"(rsrc), "{m0}"(lds_addr)
+               : "memory");
+}
+
+__device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
+
+// At the start and the end of code that two branches hold in two forms: keeps the
+// compiler from moving what they have in common (operand reads for the most part) in
+// front of or behind the branch, where it would fill the registers.
+template <bool A>
+__device__ __forceinline__ void keep_apart() {
+  if constexpr (A) asm volatile("; a" ::: "memory");
+  else asm volatile("; b" ::: "memory");
+}
+
+// lo and hi of a row, inside [0, S]; empty spans as lo = hi = 0.
+__device__ __forceinline__ void span_of(const int *spans, size_t beta, int S, int row, int &lo,
+                                        int &hi) {
+  lo = 0;
+  hi = row + 1;
+  if (spans) {
+    const u32x2 x = *reinterpret_cast<const u32x2 *>(spans + (beta * S + row) * 2);
+    lo = max((int)x.x, 0);
+    hi = min((int)x.y, S);
+    if (hi <= lo) lo = hi = 0;
+  }
+}
+
+// Which keys some and all rows of a group see: keys outside [any_lo, any_hi)
+// no row, keys of [all_lo, all_hi) every row.
+struct SpanHull {
+  int any_lo, any_hi, all_lo, all_hi;
+  __device__ __forceinline__ bool none(int j0, int n) const {
+    return j0 >= any_hi || j0 + n <= any_lo;
+  }
+  __device__ __forceinline__ bool full(int j0, int n) const {
+    return j0 >= all_lo && j0 + n <= all_hi;
+  }
+};
+
+// A row's own hull; rows past S stand back.
+__device__ __forceinline__ SpanHull hull_of(int lo, int hi, bool row_exists) {
+  if (!row_exists) return SpanHull{0x7fffffff, 0, 0, 0x7fffffff};
+  if (hi <= lo) return SpanHull{0x7fffffff, 0, 0x7fffffff, 0};
+  return SpanHull{lo, hi, lo, hi};
+}
+__device__ __forceinline__ SpanHull join(const SpanHull &x, const SpanHull &y) {
+  return SpanHull{min(x.any_lo, y.any_lo), max(x.any_hi, y.any_hi), max(x.all_lo, y.all_lo),
+                  min(x.all_hi, y.all_hi)};
+}
+// Over the 32 lanes l % 32, in scalar registers (lanes l and l + 32 hold the
+// same row).
+__device__ __forceinline__ SpanHull wave_hull(SpanHull h) {
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) {
+    const SpanHull y{__shfl_xor(h.any_lo, x), __shfl_xor(h.any_hi, x), __shfl_xor(h.all_lo, x),
+                     __shfl_xor(h.all_hi, x)};
+    h = join(h, y);
+  }
+  return SpanHull{__builtin_amdgcn_readfirstlane(h.any_lo),
+                  __builtin_amdgcn_readfirstlane(h.any_hi),
+                  __builtin_amdgcn_readfirstlane(h.all_lo),
+                  __builtin_amdgcn_readfirstlane(h.all_hi)};
+}
+
+// 1 / (1 + e^(2 s / cap)) of a raw product x = s / scale, with c1 = 2 scale
+// log2(e) / cap: tanh(s / cap) = 1 - 2 r, and its derivative is 4 r (1 - r).
+// Off by about 2^-22 from 0 to 1, so cap tanh by 2^-21 cap.
+__device__ __forceinline__ float cap_r(float x, float c1) {
+  return fast_rcp(1.f + fast_exp2(x * c1));
+}
+
+// Words of two bf16: the bits 15 and 31 are set where a half is infinite or NaN.
+__device__ __forceinline__ uint32_t nonfinite_halves(uint32_t w) {
+  return ((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;
+}
+
+}  // namespace basp
