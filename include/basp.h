@@ -29,6 +29,8 @@
  *   basp_kv_write / basp_kv_read   the rank's K and V into the pages of a
  *                  key-value cache (bf16, or 8 bits with a scale), and back
  *   basp_attn_decode   attention of one new token per sequence over the pages
+ *   basp_attn_decode_shared   the same for sequences that share prefixes, with
+ *                  capped and biased scores
  *   basp_attn_span_fwd / basp_attn_span_bwd   attention of packed documents,
  *                  prefixes and padding, with capped and biased scores
  *
@@ -540,6 +542,40 @@ int basp_attn_decode(const void *q, const void *k_pages, const void *v_pages,
                      void *workspace, size_t workspace_bytes, int b, int n_q, int n_k, int d,
                      int page, int n_pages, int max_pages, int max_len, long long q_row,
                      float scale, basp_dtype cache_dtype, void *stream);
+
+/* Bytes of device workspace basp_attn_decode_shared needs.  0 for an invalid or empty
+ * shape. */
+size_t basp_attn_decode_shared_workspace_bytes(int b, int n_q, int n_k, int d, int max_len,
+                                               int n_groups);
+
+/* basp_attn_decode for sequences in groups that share a prefix (a system prompt, the
+ * answers to one question), whose keys are read once for the whole group, and with the
+ * scores of basp_attn_span_fwd:
+ *   s_j = scale * q . k_j,  u_j = cap * tanh(s_j / cap) - slope_h * (lens[s] - 1 - j)
+ *   O = sum_{j < lens[s]} softmax_j(u_j) v_j,  LSE = log sum_{j < lens[s]} exp(u_j)
+ * cap: 0 for none, else up to 1024; slopes: fp32 [n_q], any finite numbers, or NULL.
+ * groups: int32 [n_groups + 1], ascending: group g is the sequences groups[g] ..
+ * groups[g+1] - 1.  prefix_lens: int32 [n_groups]: those of the group's sequences that are
+ * at least so long all list pages with the same first prefix_lens[g] tokens (the very
+ * same pages, but for a last one that the prefix does not fill); the call reads these
+ * tokens through the first such sequence's row of the table.  Shorter sequences of the
+ * group and sequences in no group are read by themselves; results are then those of
+ * basp_attn_decode, but for rounding (the weights of a shared prefix are one bf16).
+ * n_groups 0: groups and prefix_lens are not read.  Arrays that are not as described
+ * give other results, no access outside the buffers.
+ * Arguments, layouts, empty slots, bad pages, NaN and infinities as basp_attn_decode;
+ * lens, groups, prefix_lens and block_table must not change while the call runs.
+ * Deterministic.  workspace: basp_attn_decode_shared_workspace_bytes(), as there.
+ * Errors: as there, plus SHAPE when n_groups < 0, and UNSUPPORTED when cap is neither 0 nor
+ * in (0, 1024] or n_groups >= 2^22. */
+int basp_attn_decode_shared(const void *q, const void *k_pages, const void *v_pages,
+                            const unsigned char *k_scales, const unsigned char *v_scales,
+                            const int *block_table, const int *lens, const int *groups,
+                            const int *prefix_lens, const float *slopes, void *o, float *lse,
+                            void *workspace, size_t workspace_bytes, int b, int n_q, int n_k,
+                            int d, int page, int n_pages, int max_pages, int max_len,
+                            int n_groups, long long q_row, float scale, float cap,
+                            basp_dtype cache_dtype, void *stream);
 
 /* ------------------------------------------------ attention over spans
  *

@@ -37,6 +37,7 @@ EXPORTS = ("basp_status_str", "basp_group_of", "basp_validate", "basp_pack",
            "basp_qk_norm_rope", "basp_qk_norm_rope_bwd",
            "basp_qk_norm_rope_bwd_workspace_bytes", "basp_kv_write", "basp_kv_read",
            "basp_attn_decode", "basp_attn_decode_workspace_bytes",
+           "basp_attn_decode_shared", "basp_attn_decode_shared_workspace_bytes",
            "basp_attn_span_fwd", "basp_attn_span_bwd", "basp_attn_span_bwd_workspace_bytes")
 # Bytes of the static device buffer basp_attn_bwd_noalloc works in.
 NOALLOC_SCRATCH_BYTES = 128 << 20
@@ -98,6 +99,9 @@ def lib() -> ctypes.CDLL:
     L.basp_attn_decode_workspace_bytes.argtypes = [i] * 5
     L.basp_attn_decode_workspace_bytes.restype = sz
     L.basp_attn_decode.argtypes = [vp] * 10 + [sz] + [i] * 8 + [ll, f, i, vp]
+    L.basp_attn_decode_shared_workspace_bytes.argtypes = [i] * 6
+    L.basp_attn_decode_shared_workspace_bytes.restype = sz
+    L.basp_attn_decode_shared.argtypes = ([vp] * 13 + [sz] + [i] * 9 + [ll] + [f] * 2 + [i, vp])
     L.basp_attn_span_fwd.argtypes = [vp] * 7 + [i] * 5 + [ll] * 3 + [f] * 2 + [vp]
     L.basp_attn_span_bwd_workspace_bytes.argtypes = [i] * 5
     L.basp_attn_span_bwd_workspace_bytes.restype = sz
@@ -791,6 +795,66 @@ def attn_decode(q, k_pages, v_pages, block_table, lens, scale: float | None = No
     workspace, ws, ws_n = _space(workspace, need, q, dev)
     _call("basp_attn_decode", L.basp_attn_decode, dev, qp, *ptrs, _on(lens, "lens", _I32, (b,), dev),
           op, lp, ws, ws_n, b, n_q, n_k, d, page, n_pages, max_pages, max_len, q_row, scale, code)
+    return out, lse
+
+
+def attn_decode_shared_workspace_bytes(b, n_q, n_k, d, max_len, n_groups) -> int:
+    return int(lib().basp_attn_decode_shared_workspace_bytes(b, n_q, n_k, d, max_len, n_groups))
+
+
+def attn_decode_shared(q, k_pages, v_pages, block_table, lens, groups=None, prefix_lens=None,
+                       scale: float | None = None, max_len: int | None = None,
+                       cap: float | None = None, slopes=None, k_scales=None, v_scales=None,
+                       out=None, lse=None, workspace=None):
+    """``attn_decode`` for sequences in groups that share a prefix, whose keys are read once for the
+    group, with the scores of ``attn_span_fwd``: capped to cap tanh(s / cap) where there is a
+    ``cap``, less slopes[h] times the key's distance where there are ``slopes`` (fp32 [n_q]).
+    ``groups`` int32 [n_groups + 1], ascending: group g is sequences groups[g] .. groups[g+1] - 1,
+    those of which that reach prefix_lens[g] (int32 [n_groups]) have their first prefix_lens[g]
+    tokens in common, in the same pages.  Both None: nothing is shared."""
+    dev = _device(q, "q", 3)
+    shape = q.shape
+    b, n_q, d = shape
+    ptrs, dims, code = _pages(k_pages, v_pages, k_scales, v_scales, block_table, b, dev)
+    n_k, dp, page, n_pages, max_pages = dims
+    if dp != d:
+        raise ValueError("q and the pages disagree in shape")
+    if (groups is None) != (prefix_lens is None):
+        raise ValueError("groups and prefix_lens go together")
+    n_groups, gp, pp = 0, None, None
+    if prefix_lens is not None:
+        if not isinstance(prefix_lens, _Tensor) or prefix_lens.dim() != 1:
+            raise ValueError("prefix_lens must be [n_groups]")
+        n_groups = prefix_lens.shape[0]
+        gp = _on(groups, "groups", _I32, (n_groups + 1,), dev)
+        pp = _on(prefix_lens, "prefix_lens", _I32, (n_groups,), dev)
+    if scale is None:
+        scale = d ** -0.5
+    if cap is None:
+        cap = 0.0
+    elif not cap > 0:
+        raise ValueError("cap must be positive, or None")
+    max_len = _int(max_pages * page if max_len is None else max_len)
+    qp, q_row = _rows(q, "q", _BF, shape, dev)
+    sp = None if slopes is None else _on(slopes, "slopes", _F32, (n_q,), dev)
+    if out is None:
+        out = _like(q)
+        op = out.data_ptr()
+    else:
+        op = _on(out, "out", _BF, shape, dev)
+    if lse is None:
+        lse = q.new_empty((b, n_q), dtype=_F32)
+        lp = lse.data_ptr()
+    else:
+        lp = _on(lse, "lse", _F32, (b, n_q), dev)
+    L = _lib or lib()
+    n_groups = _int(n_groups)
+    need = 0 if workspace is not None else L.basp_attn_decode_shared_workspace_bytes(
+        b, n_q, n_k, d, max_len, n_groups)
+    workspace, ws, ws_n = _space(workspace, need, q, dev)
+    _call("basp_attn_decode_shared", L.basp_attn_decode_shared, dev, qp, *ptrs,
+          _on(lens, "lens", _I32, (b,), dev), gp, pp, sp, op, lp, ws, ws_n, b, n_q, n_k, d, page,
+          n_pages, max_pages, max_len, n_groups, q_row, scale, cap, code)
     return out, lse
 
 

@@ -15,7 +15,7 @@ from __future__ import annotations
 
 import torch
 
-from . import attn_decode, kv_read, kv_write
+from . import attn_decode, attn_decode_shared, kv_read, kv_write
 
 
 class PagedKV:
@@ -48,3 +48,13 @@ class PagedKV:
         return attn_decode(q, self.k_pages, self.v_pages, block_table, lens, scale=scale,
                            max_len=max_len, k_scales=self.k_scales, v_scales=self.v_scales,
                            out=out, lse=lse, workspace=workspace)
+
+    def attend_shared(self, q, block_table, lens, groups=None, prefix_lens=None,
+                      scale: float | None = None, max_len: int | None = None,
+                      cap: float | None = None, slopes=None, out=None, lse=None, workspace=None):
+        """The same for sequences in groups that share a prefix, and with scores capped and biased by
+        distance (`attn_decode_shared`)."""
+        return attn_decode_shared(q, self.k_pages, self.v_pages, block_table, lens, groups,
+                                  prefix_lens, scale=scale, max_len=max_len, cap=cap,
+                                  slopes=slopes, k_scales=self.k_scales, v_scales=self.v_scales,
+                                  out=out, lse=lse, workspace=workspace)

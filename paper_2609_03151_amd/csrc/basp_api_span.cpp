@@ -1,22 +1,12 @@
 // basp_api_span.cpp -- the extern "C" surface of attention over spans.  As in
 // basp_api.cpp every argument check runs on the host before the first HIP call,
 // and nothing here allocates, frees or synchronises.
-#include <hip/hip_runtime.h>
-#include <math.h>
-#include <stdint.h>
-
 #include <initializer_list>
 
-#include "../../include/basp.h"
+#include "basp_api_checks.hpp"
 #include "basp_span.hpp"
 
 namespace {
-
-bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-int hip_status(hipError_t e) { return e == hipSuccess ? BASP_OK : BASP_ERR_HIP; }
-
-bool head_dim(int d) { return d == 64 || d == 80 || d == 96 || d == 128; }
 
 int check_shape(int b, int S, int n_q, int n_k, int d) {
   if (b < 0 || S < 0 || n_q < 1 || n_k < 1 || d < 1 || n_q % n_k != 0) return BASP_ERR_SHAPE;

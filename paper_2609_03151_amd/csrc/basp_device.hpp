@@ -47,6 +47,15 @@ __device__ __forceinline__ float fast_log2(float x) {
   return __builtin_amdgcn_logf(x);
 }
 
+__device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
+
+// 1 / (1 + e^(2 s / cap)) of a raw product x = s / scale, with c1 = 2 scale
+// log2(e) / cap: tanh(s / cap) = 1 - 2 r, and its derivative is 4 r (1 - r).
+// Off by about 2^-22 from 0 to 1, so cap tanh by 2^-21 cap.
+__device__ __forceinline__ float cap_r(float x, float c1) {
+  return fast_rcp(1.f + fast_exp2(x * c1));
+}
+
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------- buffers

@@ -1,0 +1,769 @@
+// basp_shared.hip -- attention of one new token per sequence over a paged
+// key-value cache, for sequences in groups that share a prefix; scores capped and
+// biased by distance (basp_span.hpp) where the model has them.
+//
+// A group's sequences list the same pages for its prefix's tokens, so those keys are
+// read once for all of them: the rows of the product are then (sequence, query head)
+// pairs, many enough for the matrix cores' 32-row tiles.  Bound by HBM for the keys and
+// values, each read once, up to some 200 rows a kv head, by the matrix cores (and
+// with a cap the vector units) past that.
+//
+//   shared_plan   which sequences share, and where their rows go
+//   shared_main   prefix workgroups: 64 rows of a group and kv head times a split of
+//                 the prefix's keys, as the causal forward's (S^T = K Q^T, O^T = V^T P^T
+//                 on v_mfma_f32_32x32x16_bf16, two row groups times two key parts, K and
+//                 V through LDS, widened to bf16 on the way from 8 bits).
+//                 Own workgroups: every sequence's other keys, dealt out evenly over
+//                 the workgroups as basp_decode.hip does.
+//   shared_join   a row's partial results of both kinds, by their maxima and sums
+#include <math.h>
+
+#include "basp_decode_device.hpp"
+#include "basp_shared.hpp"
+
+namespace basp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kUnit = kWaves * kBlockKeys;  // own keys: a block per wave
+static_assert(kUnit == kDecodeUnit, "the host's cut");
+constexpr float kFixedCap = 64.f;      // up to it P needs no running maximum (basp_span.hpp)
+constexpr float kRescaleSlack = 8.f;   // log2 headroom before the reference max moves
+constexpr int kPlanThreads = 1024;
+
+// The plan, in the workspace.
+struct Plan {
+  int *total;    // chunks there are
+  int *start;    // [b] a sequence's first own key: its group's prefix length, or 0
+  int *row;      // [b] its first prefix row, in chunks of kSharedRows; -1: it shares nothing
+  int *member;   // [b] sequences that share, group by group, from its first sequence on
+  int *units;    // [b + 1] units of the sequences before, times their heads
+  int *group_n, *group_chunk;  // [n_groups]
+  int4 *chunk;   // first member's place, members, prefix length, row of the first
+};
+__device__ __forceinline__ Plan plan_at(const SharedArgs &a, const SharedCut &c) {
+  char *ws = static_cast<char *>(a.d.workspace);
+  Plan p;
+  const int b = a.d.s.b;
+  p.total = reinterpret_cast<int *>(ws + c.ints);
+  p.start = p.total + 1;
+  p.row = p.start + b;
+  p.member = p.row + b;
+  p.units = p.member + b;
+  p.group_n = p.units + b + 1;
+  p.group_chunk = p.group_n + a.n_groups;
+  p.chunk = reinterpret_cast<int4 *>(ws + c.records);
+  return p;
+}
+
+// Units of a sequence's own keys, from the tile of 16 that `start` is in.
+__device__ __forceinline__ int units_of(int len, int start, int max_len) {
+  return len <= start || len > max_len ? 0 : (len - (start & ~15) - 1) / kUnit + 1;
+}
+
+__device__ __forceinline__ int clamp(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// Sum over the workgroup of x of the threads before this one; `total`: of all.
+__device__ __forceinline__ int before(int x, int *sums, int &total) {
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int incl = wave_scan(x);
+  __syncthreads();  // sums of the turn before are read
+  if (lane == 63) sums[wave] = incl;
+  __syncthreads();
+  int at = incl - x;
+  total = 0;
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    if (w < wave) at += sums[w];
+    total += sums[w];
+  }
+  return at;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedArgs a,
+                                                                   const SharedCut c) {
+  const Plan p = plan_at(a, c);
+  const int b = a.d.s.b, rep = a.d.n_q / a.d.s.n_k;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  __shared__ int sums[kPlanThreads / 64], room;
+  if (tid == 0) room = c.chunks;
+  for (int s = tid; s < b; s += kPlanThreads) {
+    p.start[s] = 0;
+    p.row[s] = -1;
+  }
+  __syncthreads();
+  auto group = [&](int g, int &g0, int &g1, int &prefix) {
+    g0 = clamp(a.groups[g], 0, b);
+    g1 = clamp(a.groups[g + 1], g0, b);
+    prefix = a.prefix_lens[g];
+  };
+  // Members of each group: a sequence as long as the prefix, or longer.
+  for (int g = wave; g < a.n_groups; g += kPlanThreads / 64) {
+    int g0, g1, prefix, n = 0;
+    group(g, g0, g1, prefix);
+    if (prefix > 0)
+      for (int s0 = g0; s0 < g1; s0 += 64) {
+        const int s = s0 + lane, len = s < g1 ? a.d.lens[s] : 0;
+        const bool in = len >= prefix && len <= a.d.max_len;
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(in);
+        if (in) p.member[g0 + n + __builtin_popcountll(mask & ((1ull << lane) - 1))] = s;
+        n += __builtin_popcountll(mask);
+      }
+    if (lane == 0) p.group_n[g] = n < 2 ? 0 : n;
+  }
+  __syncthreads();
+  int chunks = 0;
+  for (int g0 = 0; g0 < a.n_groups; g0 += kPlanThreads) {
+    const int g = g0 + tid;
+    const long long rows = g < a.n_groups ? (long long)p.group_n[g] * rep : 0;
+    const int mine = (int)((rows + kSharedRows - 1) / kSharedRows);
+    int total;
+    const int at = chunks + before(mine, sums, total);
+    if (g < a.n_groups) {
+      // groups that overlap may have more rows than there is room for
+      if (at + mine > c.chunks) {
+        p.group_n[g] = 0;
+        atomicMin(&room, at);
+      }
+      p.group_chunk[g] = at;
+    }
+    chunks += total;
+  }
+  __syncthreads();
+  if (tid == 0) *p.total = chunks < room ? chunks : room;
+  for (int g = wave; g < a.n_groups; g += kPlanThreads / 64) {
+    int g0, g1, prefix;
+    group(g, g0, g1, prefix);
+    const int n = p.group_n[g], at = p.group_chunk[g];
+    for (int i = lane; i < n; i += 64) {
+      const int s = p.member[g0 + i];
+      p.start[s] = prefix;
+      p.row[s] = at * kSharedRows + i * rep;
+    }
+    const int mine = (int)(((long long)n * rep + kSharedRows - 1) / kSharedRows);
+    for (int i = lane; i < mine; i += 64) p.chunk[at + i] = int4{g0, n, prefix, i * kSharedRows};
+  }
+  __syncthreads();
+  int units = 0;
+  for (int s0 = 0; s0 < b; s0 += kPlanThreads) {
+    const int s = s0 + tid;
+    const int mine = s < b ? units_of(a.d.lens[s], p.start[s], a.d.max_len) * c.vheads : 0;
+    int total;
+    const int at = units + before(mine, sums, total);
+    if (s < b) p.units[s] = at;
+    units += total;
+  }
+  if (tid == 0) p.units[b] = units;
+}
+
+// ------------------------------------------------------------- prefix pass
+template <int D>
+struct PrefixCfg {
+  static constexpr int R = 2, P = 2;  // row groups, key parts
+  static constexpr int DC = HeadDim<D>::DC;
+  static constexpr int LW = HeadDim<D>::LW;
+  static constexpr int TILE_BYTES = kSharedTile * LW * 2;
+  static constexpr int LDS_BYTES = 2 * 2 * TILE_BYTES;  // two stages of K and V
+  static constexpr int NS = D / 16;
+  static constexpr int NE = DC / 32;
+  static constexpr int PART_BYTES = NE * 4 * 1024 + 512;
+  static_assert(R * PART_BYTES <= LDS_BYTES, "the merge area fits the stages");
+};
+
+// Chunks of 16 bytes of a tile's rows that a thread carries from the pages to LDS.
+template <int D, bool E4M3>
+struct Carry {
+  static constexpr int kPerRow = D * (E4M3 ? 1 : 2) / 16;
+  static constexpr int kChunks = kSharedTile * kPerRow;
+  static constexpr int N = (kChunks + kThreads - 1) / kThreads;
+  u32x4 k[N], v[N];
+  float ks[N], vs[N];
+  int id[N];  // page numbers of the next tile
+  bool bad[N];
+};
+
+template <int D, bool E4M3>
+__device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned char *smem) {
+  using C = PrefixCfg<D>;
+  using T = LdsTile<C::LW>;
+  using W = Carry<D, E4M3>;
+  constexpr int kVRegion = 2 * C::TILE_BYTES;
+  const Plan plan = plan_at(a, c);
+  const CacheShape &cs = a.d.s;
+  const int rep = a.d.n_q / cs.n_k;
+  // Splits fastest, in eights where there are as many: workgroups go round the eight
+  // XCDs, so a split's chunks of rows read its keys through one L2.
+  const int x = blockIdx.x;
+  const int split = scalar(x % c.splits), rest = scalar(x / c.splits);
+  const int chunk = scalar(rest / cs.n_k), kvh = scalar(rest % cs.n_k);
+  if (chunk >= *plan.total) return;  // workgroup-uniform
+  const int4 rec = plan.chunk[chunk];
+  const int first = scalar(rec.x), members = scalar(rec.y), prefix = scalar(rec.z),
+            row0 = scalar(rec.w);
+  const int rows = members * rep - row0;  // of this chunk (and those after it)
+  const int lead = scalar(plan.member[first]);
+  const int *table = a.d.table + (size_t)lead * cs.max_pages;
+  const int tiles = (prefix + kSharedTile - 1) / kSharedTile;
+  const int t0 = (int)((long long)split * tiles / c.splits);
+  const int t1 = (int)((long long)(split + 1) * tiles / c.splits);
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = scalar(tid >> 6);
+  const int l32 = lane & 31, hh = lane >> 5;
+  const int rg = w % C::R, part = w / C::R;
+  const int i = 32 * rg + l32;  // the lane's row
+  const bool live = i < rows;
+  const int seq = live ? plan.member[first + (row0 + i) / rep] : 0;
+  const int head = kvh * rep + (live ? (row0 + i) % rep : 0);
+  bf16x8 qf[C::NS];
+  {
+    const uint16_t *qp = static_cast<const uint16_t *>(a.d.q) + (long long)seq * a.d.q_row +
+                         (size_t)head * D;
+#pragma unroll
+    for (int s = 0; s < C::NS; ++s) {
+      u32x4 v = {0, 0, 0, 0};
+      if (live) v = *reinterpret_cast<const u32x4 *>(qp + 16 * s + 8 * hh);
+      qf[s] = as_bf16x8(v);
+    }
+  }
+  const float at = live ? (float)(a.d.lens[seq] - 1) : 0.f;
+  const float sl = a.slopes && live ? a.slopes[head] * kLog2e : 0.f;
+  const float c2 = a.d.scale * kLog2e;
+  const bool capped = a.cap > 0.f, fixed = capped && a.cap <= kFixedCap;
+  const float c1 = capped ? 2.f * c2 / a.cap : 0.f, cap2 = a.cap * kLog2e;
+  float m_ref = -INFINITY, l_run = 0.f;
+  if (fixed) m_ref = fmaxf(-sl * (at - (float)(prefix - 1)), -sl * at);
+
+  f32x16 oacc[C::NE];
+#pragma unroll
+  for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[n][r] = 0.f;
+
+  W x_;
+  auto load_pages = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < W::N; ++j) {
+      const int ch = tid + kThreads * j, key0 = t * kSharedTile + ch / W::kPerRow;
+      const int key = key0 < prefix ? key0 : prefix - 1, pi = key >> cs.page_log2;
+      x_.id[j] = ch < W::kChunks && t < t1 && pi < cs.max_pages ? table[pi] : -1;
+    }
+  };
+  auto load_rows = [&](int t) {  // of the pages at hand
+#pragma unroll
+    for (int j = 0; j < W::N; ++j) {
+      const int ch = tid + kThreads * j, key0 = t * kSharedTile + ch / W::kPerRow;
+      if (ch >= W::kChunks) continue;
+      const int key = key0 < prefix ? key0 : prefix - 1;  // past the end: the last one again
+      const bool there = x_.id[j] >= 0 && x_.id[j] < cs.n_pages;
+      const size_t row = there ? (((size_t)x_.id[j] * cs.n_k + kvh) << cs.page_log2) +
+                                     (key & ((1 << cs.page_log2) - 1))
+                               : 0;
+      const size_t off = row * (D * (E4M3 ? 1 : 2)) + ch % W::kPerRow * 16;
+      x_.k[j] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.d.k_pages) + off);
+      x_.v[j] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.d.v_pages) + off);
+      if constexpr (E4M3) {
+        x_.ks[j] = __builtin_bit_cast(float, (uint32_t)a.d.k_scales[row] << 23);
+        x_.vs[j] = __builtin_bit_cast(float, (uint32_t)a.d.v_scales[row] << 23);
+      }
+      x_.bad[j] = !there;
+    }
+  };
+  auto widen8 = [&](uint32_t lo, uint32_t hi, float scale) {
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
+  };
+  auto put = [&](int stage) {  // into LDS
+    unsigned char *Ks = smem + stage * C::TILE_BYTES;
+#pragma unroll
+    for (int j = 0; j < W::N; ++j) {
+      const int ch = tid + kThreads * j, r = ch / W::kPerRow, cc = ch % W::kPerRow;
+      if (ch >= W::kChunks) continue;
+      constexpr uint32_t kNan = 0x7FFF7FFFu;
+      if constexpr (E4M3) {
+        u32x4 k0 = widen8(x_.k[j].x, x_.k[j].y, x_.ks[j]), k1 = widen8(x_.k[j].z, x_.k[j].w, x_.ks[j]);
+        if (x_.bad[j]) k0 = u32x4{kNan, kNan, kNan, kNan};
+        *reinterpret_cast<u32x4 *>(Ks + T::off(r, 2 * cc)) = k0;
+        *reinterpret_cast<u32x4 *>(Ks + T::off(r, 2 * cc + 1)) = k1;
+        *reinterpret_cast<u32x4 *>(Ks + kVRegion + T::off(r, 2 * cc)) =
+            widen8(x_.v[j].x, x_.v[j].y, x_.vs[j]);
+        *reinterpret_cast<u32x4 *>(Ks + kVRegion + T::off(r, 2 * cc + 1)) =
+            widen8(x_.v[j].z, x_.v[j].w, x_.vs[j]);
+      } else {
+        u32x4 k0 = x_.k[j];
+        if (x_.bad[j]) k0 = u32x4{kNan, kNan, kNan, kNan};
+        *reinterpret_cast<u32x4 *>(Ks + T::off(r, cc)) = k0;
+        *reinterpret_cast<u32x4 *>(Ks + kVRegion + T::off(r, cc)) = x_.v[j];
+      }
+    }
+  };
+
+  const int part_off = part * 32 * T::ROW_BYTES;
+  int k_off[C::NS], v_off[C::NE][2];
+#pragma unroll
+  for (int s = 0; s < C::NS; ++s) k_off[s] = T::off(l32, 2 * s + hh) + part_off;
+#pragma unroll
+  for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+      v_off[n][y] = kVRegion + part_off +
+                    tr_piece_off<C::LW>(4 * hh + 8 * y, 32 * n + 16 * ((lane >> 4) & 1), lane);
+  auto tile = [&](int t, int stage) __attribute__((always_inline)) {
+    const unsigned char *Ks = smem + stage * C::TILE_BYTES;
+    f32x16 sc;
+#pragma unroll
+    for (int s = 0; s < C::NS; ++s)
+      sc = mfma32x32x16(*reinterpret_cast<const bf16x8 *>(Ks + k_off[s]), qf[s],
+                        s == 0 ? f32x16{} : sc);
+    // sc[r] = (q . k) of key jl + 8(r/4) + r%4 for this lane's row
+    const int jl = t * kSharedTile + 32 * part + 4 * hh;
+    const float away = at - (float)jl;
+    if (capped) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = fmaf(cap_r(sc[r], c1), -2.f * cap2, cap2);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] *= c2;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = fmaf(-sl, away - (float)(8 * (r >> 2) + (r & 3)), sc[r]);
+    if (jl - 4 * hh + 32 > prefix) {  // wave-uniform: the last tile
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (jl + 8 * (r >> 2) + (r & 3) >= prefix) sc[r] = -INFINITY;
+    }
+    if (!fixed) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+      mx = pair_max(mx);
+      const bool grow = mx > m_ref + kRescaleSlack;
+      if (__builtin_amdgcn_ballot_w64(grow)) {  // wave-uniform, rare after the first tiles
+        asm volatile("" ::: "memory");
+        const float alpha = grow ? fast_exp2(m_ref - mx) : 1.f;
+        m_ref = grow ? mx : m_ref;
+        l_run *= alpha;
+#pragma unroll
+        for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[n][r] *= alpha;
+      }
+    }
+    const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+    float psum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      sc[r] = fast_exp2(sc[r] - m_use);
+      psum += sc[r];
+    }
+    l_run += psum;
+    bf16x8 pf[2];
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      const int b8 = 8 * s2;
+      pf[s2] = as_bf16x8(u32x4{pack_bf16x2(sc[b8 + 0], sc[b8 + 1]), pack_bf16x2(sc[b8 + 2], sc[b8 + 3]),
+                               pack_bf16x2(sc[b8 + 4], sc[b8 + 5]),
+                               pack_bf16x2(sc[b8 + 6], sc[b8 + 7])});
+    }
+#pragma unroll
+    for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const int ro = s2 * 16 * T::ROW_BYTES;
+        oacc[n] = mfma32x32x16(tr_operand(Ks, v_off[n][0] + ro, v_off[n][1] + ro), pf[s2], oacc[n]);
+      }
+  };
+  // One tile of rows and the next one's page numbers in flight over a tile's
+  // products; two stages, so that one barrier a tile is enough.
+  load_pages(t0);
+  if (t0 < t1) load_rows(t0);
+  load_pages(t0 + 1);
+  for (int t = t0; t < t1; ++t) {
+    put((t - t0) & 1);
+    if (t + 1 < t1) {
+      load_rows(t + 1);
+      load_pages(t + 2);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier_no_fence();
+    tile(t, (t - t0) & 1);
+  }
+
+  // The two parts of a row group, and out.
+  float l_tot = pair_sum(l_run);
+  __syncthreads();
+  unsigned char *area = smem + rg * C::PART_BYTES;
+  constexpr int kScalars = C::NE * 4 * 1024;
+  if (part == 1) {
+#pragma unroll
+    for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4 *>(area + (n * 4 + g) * 1024 + 16 * lane) =
+            f32x4{oacc[n][4 * g], oacc[n][4 * g + 1], oacc[n][4 * g + 2], oacc[n][4 * g + 3]};
+    *reinterpret_cast<float *>(area + kScalars + 4 * lane) = m_ref;
+    *reinterpret_cast<float *>(area + kScalars + 256 + 4 * lane) = l_tot;
+  }
+  __syncthreads();
+  if (part == 1 || !live) return;
+  const float m1 = *reinterpret_cast<const float *>(area + kScalars + 4 * lane);
+  const float l1 = *reinterpret_cast<const float *>(area + kScalars + 256 + 4 * lane);
+  const float m = fmaxf(m_ref, m1), ref = m == -INFINITY ? 0.f : m;
+  const float w0 = fast_exp2(m_ref - ref), w1 = fast_exp2(m1 - ref);
+  char *ws = static_cast<char *>(a.d.workspace);
+  const size_t slot = ((size_t)(chunk * cs.n_k + kvh) * c.splits + split) * kSharedRows + i;
+  float *po = reinterpret_cast<float *>(ws + c.part_o) + slot * D;
+#pragma unroll
+  for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (32 * n + 8 * g >= D) continue;  // padding columns
+      const f32x4 z = *reinterpret_cast<const f32x4 *>(area + (n * 4 + g) * 1024 + 16 * lane);
+      f32x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = oacc[n][4 * g + e] * w0 + z[e] * w1;
+      *reinterpret_cast<f32x4 *>(po + 32 * n + 8 * g + 4 * hh) = y;
+    }
+  if (hh == 0)
+    reinterpret_cast<f32x2 *>(ws + c.part_ml)[slot] = f32x2{m, l_tot * w0 + l1 * w1};
+}
+
+// ------------------------------------------------------------ the own keys
+// Workgroup g of `own.groups`: its run of units, as in basp_decode.hip.  A head that is whole
+// in one run is final where its sequence shares nothing, else it goes to its rows'
+// places; one that several runs share leaves partial results in the slot of either's
+// first (0) or last (1) head.  open[sequence * vheads + vhead] says which: `count` 0: final,
+// or nothing; -1: in the rows' places; else the partial results, the first in slot
+// first % 2 of workgroup first / 2, the others in slot 0 of the next ones.
+template <int D, bool E4M3, int RG>
+__device__ void own_unit(const SharedArgs &a, const SharedCut &c, int g, unsigned char *smem,
+                         int *found) {
+  using B = Block<D, E4M3>;
+  constexpr int kRows = 16 * RG;
+  const DecodeArgs &d = a.d;
+  const Plan plan = plan_at(a, c);
+  const int rep = scalar(d.n_q / d.s.n_k), row_groups = c.own.row_groups, R = c.vheads;
+  const int b = d.s.b, G = c.own.groups;
+  const int wave = scalar(threadIdx.x / 64);
+  const int lane = threadIdx.x % 64, m = lane % 16, cq = lane / 16;
+  float(*so)[kRows][D + 4] = reinterpret_cast<float(*)[kRows][D + 4]>(smem);
+  float(*sm)[kRows] = reinterpret_cast<float(*)[kRows]>(so + kWaves);
+  float(*sl)[kRows] = sm + kWaves;
+  char *ws = static_cast<char *>(d.workspace);
+  DecodeOpen *opens = reinterpret_cast<DecodeOpen *>(ws + c.open);
+  f32x2 *own_ml = reinterpret_cast<f32x2 *>(ws + c.own_ml);
+  float *own_o = reinterpret_cast<float *>(ws + c.own_o);
+  f32x2 *row_ml = reinterpret_cast<f32x2 *>(ws + c.row_ml);
+  float *row_o = reinterpret_cast<float *>(ws + c.row_o);
+
+  // Sequences without own keys, or with more than the call allows, are shared out.
+  for (int s = g; s < b; s += G) {
+    const int len = scalar_load(d.lens, s), start = plan.start[s];
+    if (units_of(len, start, d.max_len) > 0) continue;
+    for (int i = threadIdx.x; i < R; i += kThreads) opens[(size_t)s * R + i].count = 0;
+    if (len == start && start > 0) continue;  // all of it is the prefix
+    uint16_t *o = static_cast<uint16_t *>(d.o) + (size_t)s * d.n_q * D;
+    for (int i = threadIdx.x; i < d.n_q * D; i += kThreads) o[i] = len <= 0 ? 0 : 0x7FFF;
+    if (d.lse)
+      for (int i = threadIdx.x; i < d.n_q; i += kThreads)
+        d.lse[(size_t)s * d.n_q + i] = len <= 0 ? -INFINITY : __builtin_nanf("");
+  }
+
+  const int total = plan.units[b];
+  const int quota = scalar((total + G - 1) / G);
+  const long long first = (long long)g * quota;
+  if (first >= total) return;
+  const int begin = (int)first, end = total - begin < quota ? total : begin + quota;
+  if (b <= 8 * kThreads) {
+    for (int s = threadIdx.x; s < b; s += kThreads)
+      if (begin >= plan.units[s] && begin < plan.units[s + 1]) *found = s;
+  } else if (threadIdx.x == 0) {
+    int lo = 0, hi = b;  // units[lo] <= begin < units[hi]
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (plan.units[mid] <= begin) lo = mid;
+      else hi = mid;
+    }
+    *found = lo;
+  }
+  __syncthreads();
+  int seq = scalar(*found);
+  int len = 0, start = 0, n = 0;
+  auto enter = [&]() {
+    len = scalar(d.lens[seq]);
+    start = scalar(plan.start[seq]);
+    n = units_of(len, start, d.max_len);
+  };
+  enter();
+  if (n == 0) return;  // not reached while lens stays as it is
+  const int at0 = begin - scalar(plan.units[seq]);
+  int head = scalar(at0 / n), u = scalar(at0 % n);
+
+  Pages pg;
+  pg.k = static_cast<const char *>(d.k_pages);
+  pg.v = static_cast<const char *>(d.v_pages);
+  pg.ks = d.k_scales;
+  pg.vs = d.v_scales;
+  pg.page_log2 = d.s.page_log2;
+  pg.n_pages = d.s.n_pages;
+  pg.max_pages = d.s.max_pages;
+  pg.n_k = d.s.n_k;
+  const float scale2 = d.scale * kLog2e;
+  KeyRule rule;
+  rule.capped = a.cap > 0.f;
+  rule.c1 = rule.capped ? 2.f * scale2 / a.cap : 0.f;
+  rule.cap2 = a.cap * kLog2e;
+
+  for (int pos = begin; pos < end;) {
+    const int take = n - u < end - pos ? n - u : end - pos;  // units of this head
+    const int base = start & ~15;
+    const int lo = base + u * kUnit;
+    const int hi = lo + take * kUnit < len ? lo + take * kUnit : len;
+    const int kvh = scalar(head / row_groups), grp = scalar(head % row_groups);
+    const int h0 = kvh * rep + grp * kRows;  // first query head
+    const int heads = rep - grp * kRows < kRows ? rep - grp * kRows : kRows;
+    pg.table = d.table + (size_t)seq * d.s.max_pages;
+    pg.kvh = kvh;
+    rule.at = (float)(len - 1);
+    rule.lo = start;
+
+    int t = lo + wave * kBlockKeys;
+    Block<D, E4M3> x;
+    int ids[kTiles];
+    load_ids(pg, t, hi, ids);
+    State<B> st[RG];
+    float slope[RG];
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const int h = 16 * rg + m;
+      const uint16_t *qp = static_cast<const uint16_t *>(d.q) + (long long)seq * d.q_row +
+                           (size_t)(h0 + h) * D;
+#pragma unroll
+      for (int s = 0; s < B::kSteps; ++s) {
+        const int e = E4M3 ? 64 * (s / 2) + 16 * cq + 8 * (s % 2) : 32 * s + 8 * cq;
+        u32x4 w = {0, 0, 0, 0};
+        if (h < heads && e < D) w = *reinterpret_cast<const u32x4 *>(qp + e);
+        st[rg].q[s] = as_bf16x8(w);
+      }
+      slope[rg] = a.slopes && h < heads ? a.slopes[h0 + h] * kLog2e : 0.f;
+      st[rg].m = -INFINITY;
+      st[rg].l = 0.f;
+#pragma unroll
+      for (int i = 0; i < B::kCols; ++i) st[rg].o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    while (t < hi) {
+      load_block<D, E4M3>(x, pg, t, hi, ids);
+      load_ids(pg, t + kUnit, hi, ids);
+      take_block<D, E4M3, RG, true>(x, st, scale2, hi - t, rule, slope, t);
+      t += kUnit;
+    }
+
+    // The four waves.
+    __syncthreads();  // the last head's
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const float l = column_sum(st[rg].l);
+      if (cq == 0) sm[wave][16 * rg + m] = st[rg].m, sl[wave][16 * rg + m] = l;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const int h = 16 * rg + m;
+      float M = sm[0][h];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm[w][h]);
+      const float f = fast_exp2(st[rg].m - (M == -INFINITY ? 0.f : M));
+      const f32x4 *acc = st[rg].o;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (B::kCols * (4 * cq + r) < D) {
+#pragma unroll
+          for (int i = 0; i < B::kCols; i += 4)
+            *reinterpret_cast<f32x4 *>(&so[wave][h][B::kCols * (4 * cq + r) + i]) =
+                f32x4{acc[i][r] * f, acc[i + 1][r] * f, acc[i + 2][r] * f, acc[i + 3][r] * f};
+        }
+    }
+    __syncthreads();
+    const size_t row0 = (size_t)seq * d.n_q + h0;
+    const bool whole = take == n, shares = start > 0;
+    const int slot = pos != begin;
+    if (u == 0 && threadIdx.x == 0)
+      opens[(size_t)seq * R + head] =
+          DecodeOpen{0, heads, !whole ? (pos + n - 1) / quota - g + 1 : shares ? -1 : 0,
+                     2 * g + slot};
+    for (int i = threadIdx.x; i < heads * (D / 4); i += kThreads) {
+      const int h = i / (D / 4), e = i % (D / 4) * 4;
+      float mx = sm[0][h], L = 0.f;
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) mx = fmaxf(mx, sm[w][h]);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+      f32x4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        L += fast_exp2(sm[w][h] - ref) * sl[w][h];
+        O += *reinterpret_cast<const f32x4 *>(&so[w][h][e]);
+      }
+      if (whole && !shares) {
+        O *= 1.f / L;
+        *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(d.o) + (row0 + h) * D + e) =
+            u32x2{pack_bf16x2(O.x, O.y), pack_bf16x2(O.z, O.w)};
+        if (e == 0 && d.lse) d.lse[row0 + h] = (mx + fast_log2(L)) * kLn2;
+      } else {
+        const size_t at = whole ? row0 + h : ((size_t)g * 2 + slot) * kRows + h;
+        *reinterpret_cast<f32x4 *>((whole ? row_o : own_o) + at * D + e) = O;
+        if (e == 0) (whole ? row_ml : own_ml)[at] = f32x2{mx, L};
+      }
+    }
+    pos += take;
+    if (pos < end) {  // the next head, of the next sequence that has own keys
+      u = 0;
+      if (++head == R) {
+        head = 0;
+        n = 0;
+        while (n == 0 && ++seq < b) enter();
+        if (n == 0) break;  // not reached while lens stays as it is
+      }
+    }
+  }
+}
+
+template <int D, bool E4M3, int RG>
+__global__ __launch_bounds__(kThreads, 2) void shared_main_kernel(const SharedArgs a,
+                                                                  const SharedCut c) {
+  constexpr int kOwn = kWaves * 16 * RG * ((D + 4) + 2) * 4;
+  constexpr int kLds = kOwn > PrefixCfg<D>::LDS_BYTES ? kOwn : PrefixCfg<D>::LDS_BYTES;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kLds];
+  __shared__ int found;
+  if ((int)blockIdx.x < c.prefix_blocks)  // workgroup-uniform
+    prefix_unit<D, E4M3>(a, c, smem);
+  else
+    own_unit<D, E4M3, RG>(a, c, (int)blockIdx.x - c.prefix_blocks, smem, &found);
+}
+
+// ------------------------------------------------------------------ the join
+// A workgroup per row that has partial results: these in turn over the four waves,
+// two elements of d a lane, each wave with a running maximum.
+template <int D>
+__global__ __launch_bounds__(kThreads) void shared_join_kernel(const SharedArgs a,
+                                                               const SharedCut c) {
+  const DecodeArgs &d = a.d;
+  const Plan plan = plan_at(a, c);
+  const int row = blockIdx.x, seq = scalar(row / d.n_q), h = scalar(row % d.n_q);
+  const int rep = scalar(d.n_q / d.s.n_k), kvh = scalar(h / rep), hr = scalar(h % rep);
+  char *ws = static_cast<char *>(d.workspace);
+  const DecodeOpen open = reinterpret_cast<const DecodeOpen *>(
+      ws + c.open)[(size_t)seq * c.vheads + kvh * c.own.row_groups + hr / c.own.rows];
+  const int prow = plan.row[seq];
+  const int own = open.count < 0 ? 1 : open.count, shared = prow >= 0 ? c.splits : 0;
+  const int n = own + shared;
+  if (n == 0) return;
+  const int at_p = prow + hr;
+  const size_t base = ((size_t)(at_p / kSharedRows * d.s.n_k + kvh) * c.splits) * kSharedRows +
+                      at_p % kSharedRows;
+  const f32x2 *part_ml = reinterpret_cast<const f32x2 *>(ws + c.part_ml);
+  const float *part_o = reinterpret_cast<const float *>(ws + c.part_o);
+  auto find = [&](int i, const f32x2 *&ml, const float *&o) {
+    if (i < shared) {
+      const size_t x = base + (size_t)i * kSharedRows;
+      ml = part_ml + x, o = part_o + x * D;
+    } else if (open.count < 0) {
+      ml = reinterpret_cast<const f32x2 *>(ws + c.row_ml) + row;
+      o = reinterpret_cast<const float *>(ws + c.row_o) + (size_t)row * D;
+    } else {
+      const int j = i - shared;
+      const size_t x = (size_t)(j ? (open.first | 1) - 1 + 2 * j : open.first) * c.own.rows +
+                       hr % c.own.rows;
+      ml = reinterpret_cast<const f32x2 *>(ws + c.own_ml) + x;
+      o = reinterpret_cast<const float *>(ws + c.own_o) + x * D;
+    }
+  };
+  const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int col = 2 * lane < D ? 2 * lane : 0;
+  float M = -INFINITY, l = 0.f;
+  f32x2 O = {0.f, 0.f};
+  constexpr int kAtOnce = 8;
+  for (int i0 = wave; i0 < n; i0 += kAtOnce * kWaves) {
+    f32x2 x[kAtOnce], o[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int i = i0 + u * kWaves < n ? i0 + u * kWaves : i0;  // again the first: dropped below
+      const f32x2 *ml;
+      const float *po;
+      find(i, ml, po);
+      x[u] = *ml;
+      o[u] = *reinterpret_cast<const f32x2 *>(po + col);
+    }
+    float mx = M;
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) mx = fmaxf(mx, x[u].x);
+    const float ref = mx == -INFINITY ? 0.f : mx, f = fast_exp2(M - ref);
+    M = mx;
+    l *= f;
+    O *= f;
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+      if (i0 + u * kWaves < n) {
+        const float w = fast_exp2(x[u].x - ref);
+        l += w * x[u].y;
+        O += w * o[u];
+      }
+  }
+  __shared__ float so[kWaves][D + 2], sm[kWaves], sl[kWaves];
+  if (2 * lane < D) so[wave][2 * lane] = O.x, so[wave][2 * lane + 1] = O.y;
+  if (lane == 0) sm[wave] = M, sl[wave] = l;
+  __syncthreads();
+  if (wave != 0) return;
+  M = sm[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm[w]);
+  const float ref = M == -INFINITY ? 0.f : M;
+  l = 0.f;
+  O = f32x2{0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float f = fast_exp2(sm[w] - ref);
+    l += f * sl[w];
+    O += f * f32x2{so[w][col], so[w][col + 1]};
+  }
+  const float inv = 1.f / l;
+  if (2 * lane < D)
+    static_cast<uint32_t *>(d.o)[((size_t)row * D + 2 * lane) / 2] =
+        pack_bf16x2(O.x * inv, O.y * inv);
+  if (lane == 0 && d.lse) d.lse[row] = (M + fast_log2(l)) * kLn2;
+}
+
+template <int D, bool E4M3>
+void main_typed(const SharedArgs &a, const SharedCut &c, hipStream_t stream) {
+  const dim3 grid(c.prefix_blocks + c.own.groups);
+  if (c.own.rows == 16)
+    hipLaunchKernelGGL((shared_main_kernel<D, E4M3, 1>), grid, dim3(kThreads), 0, stream, a, c);
+  else
+    hipLaunchKernelGGL((shared_main_kernel<D, E4M3, 2>), grid, dim3(kThreads), 0, stream, a, c);
+}
+
+template <int D>
+hipError_t launch_dim(const SharedArgs &a, const SharedCut &c, hipStream_t stream) {
+  hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, c);
+  if (a.d.s.e4m3) main_typed<D, true>(a, c, stream);
+  else main_typed<D, false>(a, c, stream);
+  hipLaunchKernelGGL((shared_join_kernel<D>), dim3((unsigned)(a.d.s.b * a.d.n_q)), dim3(kThreads),
+                     0, stream, a, c);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_decode_shared(const SharedArgs &a, hipStream_t stream) {
+  const SharedCut c =
+      shared_cut(a.d.s.b, a.d.n_q, a.d.s.n_k, a.d.s.d, a.d.max_len, a.n_groups);
+  switch (a.d.s.d) {
+    case 64: return launch_dim<64>(a, c, stream);
+    case 80: return launch_dim<80>(a, c, stream);
+    case 96: return launch_dim<96>(a, c, stream);
+    default: return launch_dim<128>(a, c, stream);
+  }
+}
+
+}  // namespace basp

@@ -18,8 +18,6 @@ __device__ __forceinline__ void copy16_to_lds(u32x4 rsrc, uint32_t off, uint32_t
                : "memory");
 }
 
-__device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
-
 // At the start and the end of code that two branches hold in two forms: keeps the
 // compiler from moving what they have in common (operand reads for the most part) in
 // front of or behind the branch, where it would fill the registers.
@@ -77,13 +75,6 @@ __device__ __forceinline__ SpanHull wave_hull(SpanHull h) {
                   __builtin_amdgcn_readfirstlane(h.any_hi),
                   __builtin_amdgcn_readfirstlane(h.all_lo),
                   __builtin_amdgcn_readfirstlane(h.all_hi)};
-}
-
-// 1 / (1 + e^(2 s / cap)) of a raw product x = s / scale, with c1 = 2 scale
-// log2(e) / cap: tanh(s / cap) = 1 - 2 r, and its derivative is 4 r (1 - r).
-// Off by about 2^-22 from 0 to 1, so cap tanh by 2^-21 cap.
-__device__ __forceinline__ float cap_r(float x, float c1) {
-  return fast_rcp(1.f + fast_exp2(x * c1));
 }
 
 // Words of two bf16: the bits 15 and 31 are set where a half is infinite or NaN.
