@@ -97,7 +97,7 @@ __device__ __forceinline__ bf16x8 finite_operand(bf16x8 x, u32x4 seen, f32x16 &a
 }
 
 // Sixteen weights of the accumulator as two operands.
-__device__ __forceinline__ void pack16(const float *x, bf16x8 (&out)[2]) {
+__device__ __forceinline__ void pack16(const f32x16 &x, bf16x8 (&out)[2]) {
 #pragma unroll
   for (int s2 = 0; s2 < 2; ++s2) {
     const int b8 = 8 * s2;
@@ -411,11 +411,13 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
   const float c = a.s.scale * kSpanLog2e;
   const float c1 = CAP ? 2.f * c / a.s.cap : 0.f, cap2 = CAP ? a.s.cap * kSpanLog2e : 0.f;
 
-  auto step = [&](int stg, int row0, auto edge_tag, auto careful_tag)
-                  __attribute__((always_inline)) {
-    constexpr bool EDGE = decltype(edge_tag)::value, CAREFUL = decltype(careful_tag)::value;
+  const float rc = 1.f / c;
+  // One step's half for this wave.  What a mask and a bias of both signs take is put
+  // into the scores (with a cap: into what their exponents start from) behind one
+  // branch, so that everything else, and above all the accumulators, exists once.
+  auto step = [&](int stg, int row0, bool edge, auto careful_tag) __attribute__((always_inline)) {
+    constexpr bool CAREFUL = decltype(careful_tag)::value;
     const unsigned char *Qs = smem + stg * C::TILE_BYTES, *dOs = Qs + kDoRegion;
-    keep_apart<EDGE>();
     f32x16 sacc, pacc;
     {
       const f32x16 negd = aux_rows(stg, 1);
@@ -434,41 +436,49 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
       }
     }
     bf16x8 bp[2], bds[2];
-    u32x4 seen[2] = {};
+    constexpr uint32_t kOnes = 0x3F803F80u;
+    u32x4 seen[2] = {{kOnes, kOnes, kOnes, kOnes}, {kOnes, kOnes, kOnes, kOnes}};
     {
       f32x16 neglse;
       if constexpr (CAP) neglse = aux_rows(stg, 0);
       // row0: first row of the wave's half
-      const float base = BIAS ? sl * (float)(key - (row0 - 32 * h)) : 0.f;
-      float ahead = (float)(row0 + 4 * hh - key);
-      asm volatile("" : "+v"(ahead));
-      const int span_lane = kAuxRegion + 1024 + 8 * (32 * h + 4 * hh);
-      float p[16], ds[16];
+      float base = BIAS ? sl * (float)(key - (row0 - 32 * h)) : 0.f;
+      if (edge) {  // wave-uniform
+        asm volatile("" ::: "memory");
+        const float ahead = (float)(row0 + 4 * hh - key), in64 = (float)(32 * h + 4 * hh);
+        const unsigned char *spans = smem + stg * C::AUX_BYTES + kAuxRegion + 1024 + 8 * 32 * h +
+                                     8 * 4 * hh;
+        base = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int io = 8 * (r >> 2) + (r & 3);
+          const u32x2 span = *reinterpret_cast<const u32x2 *>(spans + 8 * io);
+          const bool vis = key - span.x < span.y - span.x;
+          const float bias = BIAS ? (in64 + (float)io) - fabsf(ahead + (float)io) : 0.f;
+          if constexpr (CAP) {
+            neglse[r] = vis ? fmaf(sl, bias, neglse[r]) : -INFINITY;
+            sacc[r] = vis ? sacc[r] : 0.f;
+          } else {
+            sacc[r] = vis ? fmaf(sl * rc, bias, sacc[r]) : -INFINITY;
+          }
+          pacc[r] = vis ? pacc[r] : 0.f;
+          if (CAREFUL && !vis) seen[r / 8][r % 8 / 2] &= r % 2 ? 0xFFFFu : 0xFFFF0000u;
+        }
+        asm volatile("" ::: "memory");
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int io = 8 * (r >> 2) + (r & 3);
-        float add = base;
-        if constexpr (BIAS && EDGE)
-          add = sl * ((float)(32 * h + 4 * hh + io) - fabsf(ahead + (float)io));
-        float wt = 1.f;
         if constexpr (CAP) {
           const float rr = cap_r(sacc[r], c1);
-          wt = fmaf(-rr, rr, rr);
-          p[r] = fast_exp2(fmaf(rr, -2.f * cap2, cap2 + add + neglse[r]));
-          ds[r] = p[r] * pacc[r] * wt;
+          sacc[r] = fast_exp2(fmaf(rr, -2.f * cap2, neglse[r] + (cap2 + base)));
+          pacc[r] = sacc[r] * pacc[r] * fmaf(-rr, rr, rr);
         } else {
-          p[r] = fast_exp2(fmaf(sacc[r], c, add));
-          ds[r] = p[r] * pacc[r];
-        }
-        if constexpr (EDGE) {
-          const u32x2 span = *reinterpret_cast<const u32x2 *>(
-              smem + span_lane + stg * C::AUX_BYTES + 8 * io);
-          if (key - span.x >= span.y - span.x) p[r] = 0.f, ds[r] = 0.f;
-          else if (CAREFUL) seen[r / 8][r % 8 / 2] |= r % 2 ? 0x3F800000u : 0x3F80u;
+          sacc[r] = fast_exp2(fmaf(sacc[r], c, base));
+          pacc[r] = sacc[r] * pacc[r];
         }
       }
-      pack16(p, bp);
-      pack16(ds, bds);
+      pack16(sacc, bp);
+      pack16(pacc, bds);
     }
     wave_priority<1>();
 #pragma unroll
@@ -486,12 +496,10 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
     if constexpr (!CAREFUL) sched_reads_ahead<4 * C::NE, 2, 4>();
     __builtin_amdgcn_sched_barrier(0);
     wave_priority<0>();
-    keep_apart<EDGE>();
   };
   using No = std::false_type;
   using Yes = std::true_type;
   auto sweep = [&](auto careful_tag) __attribute__((always_inline)) {
-    constexpr bool CAREFUL = decltype(careful_tag)::value;
     const int heads = rep1 - rep0;
     const int n = count * heads;
     int ld_i = 0, ld_h = rep0;  // the next step to copy
@@ -514,13 +522,7 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
       load_next(st + 1);
       const int row0 = r_lo + (int)(e & 0xFFFFu) * kQM + 32 * h;
       const uint32_t kind = (e >> (16 + 2 * (4 * h + kw))) & 3u;
-      if (CAREFUL) {
-        if (kind != 0) step(STG, row0, Yes{}, Yes{});
-      } else if (kind == 2) {
-        step(STG, row0, No{}, No{});
-      } else if (kind == 1) {
-        step(STG, row0, Yes{}, No{});
-      }
+      if (kind != 0) step(STG, row0, kind == 1, careful_tag);
       if (++i == count) i = 0, ++hr;
     };
     // Two stages: step st's copies landed, then the barrier, after which the
@@ -752,12 +754,12 @@ __device__ __forceinline__ void dq_tile(const BwdArgs &a, int L, unsigned char *
       for (int r = 0; r < 16; ++r) qacc[n][r] = 0.f;
   };
   clear();
-  auto tile = [&](int u, int st, auto edge_tag, auto careful_tag)  // st: u % kSt
+  const float rc = 1.f / c;
+  auto tile = [&](int u, int st, bool edge, auto careful_tag)  // st: u % kSt
                   __attribute__((always_inline)) {
-    constexpr bool EDGE = decltype(edge_tag)::value, CAREFUL = decltype(careful_tag)::value;
+    constexpr bool CAREFUL = decltype(careful_tag)::value;
     const int j0 = (t0 + u) * C::BN + 32 * C::KM * part;
     const unsigned char *Ks = smem + st * C::TILE_BYTES;
-    keep_apart<EDGE>();
 #pragma unroll
     for (int m = 0; m < C::KM; ++m) {
       f32x16 sacc, pacc;
@@ -770,35 +772,53 @@ __device__ __forceinline__ void dq_tile(const BwdArgs &a, int L, unsigned char *
       }
       sched_reads_ahead<2 * C::NS, 1, 4>();
       const int jl = j0 + 32 * m + 4 * hh;
-      float ahead = (float)(row - jl);
-      int past = jl - lo;
-      // (else sums of these and the 16 offsets are kept over the whole loop)
-      asm volatile("" : "+v"(ahead), "+v"(past));
-      const float slp = j0 + 32 * m > wrow0 ? -sl : sl;
-      u32x4 seen[2] = {};
-      float ds[16];
+      const float ahead = (float)(row - jl);
+      // not an edge: all keys on one side of the rows
+      float slp = j0 + 32 * m > wrow0 ? -sl : sl;
+      float base = BIAS ? fmaf(-slp, ahead, nlse) : nlse;
+      constexpr uint32_t kOnes = 0x3F803F80u;
+      u32x4 seen[2] = {{kOnes, kOnes, kOnes, kOnes}, {kOnes, kOnes, kOnes, kOnes}};
+      f32x16 add;  // with a cap
+      if constexpr (CAP) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          add[r] = (BIAS ? fmaf(slp, (float)(8 * (r >> 2) + (r & 3)), base) : base) + cap2;
+      }
+      if (edge) {  // wave-uniform; as in the key pass
+        asm volatile("" ::: "memory");
+        const int past = jl - lo;
+        slp = 0.f;
+        base = nlse;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int jo = 8 * (r >> 2) + (r & 3);
+          const bool vis = (uint32_t)(past + jo) < (uint32_t)(hi - lo);
+          const float dist = BIAS ? fabsf(ahead - (float)jo) : 0.f;
+          if constexpr (CAP) {
+            add[r] = vis ? fmaf(-sl, dist, nlse + cap2) : -INFINITY;
+            sacc[r] = vis ? sacc[r] : 0.f;
+          } else {
+            sacc[r] = vis ? fmaf(-sl * rc, dist, sacc[r]) : -INFINITY;
+          }
+          pacc[r] = vis ? pacc[r] : 0.f;
+          if (CAREFUL && !vis) seen[r / 8][r % 8 / 2] &= r % 2 ? 0xFFFFu : 0xFFFF0000u;
+        }
+        asm volatile("" ::: "memory");
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int jo = 8 * (r >> 2) + (r & 3);
-        float add = nlse;
-        if constexpr (BIAS) {
-          if constexpr (EDGE) add = fmaf(-sl, fabsf(ahead - (float)jo), nlse);
-          else add = fmaf(-slp, ahead - (float)jo, nlse);
-        }
         if constexpr (CAP) {
           const float rr = cap_r(sacc[r], c1);
-          const float p = fast_exp2(fmaf(rr, -2.f * cap2, cap2 + add));
-          ds[r] = p * pacc[r] * fmaf(-rr, rr, rr);
+          const float p = fast_exp2(fmaf(rr, -2.f * cap2, add[r]));
+          pacc[r] = p * pacc[r] * fmaf(-rr, rr, rr);
         } else {
-          ds[r] = fast_exp2(fmaf(sacc[r], c, add)) * pacc[r];
-        }
-        if constexpr (EDGE) {
-          if ((uint32_t)(past + jo) >= (uint32_t)(hi - lo)) ds[r] = 0.f;
-          else if (CAREFUL) seen[r / 8][r % 8 / 2] |= r % 2 ? 0x3F800000u : 0x3F80u;
+          const int jo = 8 * (r >> 2) + (r & 3);
+          const float b = BIAS ? fmaf(slp, (float)jo, base) : base;
+          pacc[r] = fast_exp2(fmaf(sacc[r], c, b)) * pacc[r];
         }
       }
       bf16x8 sb[2];
-      pack16(ds, sb);
+      pack16(pacc, sb);
       wave_priority<1>();
 #pragma unroll
       for (int n = 0; n < C::NE; ++n)
@@ -813,7 +833,6 @@ __device__ __forceinline__ void dq_tile(const BwdArgs &a, int L, unsigned char *
       __builtin_amdgcn_sched_barrier(0);
       wave_priority<0>();
     }
-    keep_apart<EDGE>();
   };
   auto begin_tile = [&](int u) __attribute__((always_inline)) {
     if constexpr (kSt == 4) {
@@ -834,18 +853,19 @@ __device__ __forceinline__ void dq_tile(const BwdArgs &a, int L, unsigned char *
   using Yes = std::true_type;
   constexpr int kWaveKeys = 32 * C::KM;
   for (int u = 0; u < kSt / 2 && u < nt; ++u) load_tile(u);
-  auto turn = [&](int u, int st) __attribute__((always_inline)) {
-    begin_tile(u);
+  auto take = [&](int u, int st, auto careful_tag) __attribute__((always_inline)) {
     const int j0 = (t0 + u) * C::BN + kWaveKeys * part;
     if (wh.none(j0, kWaveKeys)) return;  // wave-uniform
     const bool crosses = BIAS && j0 + kWaveKeys - 1 > wrow0 && j0 < wrow0 + 31;
-    if (wh.full(j0, kWaveKeys) && !crosses) tile(u, st, No{}, No{});
-    else tile(u, st, Yes{}, No{});
+    tile(u, st, !wh.full(j0, kWaveKeys) || crosses, careful_tag);
   };
   for (int u0 = 0; u0 < nt; u0 += kSt)
 #pragma unroll
     for (int st = 0; st < kSt; ++st)
-      if (u0 + st < nt) turn(u0 + st, st);
+      if (u0 + st < nt) {
+        begin_tile(u0 + st);
+        take(u0 + st, st, No{});
+      }
   // As in the key pass: infinities or NaN in K.
   {
     float z = 0.f;
@@ -860,8 +880,7 @@ __device__ __forceinline__ void dq_tile(const BwdArgs &a, int L, unsigned char *
         load_tile(u);
         wait_vmcnt<0>();
         barrier_no_fence();
-        if (!wh.none((t0 + u) * C::BN + kWaveKeys * part, kWaveKeys))
-          tile(u, u % kSt, Yes{}, Yes{});
+        take(u, u % kSt, Yes{});
       }
       __syncthreads();
     }
