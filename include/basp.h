@@ -553,7 +553,7 @@ size_t basp_attn_decode_shared_workspace_bytes(int b, int n_q, int n_k, int d, i
  * scores of basp_attn_span_fwd:
  *   s_j = scale * q . k_j,  u_j = cap * tanh(s_j / cap) - slope_h * (lens[s] - 1 - j)
  *   O = sum_{j < lens[s]} softmax_j(u_j) v_j,  LSE = log sum_{j < lens[s]} exp(u_j)
- * cap: 0 for none, else up to 1024; slopes: fp32 [n_q], any finite numbers, or NULL.
+ * cap: 0 for none, else up to 1024; slopes: fp32 [n_q], up to 2^64, or NULL.
  * groups: int32 [n_groups + 1], ascending: group g is the sequences groups[g] ..
  * groups[g+1] - 1.  prefix_lens: int32 [n_groups]: those of the group's sequences that are
  * at least so long all list pages with the same first prefix_lens[g] tokens (the very
@@ -592,7 +592,7 @@ int basp_attn_decode_shared(const void *q, const void *k_pages, const void *v_pa
  * spans: int32 [b, S, 2], (lo, hi) of every row, cut to [0, S]; hi <= lo: the row sees
  * nothing (padding), its O is 0, its LSE -inf and all its gradients 0.  NULL: causal.
  * Spans are read on the device; whatever they hold, nothing outside the tensors is
- * read.  slopes: fp32 [n_q], any finite numbers, constants of the model (no
+ * read.  slopes: fp32 [n_q], of either sign, up to 2^64, constants of the model (no
  * gradients), or NULL.  cap: 0 for none, else up to 1024.
  * q [b, S, n_q, d], k and v [b, S, n_k, d] bf16, tokens q_row (k_row, v_row) elements
  * apart, b*S of them in one run, so they may be columns of one projection's output;
@@ -604,7 +604,7 @@ int basp_attn_decode_shared(const void *q, const void *k_pages, const void *v_pa
  * P.  A value, key, query or gradient outside every span that it would meet does not
  * count, infinities and NaN too; inside one they make what they reach NaN: a value
  * its element of O, a score of plus infinity or NaN its row.
- * Conditions: d 64, 80, 96 or 128; scale finite and positive; 16-byte aligned q, k, v, o,
+ * Conditions: d 64, 80, 96 or 128; scale 2^-40 to 2^40; 16-byte aligned q, k, v, o,
  * d_o and gradients, strides multiples of 8; spans 8, lse and slopes 4.  Errors: NULL, SHAPE
  * (negative size, n_q % n_k != 0, a row stride below n*d), UNSUPPORTED (d, scale, cap;
  * (S + 256) * row stride * 2 >= 2^31 bytes for any of the tensors, b > 65535, or b*n_q

@@ -26,7 +26,7 @@ int check_rule(int S, int n_q, int n_k, int d, long long q_row, long long k_row,
                float scale, float cap) {
   if (q_row < (long long)n_q * d || k_row < (long long)n_k * d || v_row < (long long)n_k * d)
     return BASP_ERR_SHAPE;
-  if (!(scale > 0.f) || !isfinite(scale) || !(cap >= 0.f) || !(cap <= 1024.f))
+  if (!(scale >= 0x1p-40f) || !(scale <= 0x1p40f) || !(cap >= 0.f) || !(cap <= 1024.f))
     return BASP_ERR_UNSUPPORTED;
   if (cap > 0.f && !isfinite(2.f * scale * basp::kSpanLog2e / cap)) return BASP_ERR_UNSUPPORTED;
   for (long long row : {q_row, k_row, v_row})  // 32-bit offsets inside a sequence

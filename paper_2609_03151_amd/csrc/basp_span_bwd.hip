@@ -73,29 +73,6 @@ __device__ __forceinline__ void store4(void *p, size_t elem, f32x4 x, int bf16) 
     *reinterpret_cast<f32x4 *>(static_cast<float *>(p) + elem) = x;
 }
 
-// An operand of eight bf16 whose infinities and NaN must not meet weights of
-// 0: they become 0, and where a key (or row) that `seen` marks has one, the element of
-// acc becomes NaN.  seen: 1 (0x3F80) in the halves of slots that count.
-__device__ __forceinline__ bf16x8 finite_operand(bf16x8 x, u32x4 seen, f32x16 &acc) {
-  u32x4 v = __builtin_bit_cast(u32x4, x), bad;
-#pragma unroll
-  for (int y = 0; y < 4; ++y) bad[y] = nonfinite_halves(v[y]);
-  if (__builtin_amdgcn_ballot_w64((bad.x | bad.y | bad.z | bad.w) != 0)) {
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const uint32_t hi = bad[y] & 0x80000000u, lo = bad[y] & 0x8000u;
-      if (hi) v[y] &= 0xFFFFu;
-      if (lo) v[y] &= 0xFFFF0000u;
-      bad[y] = (hi ? 0x3F800000u : 0u) | (lo ? 0x3F80u : 0u);
-    }
-    const f32x16 count = mfma32x32x16(as_bf16x8(bad), as_bf16x8(seen), f32x16{});
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      if (count[r] > 0.f) acc[r] = __builtin_nanf("");
-  }
-  return as_bf16x8(v);
-}
-
 // Sixteen weights of the accumulator as two operands.
 __device__ __forceinline__ void pack16(const f32x16 &x, bf16x8 (&out)[2]) {
 #pragma unroll

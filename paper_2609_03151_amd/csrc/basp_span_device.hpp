@@ -18,15 +18,6 @@ __device__ __forceinline__ void copy16_to_lds(u32x4 rsrc, uint32_t off, uint32_t
                : "memory");
 }
 
-// At the start and the end of code that two branches hold in two forms: keeps the
-// compiler from moving what they have in common (operand reads for the most part) in
-// front of or behind the branch, where it would fill the registers.
-template <bool A>
-__device__ __forceinline__ void keep_apart() {
-  if constexpr (A) asm volatile("; a" ::: "memory");
-  else asm volatile("; b" ::: "memory");
-}
-
 // lo and hi of a row, inside [0, S]; empty spans as lo = hi = 0.
 __device__ __forceinline__ void span_of(const int *spans, size_t beta, int S, int row, int &lo,
                                         int &hi) {
@@ -80,6 +71,29 @@ __device__ __forceinline__ SpanHull wave_hull(SpanHull h) {
 // Words of two bf16: the bits 15 and 31 are set where a half is infinite or NaN.
 __device__ __forceinline__ uint32_t nonfinite_halves(uint32_t w) {
   return ((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;
+}
+
+// An operand of eight bf16 whose infinities and NaN must not meet weights of
+// 0: they become 0, and where a key (or row) that `seen` marks has one, the element of
+// acc becomes NaN.  seen: 1 (0x3F80) in the halves of slots that count.
+__device__ __forceinline__ bf16x8 finite_operand(bf16x8 x, u32x4 seen, f32x16 &acc) {
+  u32x4 v = __builtin_bit_cast(u32x4, x), bad;
+#pragma unroll
+  for (int y = 0; y < 4; ++y) bad[y] = nonfinite_halves(v[y]);
+  if (__builtin_amdgcn_ballot_w64((bad.x | bad.y | bad.z | bad.w) != 0)) {
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const uint32_t hi = bad[y] & 0x80000000u, lo = bad[y] & 0x8000u;
+      if (hi) v[y] &= 0xFFFFu;
+      if (lo) v[y] &= 0xFFFF0000u;
+      bad[y] = (hi ? 0x3F800000u : 0u) | (lo ? 0x3F80u : 0u);
+    }
+    const f32x16 count = mfma32x32x16(as_bf16x8(bad), as_bf16x8(seen), f32x16{});
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (count[r] > 0.f) acc[r] = __builtin_nanf("");
+  }
+  return as_bf16x8(v);
 }
 
 }  // namespace basp

@@ -12,8 +12,9 @@
 // ring of stages.  A lane holds one row's scores of 16 keys per 32.
 //
 // Masks cost what lies on their edges: the workgroup visits the tiles between
-// its rows' least lo and largest hi, and a wave skips tiles that none of its 32
-// rows sees and takes tiles that all of them see without any mask.
+// its rows' least lo and largest hi, a wave skips tiles that none of its 32 rows sees,
+// and only where some row sees some keys of a tile are its scores masked one by one,
+// in place behind one branch: two forms of a whole tile would fill the registers.
 #include <math.h>
 
 #include <type_traits>
@@ -26,6 +27,8 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kWaves = 8;
 constexpr float kRescaleSlack = 8.f;  // log2 headroom before the reference max moves
+// A lane's sum of a tile's P past which the pipelined loop moves the reference.
+constexpr float kFollowSum = 65536.f;
 constexpr int kSchedMfma = 0x008;
 constexpr int kSchedDsRead = 0x100;
 
@@ -106,302 +109,115 @@ __device__ __forceinline__ bool merge_parts(unsigned char *smem, int rg, int par
   return true;
 }
 
-template <int D, int R, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kThreads, 1) void span_fwd_kernel(const SpanArgs a,
-                                                               uint16_t *__restrict__ o,
-                                                               float *__restrict__ lse,
-                                                               int heads_total, int qtiles) {
-  using C = Cfg<D, R>;
-  using T = LdsTile<C::LW>;
-  // LDS: the K tiles of the ring stages, then their V tiles.
-  __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
-  __shared__ int hulls[2][kWaves];
-  constexpr int kSt = C::STAGES, kVRegion = kSt * C::TILE_BYTES;
+// What the workgroup and this lane work on: one head's rows q0 .. q0 + BM - 1, the
+// lane's row (with lane l ^ 32) and its rule.
+template <class C>
+struct Work {
+  int beta, h, wrow0, row, lo, hi;
+  int t0, nt;            // the tiles some row sees
+  SpanHull hull;         // of the wave's rows
+  float sl, c, rc, c1, cap2;
+  bool fixed;            // the reference stands still (kSpanFixedCap)
+  float m_ref, l_run;
+  u32x4 rk, rv;
+  uint32_t k_row_bytes, v_row_bytes;
 
-  const int S = a.S, Hl = a.Hl;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, hh = lane >> 5;
-  const int rg = w % R, part = w / R;  // row group, key part
+  // First key of the wave in tile u.
+  __device__ __forceinline__ int first_key(int u, int part) const {
+    return (t0 + u) * C::BN + 32 * C::KM * part;
+  }
+  __device__ __forceinline__ bool none(int u, int part) const {
+    return hull.none(first_key(u, part), 32 * C::KM);
+  }
+  // Some row sees only some of the keys, or the bias changes its sign among them.
+  template <bool BIAS>
+  __device__ __forceinline__ bool edge(int u, int part) const {
+    const int j0 = first_key(u, part), n = 32 * C::KM;
+    return !hull.full(j0, n) || (BIAS && j0 + n - 1 > wrow0 && j0 < wrow0 + 31);
+  }
+  // Scores of the keys from j0 on (32 of them) of an edge: the bias goes into them,
+  // and what the row does not see becomes -inf.
+  template <bool BIAS>
+  __device__ __forceinline__ void fix_scores(f32x16 &sc, int jl) const {
+    asm volatile("" ::: "memory");
+    const float ahead = (float)(row - jl);
+    const int past = jl - lo;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int jo = 8 * (r >> 2) + (r & 3);
+      const bool vis = (uint32_t)(past + jo) < (uint32_t)(hi - lo);
+      const float x = BIAS ? fmaf(-sl * rc, fabsf(ahead - (float)jo), sc[r]) : sc[r];
+      sc[r] = vis ? x : -INFINITY;
+    }
+    asm volatile("" ::: "memory");
+  }
+};
 
-  const int L = blockIdx.x;
-  const int qt = qtiles - 1 - L / heads_total;
-  const int hb = L % heads_total;
-  const int beta = hb / Hl, h = hb % Hl, kvh = h / (Hl / a.Hkl);
-  const int q0 = qt * C::BM;
-  const int wrow0 = q0 + 32 * rg;
-  const int row = wrow0 + l32;
-
+template <class C, int D, bool CAP, bool BIAS>
+__device__ __forceinline__ void enter(Work<C> &wk, bf16x8 (&qf)[C::NS], const SpanArgs &a,
+                                      int heads_total, int qtiles, int (&hulls)[2][kWaves]) {
+  const int S = a.S, Hl = a.Hl, lane = threadIdx.x & 63, hh = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int L = blockIdx.x, qt = qtiles - 1 - L / heads_total, hb = L % heads_total;
+  wk.beta = hb / Hl, wk.h = hb % Hl;
+  const int kvh = wk.h / (Hl / a.Hkl), q0 = qt * C::BM;
+  wk.wrow0 = q0 + 32 * (w % C::R);
+  wk.row = wk.wrow0 + (lane & 31);
   const uint32_t q_row_bytes = a.q.row_elems * 2;
-  const uint32_t k_row_bytes = a.k.row_elems * 2, v_row_bytes = a.v.row_elems * 2;
-  const rsrc_t rq = make_rsrc(a.q.p + ((size_t)beta * S + q0) * a.q.row_elems + (size_t)h * D,
+  wk.k_row_bytes = a.k.row_elems * 2;
+  wk.v_row_bytes = a.v.row_elems * 2;
+  const size_t first = (size_t)wk.beta * S;
+  const rsrc_t rq = make_rsrc(a.q.p + (first + q0) * a.q.row_elems + (size_t)wk.h * D,
                               (uint32_t)(S - q0) * q_row_bytes);
-  const u32x4 rk = make_rsrc_words(a.k.p + (size_t)beta * S * a.k.row_elems + (size_t)kvh * D,
-                                   (uint32_t)S * k_row_bytes);
-  const u32x4 rv = make_rsrc_words(a.v.p + (size_t)beta * S * a.v.row_elems + (size_t)kvh * D,
-                                   (uint32_t)S * v_row_bytes);
-  const uint32_t smem_lds = lds_addr_of(smem);
-
-  bf16x8 qf[C::NS];
+  wk.rk = make_rsrc_words(a.k.p + first * a.k.row_elems + (size_t)kvh * D,
+                          (uint32_t)S * wk.k_row_bytes);
+  wk.rv = make_rsrc_words(a.v.p + first * a.v.row_elems + (size_t)kvh * D,
+                          (uint32_t)S * wk.v_row_bytes);
 #pragma unroll
   for (int s = 0; s < C::NS; ++s)
-    qf[s] = as_bf16x8(buf_load16(rq, (uint32_t)(row - q0) * q_row_bytes + (2 * s + hh) * 16));
-  int lo = 0, hi = 0;
-  if (row < S) span_of(a.spans, beta, S, row, lo, hi);
-  float sl = 0.f;  // the slope in log2 units
-  if constexpr (BIAS) sl = a.slopes[h] * kSpanLog2e;
-  const SpanHull wh = wave_hull(hull_of(lo, hi, row < S));
-  if (lane == 0) hulls[0][w] = wh.any_lo, hulls[1][w] = wh.any_hi;
+    qf[s] = as_bf16x8(
+        buf_load16(rq, (uint32_t)(wk.row - q0) * q_row_bytes + (2 * s + hh) * 16));
+  wk.lo = wk.hi = 0;
+  if (wk.row < S) span_of(a.spans, wk.beta, S, wk.row, wk.lo, wk.hi);
+  wk.sl = BIAS ? a.slopes[wk.h] * kSpanLog2e : 0.f;  // in log2 units
+  wk.hull = wave_hull(hull_of(wk.lo, wk.hi, wk.row < S));
+  if (lane == 0) hulls[0][w] = wk.hull.any_lo, hulls[1][w] = wk.hull.any_hi;
   wait_vmcnt<0>();  // retire the tracked loads before untracked copies start
   __syncthreads();
-  int all_lo = hulls[0][0], all_hi = hulls[1][0];
+  int lo = hulls[0][0], hi = hulls[1][0];
 #pragma unroll
-  for (int i = 1; i < R; ++i) {
-    all_lo = min(all_lo, hulls[0][i]);
-    all_hi = max(all_hi, hulls[1][i]);
+  for (int i = 1; i < C::R; ++i) {
+    lo = min(lo, hulls[0][i]);
+    hi = max(hi, hulls[1][i]);
   }
-  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-  const int t0 = all_lo < all_hi ? all_lo / C::BN : 0;
-  const int nt = all_lo < all_hi ? (all_hi + C::BN - 1) / C::BN - t0 : 0;  // tiles t0 .. t0+nt-1
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  wk.t0 = lo < hi ? lo / C::BN : 0;
+  wk.nt = lo < hi ? (hi + C::BN - 1) / C::BN - wk.t0 : 0;
+  wk.c = a.scale * kSpanLog2e;
+  wk.rc = 1.f / wk.c;
+  wk.c1 = CAP ? 2.f * wk.c / a.cap : 0.f;
+  wk.cap2 = CAP ? a.cap * kSpanLog2e : 0.f;
+  wk.fixed = CAP && a.cap <= kSpanFixedCap;
+  wk.l_run = 0.f;
+  wk.m_ref = -INFINITY;
+  if (wk.fixed) {  // the largest bias of the row, at its nearest or farthest key
+    const int near = wk.row < wk.lo ? wk.lo - wk.row : wk.row >= wk.hi ? wk.row - wk.hi + 1 : 0;
+    const int far = max(abs(wk.row - wk.lo), abs(wk.row - wk.hi + 1));
+    wk.m_ref = BIAS && wk.hi > wk.lo ? fmaxf(-wk.sl * (float)near, -wk.sl * (float)far) : 0.f;
+  }
+}
 
-  uint32_t gk[C::DMA_PER_WAVE], gv[C::DMA_PER_WAVE];
-#pragma unroll
-  for (int i = 0; i < C::DMA_PER_WAVE; ++i) {
-    gk[i] = dma_src_off<C::LW, D>((w * C::DMA_PER_WAVE + i) * 64 + lane, k_row_bytes);
-    gv[i] = dma_src_off<C::LW, D>((w * C::DMA_PER_WAVE + i) * 64 + lane, v_row_bytes);
-  }
-  auto load_tile = [&](int u) __attribute__((always_inline)) {  // tile t0 + u
-    const uint32_t ks = smem_lds + (u % kSt) * C::TILE_BYTES;
-    const uint32_t kb = (uint32_t)((t0 + u) * C::BN) * k_row_bytes;
-    const uint32_t vb = (uint32_t)((t0 + u) * C::BN) * v_row_bytes;
-#pragma unroll
-    for (int i = 0; i < C::DMA_PER_WAVE; ++i) {
-      const uint32_t lds_off = ks + (w * C::DMA_PER_WAVE + i) * 1024;
-      copy16_to_lds(rk, kb + gk[i], lds_off);
-      copy16_to_lds(rv, vb + gv[i], lds_off + kVRegion);
-    }
-  };
-  // Tiles 0 .. kSt-2 are issued up front; iteration u waits for its own copies of
-  // tile u, passes the barrier and issues tile u + kSt-1 into the stage of tile
-  // u-1, which every wave has finished with.
-  auto begin_tile = [&](int u) __attribute__((always_inline)) {
-    if constexpr (kSt == 4) {
-      const int ahead = min(2, nt - 1 - u);
-      if (ahead >= 2) wait_vmcnt<4 * C::DMA_PER_WAVE>();
-      else if (ahead == 1) wait_vmcnt<2 * C::DMA_PER_WAVE>();
-      else wait_vmcnt<0>();
-    } else {
-      wait_vmcnt<0>();
-    }
-    barrier_no_fence();
-    if (u + kSt - 1 < nt) load_tile(u + kSt - 1);
-  };
-#pragma unroll
-  for (int u = 0; u < kSt - 1; ++u)
-    if (u < nt) load_tile(u);
-
-  // This lane's operand reads: K row l32 and V^T rows of the wave's part.
-  const int part_off = part * 32 * C::KM * T::ROW_BYTES;
-  int k_off[C::NS], v_off[C::NE][2];
-#pragma unroll
-  for (int s = 0; s < C::NS; ++s) {
-    k_off[s] = T::off(l32, 2 * s + hh) + part_off;
-    asm volatile("" : "+v"(k_off[s]));
-  }
-#pragma unroll
-  for (int n = 0; n < C::NE; ++n)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      v_off[n][x] = kVRegion + part_off +
-                    tr_piece_off<C::LW>(4 * hh + 8 * x, 32 * n + 16 * ((lane >> 4) & 1), lane);
-      asm volatile("" : "+v"(v_off[n][x]));
-    }
-
-  const float c = a.scale * kSpanLog2e;
-  const float c1 = CAP ? 2.f * c / a.cap : 0.f, cap2 = CAP ? a.cap * kSpanLog2e : 0.f;
-  const bool fixed = CAP && a.cap <= kSpanFixedCap;
-  // The exponents' reference.  With a cap that allows it (kSpanFixedCap) it
-  // is the largest bias of the row, at its nearest or farthest key; else the
-  // running maximum.
-  float m_ref = -INFINITY, l_run = 0.f;
-  if (fixed) {
-    const int near = row < lo ? lo - row : row >= hi ? row - hi + 1 : 0;
-    const int far = max(abs(row - lo), abs(row - hi + 1));
-    m_ref = BIAS && hi > lo ? fmaxf(-sl * (float)near, -sl * (float)far) : 0.f;
-  }
-  f32x16 oacc[C::NE];
-  auto clear = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int n = 0; n < C::NE; ++n)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[n][r] = 0.f;
-  };
-  clear();
-
-  // One tile.  EDGE: some row sees only some of its keys (or the bias changes its
-  // sign in it).  CAREFUL: V holds infinities or NaN somewhere, which must not
-  // reach a row through a weight of 0.
-  auto tile = [&](int u, auto edge_tag, auto careful_tag) __attribute__((always_inline)) {
-    constexpr bool EDGE = decltype(edge_tag)::value, CAREFUL = decltype(careful_tag)::value;
-    const int j0 = (t0 + u) * C::BN + 32 * C::KM * part;
-    const unsigned char *Ks = smem + (u % kSt) * C::TILE_BYTES;
-    keep_apart<EDGE>();
-#pragma unroll
-    for (int m = 0; m < C::KM; ++m) {
-      f32x16 sc;
-      wave_priority<1>();
-#pragma unroll
-      for (int s = 0; s < C::NS; ++s) {
-        const bf16x8 x = *reinterpret_cast<const bf16x8 *>(Ks + k_off[s] + m * 32 * T::ROW_BYTES);
-        sc = mfma32x32x16(x, qf[s], s == 0 ? f32x16{} : sc);
-      }
-      wave_priority<0>();
-      // sc[r] = (q . k) of key jl + 8(r/4) + r%4 for this lane's row
-      const int jl = j0 + 32 * m + 4 * hh;
-      float ahead = (float)(row - jl);  // distance to the lane's first key
-      int past = jl - lo;
-      // (else sums of these and the 16 offsets are kept over the whole loop)
-      asm volatile("" : "+v"(ahead), "+v"(past));
-      const float slp = j0 + 32 * m > wrow0 ? -sl : sl;  // not EDGE: all keys on one side
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int jo = 8 * (r >> 2) + (r & 3);
-        float x = sc[r];
-        if constexpr (CAP) x = fmaf(cap_r(x, c1), -2.f * cap2, cap2);
-        else x *= c;
-        if constexpr (BIAS) {
-          if constexpr (EDGE) x = fmaf(-sl, fabsf(ahead - (float)jo), x);
-          else x = fmaf(-slp, ahead - (float)jo, x);
-        }
-        if constexpr (EDGE)
-          if ((uint32_t)(past + jo) >= (uint32_t)(hi - lo)) x = -INFINITY;
-        sc[r] = x;
-      }
-      if (!fixed) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-        mx = pair_max(mx);
-        const bool grow = mx > m_ref + kRescaleSlack;
-        if (__builtin_amdgcn_ballot_w64(grow)) {  // wave-uniform, rare after the first tiles
-          asm volatile("" ::: "memory");
-          const float alpha = grow ? fast_exp2(m_ref - mx) : 1.f;
-          m_ref = grow ? mx : m_ref;
-          l_run *= alpha;
-#pragma unroll
-          for (int n = 0; n < C::NE; ++n)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) oacc[n][r] *= alpha;
-        }
-      }
-      // A row of which no key has come yet: every score is -inf, P = 0.
-      const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-      float psum = 0.f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        sc[r] = fast_exp2(sc[r] - m_use);
-        psum += sc[r];
-      }
-      l_run += psum;
-      u32x4 pw[2];
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        const int b8 = 8 * s2;
-        pw[s2] = u32x4{pack_bf16x2(sc[b8 + 0], sc[b8 + 1]), pack_bf16x2(sc[b8 + 2], sc[b8 + 3]),
-                       pack_bf16x2(sc[b8 + 4], sc[b8 + 5]), pack_bf16x2(sc[b8 + 6], sc[b8 + 7])};
-      }
-#pragma unroll
-      for (int n = 0; n < C::NE; ++n) {
-#pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
-          const int ro = (2 * m + s2) * 16 * T::ROW_BYTES;
-          bf16x8 x = tr_operand(Ks, v_off[n][0] + ro, v_off[n][1] + ro);
-          if constexpr (CAREFUL) {
-            u32x4 v = __builtin_bit_cast(u32x4, x), bad;
-#pragma unroll
-            for (int y = 0; y < 4; ++y) bad[y] = nonfinite_halves(v[y]);
-            if (__builtin_amdgcn_ballot_w64((bad.x | bad.y | bad.z | bad.w) != 0)) {
-              // how many such values of its column each row sees: 1 for each
-              // in V's place, 1 for each key seen in P's
-              u32x4 seen;
-#pragma unroll
-              for (int y = 0; y < 4; ++y) {
-                const uint32_t one_hi = bad[y] & 0x80000000u, one_lo = bad[y] & 0x8000u;
-                if (one_hi) v[y] &= 0xFFFFu;
-                if (one_lo) v[y] &= 0xFFFF0000u;
-                bad[y] = (one_hi ? 0x3F800000u : 0u) | (one_lo ? 0x3F80u : 0u);
-                const int r = 8 * s2 + 2 * y, j = jl + 8 * (r >> 2) + (r & 3);
-                seen[y] = ((uint32_t)(j - lo) < (uint32_t)(hi - lo) ? 0x3F80u : 0u) |
-                          ((uint32_t)(j + 1 - lo) < (uint32_t)(hi - lo) ? 0x3F800000u : 0u);
-              }
-              const f32x16 count = mfma32x32x16(as_bf16x8(bad), as_bf16x8(seen), f32x16{});
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                if (count[r] > 0.f) oacc[n][r] = __builtin_nanf("");
-              x = as_bf16x8(v);
-            }
-          }
-          oacc[n] = mfma32x32x16(x, as_bf16x8(pw[s2]), oacc[n]);
-        }
-      }
-      if constexpr (!CAREFUL) {
-        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 4, 0);
-#pragma unroll
-        for (int i = 0; i < 2 * C::NE - 2; ++i) {
-          __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    keep_apart<EDGE>();
-  };
-  using No = std::false_type;
-  using Yes = std::true_type;
-  constexpr int kWaveKeys = 32 * C::KM;
-  for (int u = 0; u < nt; ++u) {
-    begin_tile(u);
-    const int j0 = (t0 + u) * C::BN + kWaveKeys * part;
-    if (wh.none(j0, kWaveKeys)) continue;  // wave-uniform
-    const bool crosses = BIAS && j0 + kWaveKeys - 1 > wrow0 && j0 < wrow0 + 31;
-    if (wh.full(j0, kWaveKeys) && !crosses) tile(u, No{}, No{});
-    else tile(u, Yes{}, No{});
-  }
-
-  // O of no finite value anywhere in the workgroup: infinities or NaN in V, which
-  // 0 * V may have carried to rows that do not see them (or an overflow).  All rows
-  // again, tile by tile, with such values kept apart.
-  {
-    float z = 0.f;
-#pragma unroll
-    for (int n = 0; n < C::NE; ++n)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) z = fmaf(0.f, oacc[n][r], z);
-    if (__syncthreads_or(!(z == 0.f))) {
-      if (!fixed) m_ref = -INFINITY;
-      l_run = 0.f;
-      clear();
-      for (int u = 0; u < nt; ++u) {
-        barrier_no_fence();  // every wave is done with the stage
-        load_tile(u);
-        wait_vmcnt<0>();
-        barrier_no_fence();
-        if (!wh.none((t0 + u) * C::BN + kWaveKeys * part, kWaveKeys)) tile(u, Yes{}, Yes{});
-      }
-    }
-  }
-
-  // oacc[n][r] = O^T[e = 32n + 8(r/4) + 4hh + r%4][query row] (unnormalised)
-  float l_tot = pair_sum(l_run);
-  if constexpr (C::P > 1) {
-    if (!merge_parts<C>(smem, rg, part, lane, m_ref, l_tot, oacc)) return;
-  }
-  if (row >= S) return;
-  const bool empty = hi <= lo;
+// O and LSE of the lane's row.  oacc[n][r] = O^T[e = 32n + 8(r/4) + 4hh + r%4][row],
+// not divided by the row's sum.
+template <class C, int D>
+__device__ __forceinline__ void leave(const Work<C> &wk, const SpanArgs &a, uint16_t *o,
+                                      float *lse, float l_tot, const f32x16 (&oacc)[C::NE]) {
+  if (wk.row >= a.S) return;
+  const int hh = (threadIdx.x & 63) >> 5;
+  const bool empty = wk.hi <= wk.lo;
   const float inv = empty ? 0.f : 1.f / l_tot;
-  uint16_t *ob = o + (((size_t)beta * S + row) * Hl + h) * D;
+  uint16_t *ob = o + (((size_t)wk.beta * a.S + wk.row) * a.Hl + wk.h) * D;
 #pragma unroll
   for (int n = 0; n < C::NE; ++n)
 #pragma unroll
@@ -413,15 +229,477 @@ __global__ __launch_bounds__(kThreads, 1) void span_fwd_kernel(const SpanArgs a,
       *reinterpret_cast<u32x2 *>(ob + 32 * n + 8 * g + 4 * hh) = val;
     }
   if (hh == 0)
-    lse[((size_t)beta * Hl + h) * S + row] =
-        empty ? -INFINITY : (m_ref + fast_log2(l_tot)) * kSpanLn2;
+    lse[((size_t)wk.beta * a.Hl + wk.h) * a.S + wk.row] =
+        empty ? -INFINITY : (wk.m_ref + fast_log2(l_tot)) * kSpanLn2;
+}
+
+template <int NE>
+__device__ __forceinline__ void clear(f32x16 (&acc)[NE]) {
+#pragma unroll
+  for (int n = 0; n < NE; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[n][r] = 0.f;
+}
+template <int NE>
+__device__ __forceinline__ bool finite(const f32x16 (&acc)[NE], float z) {
+#pragma unroll
+  for (int n = 0; n < NE; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = fmaf(0.f, acc[n][r], z);
+  return z == 0.f;
+}
+
+// Maximum `mx` of new scores (log2 units) against the row's reference.
+template <class C>
+__device__ __forceinline__ void move_reference(Work<C> &wk, f32x16 (&oacc)[C::NE], float mx) {
+  const bool grow = mx > wk.m_ref + kRescaleSlack;
+  if (__builtin_amdgcn_ballot_w64(grow)) {  // wave-uniform, rare after the first tiles
+    asm volatile("" ::: "memory");
+    const float alpha = grow ? fast_exp2(wk.m_ref - mx) : 1.f;
+    wk.m_ref = grow ? mx : wk.m_ref;
+    wk.l_run *= alpha;
+#pragma unroll
+    for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[n][r] *= alpha;
+  }
+}
+
+__device__ __forceinline__ u32x4 pack8(const f32x16 &x, int b8) {
+  return u32x4{pack_bf16x2(x[b8 + 0], x[b8 + 1]), pack_bf16x2(x[b8 + 2], x[b8 + 3]),
+               pack_bf16x2(x[b8 + 4], x[b8 + 5]), pack_bf16x2(x[b8 + 6], x[b8 + 7])};
+}
+
+// LDS offsets of the lane's operand reads.
+template <class C, int D>
+struct Offsets {
+  using T = LdsTile<C::LW>;
+  int k[C::NS], v[C::NE][2];
+  __device__ __forceinline__ Offsets(int part) {
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5;
+    const int part_off = part * 32 * C::KM * T::ROW_BYTES;
+#pragma unroll
+    for (int s = 0; s < C::NS; ++s) {
+      k[s] = T::off(l32, 2 * s + hh) + part_off;
+      asm volatile("" : "+v"(k[s]));
+    }
+#pragma unroll
+    for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        v[n][x] = C::STAGES * C::TILE_BYTES + part_off +
+                  tr_piece_off<C::LW>(4 * hh + 8 * x, 32 * n + 16 * ((lane >> 4) & 1), lane);
+        asm volatile("" : "+v"(v[n][x]));
+      }
+  }
+};
+
+// Tile u's K and V of the workgroup into stage u % STAGES.
+template <class C, int D>
+struct Copies {
+  uint32_t gk[C::DMA_PER_WAVE], gv[C::DMA_PER_WAVE], base;
+  __device__ __forceinline__ Copies(const Work<C> &wk, const void *smem) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < C::DMA_PER_WAVE; ++i) {
+      const int pos = (w * C::DMA_PER_WAVE + i) * 64 + lane;
+      gk[i] = dma_src_off<C::LW, D>(pos, wk.k_row_bytes);
+      gv[i] = dma_src_off<C::LW, D>(pos, wk.v_row_bytes);
+    }
+    base = lds_addr_of(smem) + w * C::DMA_PER_WAVE * 1024;
+  }
+  __device__ __forceinline__ void load(const Work<C> &wk, int u) const {
+    const uint32_t ks = base + (u % C::STAGES) * C::TILE_BYTES;
+    const uint32_t kb = (uint32_t)((wk.t0 + u) * C::BN) * wk.k_row_bytes;
+    const uint32_t vb = (uint32_t)((wk.t0 + u) * C::BN) * wk.v_row_bytes;
+#pragma unroll
+    for (int i = 0; i < C::DMA_PER_WAVE; ++i) {
+      copy16_to_lds(wk.rk, kb + gk[i], ks + i * 1024);
+      copy16_to_lds(wk.rv, vb + gv[i], ks + i * 1024 + C::STAGES * C::TILE_BYTES);
+    }
+  }
+};
+
+// One tile by itself: scores, reference, exponentials, P V, 32 keys at a time.  CAREFUL: V
+// holds infinities or NaN somewhere, which must not reach a row through a weight of 0.
+template <class C, int D, bool CAP, bool BIAS, bool CAREFUL>
+__device__ __forceinline__ void one_tile(Work<C> &wk, const Offsets<C, D> &off,
+                                         const bf16x8 (&qf)[C::NS], f32x16 (&oacc)[C::NE],
+                                         const unsigned char *Ks, int u, int part) {
+  using T = LdsTile<C::LW>;
+  const int hh = (threadIdx.x & 63) >> 5;
+  const bool edge = wk.template edge<BIAS>(u, part);
+  const int j0 = wk.first_key(u, part);
+#pragma unroll
+  for (int m = 0; m < C::KM; ++m) {
+    f32x16 sc;
+    wave_priority<1>();
+#pragma unroll
+    for (int s = 0; s < C::NS; ++s) {
+      const bf16x8 x = *reinterpret_cast<const bf16x8 *>(Ks + off.k[s] + m * 32 * T::ROW_BYTES);
+      sc = mfma32x32x16(x, qf[s], s == 0 ? f32x16{} : sc);
+    }
+    wave_priority<0>();
+    // sc[r] = (q . k) of key jl + 8(r/4) + r%4 for this lane's row
+    const int jl = j0 + 32 * m + 4 * hh;
+    const float slp = edge ? 0.f : j0 + 32 * m > wk.wrow0 ? -wk.sl : wk.sl;
+    const float base = BIAS ? -slp * (float)(wk.row - jl) : 0.f;
+    u32x4 seen[2] = {};
+    if (CAREFUL) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if ((uint32_t)(jl + 8 * (r >> 2) + (r & 3) - wk.lo) < (uint32_t)(wk.hi - wk.lo))
+          seen[r / 8][r % 8 / 2] |= r % 2 ? 0x3F800000u : 0x3F80u;
+    }
+    if constexpr (CAP) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = fmaf(cap_r(sc[r], wk.c1), -2.f * wk.cap2, wk.cap2) * wk.rc;
+    }
+    if (edge) wk.template fix_scores<BIAS>(sc, jl);  // wave-uniform
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      sc[r] = fmaf(sc[r], wk.c, BIAS ? fmaf(slp, (float)(8 * (r >> 2) + (r & 3)), base) : base);
+    if (!wk.fixed) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+      move_reference<C>(wk, oacc, pair_max(mx));
+    }
+    // A row of which no key has come yet: every score is -inf, P = 0.
+    const float m_use = wk.m_ref == -INFINITY ? 0.f : wk.m_ref;
+    float psum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      sc[r] = fast_exp2(sc[r] - m_use);
+      psum += sc[r];
+    }
+    wk.l_run += psum;
+    const bf16x8 pf[2] = {as_bf16x8(pack8(sc, 0)), as_bf16x8(pack8(sc, 8))};
+#pragma unroll
+    for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const int ro = (2 * m + s2) * 16 * T::ROW_BYTES;
+        bf16x8 x = tr_operand(Ks, off.v[n][0] + ro, off.v[n][1] + ro);
+        if constexpr (CAREFUL) x = finite_operand(x, seen[s2], oacc[n]);
+        oacc[n] = mfma32x32x16(x, pf[s2], oacc[n]);
+      }
+    if constexpr (!CAREFUL) {
+      __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 4, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * C::NE - 2; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// O of no finite value anywhere in the workgroup: infinities or NaN in V, which 0 * V
+// may have carried to rows that do not see them, or P past fp32's range.  All rows again,
+// tile by tile.
+template <class C, int D, bool CAP, bool BIAS>
+__device__ __forceinline__ void again_if_needed(Work<C> &wk, const Offsets<C, D> &off,
+                                                const Copies<C, D> &copies,
+                                                const bf16x8 (&qf)[C::NS], f32x16 (&oacc)[C::NE],
+                                                const unsigned char *smem, int part) {
+  if (!__syncthreads_or(!finite<C::NE>(oacc, 0.f * wk.l_run))) return;
+  if (!wk.fixed) wk.m_ref = -INFINITY;
+  wk.l_run = 0.f;
+  clear<C::NE>(oacc);
+  for (int u = 0; u < wk.nt; ++u) {
+    barrier_no_fence();  // every wave is done with the stage
+    copies.load(wk, u);
+    wait_vmcnt<0>();
+    barrier_no_fence();
+    if (!wk.none(u, part))
+      one_tile<C, D, CAP, BIAS, true>(wk, off, qf, oacc,
+                                      smem + (u % C::STAGES) * C::TILE_BYTES, u, part);
+  }
+}
+
+// Workgroups of 64 or 128 rows, the keys of a tile shared by 4 or 2 waves.
+template <int D, int R, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 1) void span_fwd_split_kernel(const SpanArgs a,
+                                                                     uint16_t *__restrict__ o,
+                                                                     float *__restrict__ lse,
+                                                                     int heads_total, int qtiles) {
+  using C = Cfg<D, R>;
+  // LDS: the K tiles of the ring stages, then their V tiles.
+  __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
+  __shared__ int hulls[2][kWaves];
+  constexpr int kSt = C::STAGES;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rg = w % R, part = w / R;  // row group, key part
+  Work<C> wk;
+  bf16x8 qf[C::NS];
+  enter<C, D, CAP, BIAS>(wk, qf, a, heads_total, qtiles, hulls);
+  const Copies<C, D> copies(wk, smem);
+  // Tiles 0 .. kSt-2 are issued up front; iteration u waits for its own copies of
+  // tile u, passes the barrier and issues tile u + kSt-1 into the stage of tile
+  // u-1, which every wave has finished with.
+  auto begin_tile = [&](int u) __attribute__((always_inline)) {
+    if constexpr (kSt == 4) {
+      const int ahead = min(2, wk.nt - 1 - u);
+      if (ahead >= 2) wait_vmcnt<4 * C::DMA_PER_WAVE>();
+      else if (ahead == 1) wait_vmcnt<2 * C::DMA_PER_WAVE>();
+      else wait_vmcnt<0>();
+    } else {
+      wait_vmcnt<0>();
+    }
+    barrier_no_fence();
+    if (u + kSt - 1 < wk.nt) copies.load(wk, u + kSt - 1);
+  };
+#pragma unroll
+  for (int u = 0; u < kSt - 1; ++u)
+    if (u < wk.nt) copies.load(wk, u);
+  const Offsets<C, D> off(part);
+  f32x16 oacc[C::NE];
+  clear<C::NE>(oacc);
+  for (int u0 = 0; u0 < wk.nt; u0 += kSt)
+#pragma unroll
+    for (int st = 0; st < kSt; ++st)
+      if (u0 + st < wk.nt) {
+        begin_tile(u0 + st);
+        if (!wk.none(u0 + st, part))  // wave-uniform
+          one_tile<C, D, CAP, BIAS, false>(wk, off, qf, oacc, smem + st * C::TILE_BYTES, u0 + st,
+                                           part);
+      }
+  again_if_needed<C, D, CAP, BIAS>(wk, off, copies, qf, oacc, smem, part);
+  float l_tot = pair_sum(wk.l_run);
+  if (!merge_parts<C>(smem, rg, part, lane, wk.m_ref, l_tot, oacc)) return;
+  leave<C, D>(wk, a, o, lse, l_tot, oacc);
+}
+
+// Workgroups of 256 rows, software-pipelined as the causal forward is: the score
+// products of tile u+1 are issued between the exponentials of tile u, and the row sum of
+// u between its P V products, one product per slot.
+// Without a cap a row's reference starts as the maximum of the first scores that it
+// sees, is checked against the maximum on edges, and on the other tiles follows the
+// row sums (half a row's sum is at least its maximum); where P passes fp32's range in
+// between, the workgroup is done again (above).
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 1) void span_fwd_kernel(const SpanArgs a,
+                                                               uint16_t *__restrict__ o,
+                                                               float *__restrict__ lse,
+                                                               int heads_total, int qtiles) {
+  using C = Cfg<D, 8>;
+  using T = LdsTile<C::LW>;
+  constexpr int kSt = C::STAGES, kPD = 2, kPf = 2;
+  static_assert(kSt == 4 && C::KM == 2 && C::P == 1, "the unrolled loop's stages and tiles");
+  __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
+  __shared__ int hulls[2][kWaves];
+  const int hh = (threadIdx.x & 63) >> 5;
+  Work<C> wk;
+  bf16x8 qf[C::NS];
+  enter<C, D, CAP, BIAS>(wk, qf, a, heads_total, qtiles, hulls);
+  const Copies<C, D> copies(wk, smem);
+  const int nt = wk.nt;
+  for (int u = 0; u <= kPD && u < nt; ++u) copies.load(wk, u);
+  const Offsets<C, D> off(0);
+  f32x16 oacc[C::NE];
+  clear<C::NE>(oacc);
+  if (!CAP && wk.row >= a.S) wk.m_ref = 0.f;  // waits for no first key
+
+  // Tile u + 1 readable (tile u if u = -1 + 1 has no next), and tile u + kPD + 1 issued into
+  // the stage of tile u - 1, which every wave has finished with.
+  auto wait_tile = [&](int ahead) __attribute__((always_inline)) {
+    if (ahead >= 2) wait_vmcnt<4 * C::DMA_PER_WAVE>();
+    else if (ahead == 1) wait_vmcnt<2 * C::DMA_PER_WAVE>();
+    else wait_vmcnt<0>();
+  };
+  auto ahead_of = [&](int u, int m) __attribute__((always_inline)) {
+    return (float)(wk.row - ((wk.t0 + u) * C::BN + 32 * m + 4 * hh));
+  };
+  auto slope_of = [&](int u, bool edge) __attribute__((always_inline)) {
+    return edge ? 0.f : (wk.t0 + u) * C::BN > wk.wrow0 ? -wk.sl : wk.sl;
+  };
+  // Tile u's scores are there: its edge, and the reference.
+  auto prepare = [&](int u, bool edge, f32x16 (&sc)[2]) __attribute__((always_inline)) {
+    if constexpr (!CAP) {
+      const bool first = __builtin_amdgcn_ballot_w64(wk.m_ref == -INFINITY) != 0;
+      if (!edge && !first) return;  // wave-uniform
+      const float slp = slope_of(u, edge);
+      float mx = -INFINITY;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        if (edge) wk.template fix_scores<BIAS>(sc[m], (wk.t0 + u) * C::BN + 32 * m + 4 * hh);
+        const float base = BIAS ? -slp * ahead_of(u, m) : 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          mx = fmaxf(mx, fmaf(sc[m][r], wk.c,
+                              BIAS ? fmaf(slp, (float)(8 * (r >> 2) + (r & 3)), base) : base));
+      }
+      move_reference<C>(wk, oacc, pair_max(mx));
+    }
+  };
+  // With a cap, an edge's P: the exponents so far hold neither bias nor reference.
+  auto fix_weights = [&](int u, f32x16 (&p)[2], u32x4 (&pf)[4]) __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float ahead = ahead_of(u, m);
+      const int past = (wk.t0 + u) * C::BN + 32 * m + 4 * hh - wk.lo;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int jo = 8 * (r >> 2) + (r & 3);
+        const bool vis = (uint32_t)(past + jo) < (uint32_t)(wk.hi - wk.lo);
+        float x = p[m][r];
+        if constexpr (BIAS) {
+          // in two halves: a key's P, of up to 2^92 before its bias, may be most of the
+          // row's sum where that bias alone would be below fp32's range
+          const float y = fast_exp2(0.5f * fmaf(-wk.sl, fabsf(ahead - (float)jo), -wk.m_ref));
+          x = x * y * y;
+        }
+        p[m][r] = vis ? x : 0.f;
+      }
+      pf[2 * m] = pack8(p[m], 0);
+      pf[2 * m + 1] = pack8(p[m], 8);
+    }
+    asm volatile("" ::: "memory");
+  };
+  auto follow = [&](float psum) __attribute__((always_inline)) {
+    if (__builtin_amdgcn_ballot_w64(!(psum <= kFollowSum))) {  // wave-uniform, rare
+      asm volatile("" ::: "memory");
+      // 2^-up in two halves: itself it can lie below fp32's normal range
+      const float up = fast_log2(fmaxf(pair_max(psum), 1.f));
+      const float half = fast_exp2(-0.5f * up);
+      wk.m_ref += up;
+      wk.l_run = wk.l_run * half * half;
+#pragma unroll
+      for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[n][r] = oacc[n][r] * half * half;
+    }
+  };
+
+  bool none = nt == 0, edge = false;  // of the current tile
+  f32x16 sa[2], sb[2];
+  // Iteration u: `cur` holds the scores of tile u, those of tile u + 1 (where there is
+  // none, of what the stage held before) go to `nxt`.
+  auto turn = [&](int u, auto stage_tag, f32x16 (&cur)[2], f32x16 (&nxt)[2])
+                  __attribute__((always_inline)) {
+    constexpr int ST = decltype(stage_tag)::value;  // u % kSt
+    wait_tile(min(1, nt - 2 - u));
+    barrier_no_fence();
+    if (u + kPD + 1 < nt) copies.load(wk, u + kPD + 1);
+    const bool none_next = u + 1 >= nt || wk.none(u + 1, 0);
+    const bool edge_next = !none_next && wk.template edge<BIAS>(u + 1, 0);
+    if (!none || !none_next) {
+      asm volatile("" : "+v"(wk.m_ref));  // keep the exponent arguments here
+      const float m_use = !CAP && wk.m_ref == -INFINITY ? 0.f : wk.m_ref;
+      const float slp = BIAS ? slope_of(u, edge) : 0.f;
+      float base[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        base[m] = CAP ? (edge && BIAS ? wk.cap2 : wk.cap2 - m_use) : -m_use;
+        if constexpr (BIAS) base[m] = fmaf(-slp, ahead_of(u, m), base[m]);
+      }
+      u32x4 pf[4];
+      // Block X: scores of tile u+1, exponentials of tile u, at raised issue
+      // priority: of the two waves of a SIMD, the one in this block keeps the
+      // matrix unit while the other is in block Y.
+      wave_priority<1>();
+      {
+        constexpr int NG = 2 * C::NS;
+        const unsigned char *Ks = smem + ((ST + 1) % kSt) * C::TILE_BYTES;
+        bf16x8 op[NG];
+        auto read = [&](int g) __attribute__((always_inline)) {
+          op[g] = *reinterpret_cast<const bf16x8 *>(Ks + off.k[g / 2] + (g % 2) * 32 * T::ROW_BYTES);
+        };
+#pragma unroll
+        for (int g = 0; g < kPf; ++g) read(g);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          if (g + kPf < NG) read(g + kPf);
+          const int m = g % 2, s2 = g / 2;
+          nxt[m] = mfma32x32x16(op[g], qf[s2], s2 == 0 ? f32x16{} : nxt[m]);
+#pragma unroll
+          for (int e = 32 * g / NG; e < 32 * (g + 1) / NG; ++e) {
+            const int mm = e / 16, r = e % 16, jo = 8 * (r >> 2) + (r & 3);
+            const float add = BIAS ? fmaf(slp, (float)jo, base[mm]) : base[mm];
+            if constexpr (CAP)
+              cur[mm][r] = fast_exp2(fmaf(cap_r(cur[mm][r], wk.c1), -2.f * wk.cap2, add));
+            else
+              cur[mm][r] = fast_exp2(fmaf(cur[mm][r], wk.c, add));
+            if (r % 8 == 7) pf[2 * mm + r / 8] = pack8(cur[mm], r - 7);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      wave_priority<0>();
+      if (CAP && edge) fix_weights(u, cur, pf);  // wave-uniform
+      if (!none) {
+        // Block Y: P V of tile u, its row sum.
+        float psum = 0.f;
+        constexpr int NG = C::NE * 4;
+        const unsigned char *Vs = smem + ST * C::TILE_BYTES;
+        bf16x8 op[NG];
+        auto read = [&](int g) __attribute__((always_inline)) {
+          const int n = g / 4, s2 = g % 4;
+          op[g] = tr_operand(Vs, off.v[n][0] + s2 * 16 * T::ROW_BYTES,
+                             off.v[n][1] + s2 * 16 * T::ROW_BYTES);
+        };
+#pragma unroll
+        for (int g = 0; g < kPf; ++g) read(g);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          if (g + kPf < NG) read(g + kPf);
+          const int n = g / 4, s2 = g % 4;
+          oacc[n] = mfma32x32x16(op[g], as_bf16x8(pf[s2]), oacc[n]);
+#pragma unroll
+          for (int e = 32 * g / NG; e < 32 * (g + 1) / NG; ++e) psum += cur[e / 16][e % 16];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        wk.l_run += psum;
+        if constexpr (!CAP) follow(psum);
+      }
+      if (!none_next) prepare(u + 1, edge_next, nxt);
+    }
+    none = none_next;
+    edge = edge_next;
+  };
+  if (nt > 0) {
+    wait_tile(min(kPD, nt - 1));
+    barrier_no_fence();
+    none = wk.none(0, 0);
+    edge = !none && wk.template edge<BIAS>(0, 0);
+    if (!none) {
+#pragma unroll
+      for (int s = 0; s < C::NS; ++s)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const bf16x8 x =
+              *reinterpret_cast<const bf16x8 *>(smem + off.k[s] + m * 32 * T::ROW_BYTES);
+          sa[m] = mfma32x32x16(x, qf[s], s == 0 ? f32x16{} : sa[m]);
+        }
+      prepare(0, edge, sa);
+    } else {
+#pragma unroll
+      for (int m = 0; m < 2; ++m) sa[m] = f32x16{};
+    }
+    for (int u = 0; u < nt; u += 4) {  // u % 4 == 0: every stage offset a constant
+      turn(u, std::integral_constant<int, 0>{}, sa, sb);
+      if (u + 1 < nt) turn(u + 1, std::integral_constant<int, 1>{}, sb, sa);
+      if (u + 2 < nt) turn(u + 2, std::integral_constant<int, 2>{}, sa, sb);
+      if (u + 3 < nt) turn(u + 3, std::integral_constant<int, 3>{}, sb, sa);
+    }
+  }
+  again_if_needed<C, D, CAP, BIAS>(wk, off, copies, qf, oacc, smem, 0);
+  leave<C, D>(wk, a, o, lse, pair_sum(wk.l_run), oacc);
 }
 
 // Row groups of a workgroup: fewer rows fill the GPU where there are few, more
-// let a K or V tile feed more products.
+// let a K or V tile feed more products.  The pipelined kernel takes the caps whose
+// reference stands still.
 int row_groups(const SpanArgs &a) {
   const long long rows = (long long)a.b * a.Hl * a.S;
-  return rows <= 32768 ? 2 : rows <= 65536 ? 4 : 8;
+  if (rows <= 32768) return 2;
+  return rows <= 65536 || a.cap > kSpanFixedCap ? 4 : 8;
 }
 
 }  // namespace
@@ -431,24 +709,24 @@ hipError_t launch_span_fwd(const SpanArgs &a, uint16_t *o, float *lse, hipStream
   const int qtiles = (a.S + 32 * R - 1) / (32 * R);
   const int heads_total = a.b * a.Hl;
   const long long blocks = (long long)qtiles * heads_total;
-  auto by_rule = [&](auto dim, auto groups, auto cap, auto bias) {
-    constexpr int D = decltype(dim)::value, RG = decltype(groups)::value;
-    hipLaunchKernelGGL((span_fwd_kernel<D, RG, decltype(cap)::value, decltype(bias)::value>),
-                       dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, o, lse, heads_total,
-                       qtiles);
-  };
-  auto by_groups = [&](auto dim, auto groups) {
-    using No = std::false_type;
-    using Yes = std::true_type;
-    if (a.cap > 0.f) a.slopes ? by_rule(dim, groups, Yes{}, Yes{}) : by_rule(dim, groups, Yes{}, No{});
-    else a.slopes ? by_rule(dim, groups, No{}, Yes{}) : by_rule(dim, groups, No{}, No{});
+  auto by_rule = [&](auto dim, auto cap, auto bias) {
+    constexpr int D = decltype(dim)::value;
+    constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, o, lse,
+                         heads_total, qtiles);
+    };
+    switch (R) {
+      case 2: go(span_fwd_split_kernel<D, 2, CAP, BIAS>); break;
+      case 4: go(span_fwd_split_kernel<D, 4, CAP, BIAS>); break;
+      default: go(span_fwd_kernel<D, CAP, BIAS>); break;
+    }
   };
   auto by_dim = [&](auto dim) {
-    switch (R) {
-      case 2: by_groups(dim, std::integral_constant<int, 2>{}); break;
-      case 4: by_groups(dim, std::integral_constant<int, 4>{}); break;
-      default: by_groups(dim, std::integral_constant<int, 8>{}); break;
-    }
+    using No = std::false_type;
+    using Yes = std::true_type;
+    if (a.cap > 0.f) a.slopes ? by_rule(dim, Yes{}, Yes{}) : by_rule(dim, Yes{}, No{});
+    else a.slopes ? by_rule(dim, No{}, Yes{}) : by_rule(dim, No{}, No{});
   };
   switch (a.d) {
     case 64: by_dim(std::integral_constant<int, 64>{}); break;

@@ -279,3 +279,48 @@ def test_attn_spans():
     assert basp.attn_spans(docs, pre).tolist() == [
         [[0, 2], [0, 2], [0, 3], [3, 5], [3, 5], [0, 0]], [[0, i + 1] for i in range(6)]]
     assert basp.attn_spans(docs).tolist()[0] == [[0, 1], [0, 2], [0, 3], [3, 4], [3, 5], [0, 0]]
+
+
+def test_scores_far_apart_in_wide_workgroups():
+    """Rows enough for 256 of them a workgroup: P outgrows the reference, within fp32's range and
+    past it, and falls below it."""
+    q, k, v, do = _inputs(1, 1500, 48, 2, 64, seed=16)
+    for span, kind, sign in ((40, "causal", 1), (40, "wild", -1), (250, "docs", 1), (250, "wild", 1),
+                             (250, "causal", -1)):
+        ramp = torch.linspace(-span, span, 1500, device="cuda")
+        k2 = (k.float() * 0.1 + sign * ramp.view(1, -1, 1, 1) / 8).to(BF16)
+        q2 = (q.float() * 0.1 + 1).to(BF16)
+        spans, slopes = _spans(kind, 1, 1500, 9), None if kind == "docs" else _slopes(48)
+        for cap in (None, 60.0):
+            print(f"case {span} {kind} {sign} {cap}", flush=True)
+            o, lse = basp.attn_span_fwd(q2, k2, v, spans, scale=1.0, cap=cap, slopes=slopes)
+            O, bo, L, bl = span_ref.fwd_ref(q2, k2, v, spans, 1.0, cap, slopes)
+            check("o", o, O, bo, BF16)
+            check("lse", lse, L, bl, F32)
+
+
+@pytest.mark.parametrize("cap", [None, 30.0, 100.0])
+@pytest.mark.parametrize("d", [80, 128])
+def test_unseen_values_in_wide_workgroups(cap, d):
+    """As test_unseen_values_do_not_count, with 256 rows a workgroup: to the forward's bound, since
+    the second pass over such a workgroup adds up in another order."""
+    b, S, n = 2, 900, 40
+    q, k, v, _ = _inputs(b, S, n, 4, d, seed=12)
+    docs = torch.zeros(b, S, dtype=torch.int32)
+    docs[:, 300:] = 1
+    docs[:, 411:] = 2
+    docs[1, 850:] = -1
+    spans = basp.attn_spans(docs.cuda(), torch.full((b, S), 100).cuda())
+    live = torch.ones(b, S, dtype=torch.bool, device="cuda")
+    live[:, 300:411] = False
+    live[1, 850:] = False
+    slopes = _slopes(n)
+    O, bound, L, bl = span_ref.fwd_ref(q, k, v, spans, 0.1, cap, slopes)
+    q2, k2, v2 = (torch.where(live[..., None, None], x, math.nan) for x in (q, k, v))
+    v2[0, 5, 0, 3] = math.inf     # seen by the first document
+    o, lse = basp.attn_span_fwd(q2, k2, v2, spans, scale=0.1, cap=cap, slopes=slopes)
+    assert not o[0, :300, :10, 3].isfinite().any()
+    o[0, :300, :10, 3] = O[0, :300, :10, 3].to(BF16)
+    check("o", o[live], O[live], bound[live], BF16)
+    check("lse", lse.transpose(1, 2)[live], L.transpose(1, 2)[live], bl.transpose(1, 2)[live], F32)
+    assert (o[1, 850:] == 0).all() and not o[:, 300:411].isfinite().any()
