@@ -5,8 +5,8 @@
 // (4 d operations a seen pair) and, with a cap, by the vector units, which form
 // three exponentials or reciprocals a score instead of one.
 //
-// gfx950 mapping, as the causal forward's: a workgroup of 8 waves owns 32 R
-// query rows of one head, R row groups times P = 8 / R key parts; S^T = K Q^T
+// gfx950 mapping, as the causal forward's: a workgroup owns 32 R query rows of one
+// head, its waves R row groups times P key parts; S^T = K Q^T
 // and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16, with Q in registers, P
 // straight from the score accumulator, and K and V copied HBM -> LDS into a
 // ring of stages.  A lane holds one row's scores of 16 keys per 32.
@@ -24,29 +24,30 @@
 namespace basp {
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWaves = 8;
+constexpr int kMaxWaves = 8;
 constexpr float kRescaleSlack = 8.f;  // log2 headroom before the reference max moves
 // A lane's sum of a tile's P past which the pipelined loop moves the reference.
 constexpr float kFollowSum = 65536.f;
 constexpr int kSchedMfma = 0x008;
 constexpr int kSchedDsRead = 0x100;
 
-template <int D, int RG>
+// WAVES waves: RG row groups of 32 query rows times WAVES / RG parts of KEYS keys each.
+template <int D, int WAVES, int RG, int KEYS>
 struct Cfg {
-  static constexpr int R = RG, P = kWaves / R;
+  static constexpr int R = RG, P = WAVES / R, THREADS = 64 * WAVES;
   static constexpr int DC = HeadDim<D>::DC;
   static constexpr int LW = HeadDim<D>::LW;
   static constexpr int BM = 32 * R;               // query rows per workgroup
-  static constexpr int KM = P == 1 ? 2 : 1;       // 32-key blocks per wave and tile
+  static constexpr int KM = KEYS / 32;            // 32-key blocks per wave and tile
   static constexpr int BN = 32 * KM * P;          // keys per tile
   static constexpr int TILE_BYTES = BN * LW * 2;
-  static constexpr int STAGES = 2 * TILE_BYTES > 32768 ? 2 : 4;
+  // 128 KB of ring for 8 waves, one workgroup a CU; 64 KB for 4, two of them.
+  static constexpr int STAGES = 16384 * WAVES >= 8 * TILE_BYTES ? 4 : 2;
   static constexpr int LDS_BYTES = STAGES * 2 * TILE_BYTES;
   static constexpr int NS = D / 16;               // 16-deep steps over the head dim
   static constexpr int NE = DC / 32;              // 32-wide head-dim subtiles of O
   static constexpr int CPR = LW / 8;              // 16-byte chunks per LDS row
-  static constexpr int DMA_PER_WAVE = BN * CPR / kThreads;
+  static constexpr int DMA_PER_WAVE = BN * CPR / THREADS;
   static constexpr int PART_BYTES = NE * 4 * 1024 + 512;
   static_assert((P - 1) * R * PART_BYTES <= LDS_BYTES, "the merge area fits the ring");
 };
@@ -155,7 +156,7 @@ struct Work {
 
 template <class C, int D, bool CAP, bool BIAS>
 __device__ __forceinline__ void enter(Work<C> &wk, bf16x8 (&qf)[C::NS], const SpanArgs &a,
-                                      int heads_total, int qtiles, int (&hulls)[2][kWaves]) {
+                                      int heads_total, int qtiles, int (&hulls)[2][kMaxWaves]) {
   const int S = a.S, Hl = a.Hl, lane = threadIdx.x & 63, hh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int L = blockIdx.x, qt = qtiles - 1 - L / heads_total, hb = L % heads_total;
@@ -308,15 +309,21 @@ struct Copies {
     }
     base = lds_addr_of(smem) + w * C::DMA_PER_WAVE * 1024;
   }
-  __device__ __forceinline__ void load(const Work<C> &wk, int u) const {
+  __device__ __forceinline__ void load_k(const Work<C> &wk, int u) const {
     const uint32_t ks = base + (u % C::STAGES) * C::TILE_BYTES;
     const uint32_t kb = (uint32_t)((wk.t0 + u) * C::BN) * wk.k_row_bytes;
+#pragma unroll
+    for (int i = 0; i < C::DMA_PER_WAVE; ++i) copy16_to_lds(wk.rk, kb + gk[i], ks + i * 1024);
+  }
+  __device__ __forceinline__ void load_v(const Work<C> &wk, int u) const {
+    const uint32_t vs = base + (C::STAGES + u % C::STAGES) * C::TILE_BYTES;
     const uint32_t vb = (uint32_t)((wk.t0 + u) * C::BN) * wk.v_row_bytes;
 #pragma unroll
-    for (int i = 0; i < C::DMA_PER_WAVE; ++i) {
-      copy16_to_lds(wk.rk, kb + gk[i], ks + i * 1024);
-      copy16_to_lds(wk.rv, vb + gv[i], ks + i * 1024 + C::STAGES * C::TILE_BYTES);
-    }
+    for (int i = 0; i < C::DMA_PER_WAVE; ++i) copy16_to_lds(wk.rv, vb + gv[i], vs + i * 1024);
+  }
+  __device__ __forceinline__ void load(const Work<C> &wk, int u) const {
+    load_k(wk, u);
+    load_v(wk, u);
   }
 };
 
@@ -422,14 +429,14 @@ __device__ __forceinline__ void again_if_needed(Work<C> &wk, const Offsets<C, D>
 
 // Workgroups of 64 or 128 rows, the keys of a tile shared by 4 or 2 waves.
 template <int D, int R, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kThreads, 1) void span_fwd_split_kernel(const SpanArgs a,
+__global__ __launch_bounds__(512, 1) void span_fwd_split_kernel(const SpanArgs a,
                                                                      uint16_t *__restrict__ o,
                                                                      float *__restrict__ lse,
                                                                      int heads_total, int qtiles) {
-  using C = Cfg<D, R>;
+  using C = Cfg<D, 8, R, 32>;
   // LDS: the K tiles of the ring stages, then their V tiles.
   __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
-  __shared__ int hulls[2][kWaves];
+  __shared__ int hulls[2][kMaxWaves];
   constexpr int kSt = C::STAGES;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rg = w % R, part = w / R;  // row group, key part
@@ -473,48 +480,53 @@ __global__ __launch_bounds__(kThreads, 1) void span_fwd_split_kernel(const SpanA
   leave<C, D>(wk, a, o, lse, l_tot, oacc);
 }
 
-// Workgroups of 256 rows, software-pipelined as the causal forward is: the score
-// products of tile u+1 are issued between the exponentials of tile u, and the row sum of
-// u between its P V products, one product per slot.
+// Workgroups of 128 rows, of 4 waves or of 8 that share the keys, software-pipelined as
+// the causal forward is: the score products of tile u+1 are issued between the
+// exponentials of tile u, and the row sum of u between its P V products, one product
+// per slot.
 // Without a cap a row's reference starts as the maximum of the first scores that it
 // sees, is checked against the maximum on edges, and on the other tiles follows the
 // row sums (half a row's sum is at least its maximum); where P passes fp32's range in
 // between, the workgroup is done again (above).
-template <int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kThreads, 1) void span_fwd_kernel(const SpanArgs a,
+template <int D, int WAVES, int R, bool CAP, bool BIAS>
+__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void span_fwd_kernel(const SpanArgs a,
                                                                uint16_t *__restrict__ o,
                                                                float *__restrict__ lse,
                                                                int heads_total, int qtiles) {
-  using C = Cfg<D, 8>;
+  using C = Cfg<D, WAVES, R, 64>;
   using T = LdsTile<C::LW>;
+  // Four stages: three tiles in flight.  Two (128 keys): K runs one tile ahead of V.
   constexpr int kSt = C::STAGES, kPD = 2, kPf = 2;
-  static_assert(kSt == 4 && C::KM == 2 && C::P == 1, "the unrolled loop's stages and tiles");
   __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
-  __shared__ int hulls[2][kWaves];
+  __shared__ int hulls[2][kMaxWaves];
   const int hh = (threadIdx.x & 63) >> 5;
   Work<C> wk;
   bf16x8 qf[C::NS];
   enter<C, D, CAP, BIAS>(wk, qf, a, heads_total, qtiles, hulls);
+  const int part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / R;
   const Copies<C, D> copies(wk, smem);
   const int nt = wk.nt;
-  for (int u = 0; u <= kPD && u < nt; ++u) copies.load(wk, u);
-  const Offsets<C, D> off(0);
+  if constexpr (kSt == 4) {
+    for (int u = 0; u <= kPD && u < nt; ++u) copies.load(wk, u);
+  } else if (nt > 0) {
+    copies.load(wk, 0);
+    if (nt > 1) copies.load_k(wk, 1);
+  }
+  const Offsets<C, D> off(part);
   f32x16 oacc[C::NE];
   clear<C::NE>(oacc);
   if (!CAP && wk.row >= a.S) wk.m_ref = 0.f;  // waits for no first key
 
-  // Tile u + 1 readable (tile u if u = -1 + 1 has no next), and tile u + kPD + 1 issued into
-  // the stage of tile u - 1, which every wave has finished with.
   auto wait_tile = [&](int ahead) __attribute__((always_inline)) {
     if (ahead >= 2) wait_vmcnt<4 * C::DMA_PER_WAVE>();
     else if (ahead == 1) wait_vmcnt<2 * C::DMA_PER_WAVE>();
     else wait_vmcnt<0>();
   };
   auto ahead_of = [&](int u, int m) __attribute__((always_inline)) {
-    return (float)(wk.row - ((wk.t0 + u) * C::BN + 32 * m + 4 * hh));
+    return (float)(wk.row - (wk.first_key(u, part) + 32 * m + 4 * hh));
   };
   auto slope_of = [&](int u, bool edge) __attribute__((always_inline)) {
-    return edge ? 0.f : (wk.t0 + u) * C::BN > wk.wrow0 ? -wk.sl : wk.sl;
+    return edge ? 0.f : wk.first_key(u, part) > wk.wrow0 ? -wk.sl : wk.sl;
   };
   // Tile u's scores are there: its edge, and the reference.
   auto prepare = [&](int u, bool edge, f32x16 (&sc)[2]) __attribute__((always_inline)) {
@@ -525,7 +537,7 @@ __global__ __launch_bounds__(kThreads, 1) void span_fwd_kernel(const SpanArgs a,
       float mx = -INFINITY;
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
-        if (edge) wk.template fix_scores<BIAS>(sc[m], (wk.t0 + u) * C::BN + 32 * m + 4 * hh);
+        if (edge) wk.template fix_scores<BIAS>(sc[m], wk.first_key(u, part) + 32 * m + 4 * hh);
         const float base = BIAS ? -slp * ahead_of(u, m) : 0.f;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
@@ -541,7 +553,7 @@ __global__ __launch_bounds__(kThreads, 1) void span_fwd_kernel(const SpanArgs a,
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const float ahead = ahead_of(u, m);
-      const int past = (wk.t0 + u) * C::BN + 32 * m + 4 * hh - wk.lo;
+      const int past = wk.first_key(u, part) + 32 * m + 4 * hh - wk.lo;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int jo = 8 * (r >> 2) + (r & 3);
@@ -582,11 +594,20 @@ __global__ __launch_bounds__(kThreads, 1) void span_fwd_kernel(const SpanArgs a,
   auto turn = [&](int u, auto stage_tag, f32x16 (&cur)[2], f32x16 (&nxt)[2])
                   __attribute__((always_inline)) {
     constexpr int ST = decltype(stage_tag)::value;  // u % kSt
-    wait_tile(min(1, nt - 2 - u));
-    barrier_no_fence();
-    if (u + kPD + 1 < nt) copies.load(wk, u + kPD + 1);
-    const bool none_next = u + 1 >= nt || wk.none(u + 1, 0);
-    const bool edge_next = !none_next && wk.template edge<BIAS>(u + 1, 0);
+    // K of tile u + 1 and V of tile u are there, and the copies after those in flight go
+    // into stages that every wave has finished with.
+    if constexpr (kSt == 4) {
+      wait_tile(min(1, nt - 2 - u));
+      barrier_no_fence();
+      if (u + kPD + 1 < nt) copies.load(wk, u + kPD + 1);
+    } else {
+      wait_vmcnt<0>();
+      barrier_no_fence();
+      if (u + 2 < nt) copies.load_k(wk, u + 2);
+      if (u + 1 < nt) copies.load_v(wk, u + 1);
+    }
+    const bool none_next = u + 1 >= nt || wk.none(u + 1, part);
+    const bool edge_next = !none_next && wk.template edge<BIAS>(u + 1, part);
     if (!none || !none_next) {
       asm volatile("" : "+v"(wk.m_ref));  // keep the exponent arguments here
       const float m_use = !CAP && wk.m_ref == -INFINITY ? 0.f : wk.m_ref;
@@ -664,10 +685,11 @@ __global__ __launch_bounds__(kThreads, 1) void span_fwd_kernel(const SpanArgs a,
     edge = edge_next;
   };
   if (nt > 0) {
-    wait_tile(min(kPD, nt - 1));
+    if constexpr (kSt == 4) wait_tile(min(kPD, nt - 1));
+    else wait_vmcnt<0>();
     barrier_no_fence();
-    none = wk.none(0, 0);
-    edge = !none && wk.template edge<BIAS>(0, 0);
+    none = wk.none(0, part);
+    edge = !none && wk.template edge<BIAS>(0, part);
     if (!none) {
 #pragma unroll
       for (int s = 0; s < C::NS; ++s)
@@ -682,44 +704,73 @@ __global__ __launch_bounds__(kThreads, 1) void span_fwd_kernel(const SpanArgs a,
 #pragma unroll
       for (int m = 0; m < 2; ++m) sa[m] = f32x16{};
     }
-    for (int u = 0; u < nt; u += 4) {  // u % 4 == 0: every stage offset a constant
-      turn(u, std::integral_constant<int, 0>{}, sa, sb);
-      if (u + 1 < nt) turn(u + 1, std::integral_constant<int, 1>{}, sb, sa);
-      if (u + 2 < nt) turn(u + 2, std::integral_constant<int, 2>{}, sa, sb);
-      if (u + 3 < nt) turn(u + 3, std::integral_constant<int, 3>{}, sb, sa);
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2 % kSt>;
+    using I3 = std::integral_constant<int, 3 % kSt>;
+    for (int u = 0; u < nt; u += kSt) {  // every stage offset a constant
+      turn(u, I0{}, sa, sb);
+      if (u + 1 < nt) turn(u + 1, I1{}, sb, sa);
+      if constexpr (kSt == 4) {
+        if (u + 2 < nt) turn(u + 2, I2{}, sa, sb);
+        if (u + 3 < nt) turn(u + 3, I3{}, sb, sa);
+      }
     }
   }
-  again_if_needed<C, D, CAP, BIAS>(wk, off, copies, qf, oacc, smem, 0);
-  leave<C, D>(wk, a, o, lse, pair_sum(wk.l_run), oacc);
+  again_if_needed<C, D, CAP, BIAS>(wk, off, copies, qf, oacc, smem, part);
+  float l_tot = pair_sum(wk.l_run);
+  if constexpr (C::P > 1) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (!merge_parts<C>(smem, w % R, part, threadIdx.x & 63, wk.m_ref, l_tot, oacc)) return;
+  }
+  leave<C, D>(wk, a, o, lse, l_tot, oacc);
 }
 
-// Row groups of a workgroup: fewer rows fill the GPU where there are few, more
-// let a K or V tile feed more products.  The pipelined kernel takes the caps whose
-// reference stands still.
-int row_groups(const SpanArgs &a) {
+// The workgroup of a call, by its query rows W = b Hl S: few rows need small ones
+// to fill the GPU, and many let a K or V tile feed more products.  Three kinds, us on
+// MI355X (8 heads on 2 of 128; one document | documents of S / 8 tokens | of 300):
+//   64 rows, 8 waves; 128 rows, 8 waves, pipelined; 128 rows, 4 waves, pipelined, two a CU
+//   W = 16K, S = 2048  29, 34, -    15, 18, -     15, 19, -
+//   32K, 4096          58, 61, 73   31, 29, 34    25, 22, 24
+//   46K, 6000          115, 91, 112 40, 39, 37    38, 36, 32
+//   64K, 8192          195, 149, 175  64, 53, 49  51, 40, 38
+//   96K, 48 x 256      62, 43, 29
+//   93K, 2 x 6000      227, 179, 153  98, 73, 66  70, 53, 39
+//   128K, 16384        717, 521, 483  393, 306, 354  91, 70, 55
+//   512K, 65536 on 1   9984, 7830, 7413  1685, 1286, 1253  364, 257, 178
+// (256 rows and 8 waves, one workgroup a CU, 493, 300 and 66 at W = 128K, lost to the
+// last kind wherever the others did.)  Caps past kSpanFixedCap take the tiles that follow the
+// running maximum, not pipelined, from 32K rows on in 128-row workgroups.
+enum class Kind { k64, k128, k128Narrow, k128Running };
+Kind kind_of(const SpanArgs &a) {
   const long long rows = (long long)a.b * a.Hl * a.S;
-  if (rows <= 32768) return 2;
-  return rows <= 65536 || a.cap > kSpanFixedCap ? 4 : 8;
+  if (rows <= 28672) return Kind::k64;
+  if (a.cap > kSpanFixedCap) return Kind::k128Running;
+  return rows <= 73728 && a.S > 512 ? Kind::k128 : Kind::k128Narrow;
 }
 
 }  // namespace
 
 hipError_t launch_span_fwd(const SpanArgs &a, uint16_t *o, float *lse, hipStream_t stream) {
-  const int R = row_groups(a);
-  const int qtiles = (a.S + 32 * R - 1) / (32 * R);
+  const Kind kind = kind_of(a);
+  const int rows = kind == Kind::k64 ? 64 : 128;
+  const int qtiles = (a.S + rows - 1) / rows;
   const int heads_total = a.b * a.Hl;
   const long long blocks = (long long)qtiles * heads_total;
   auto by_rule = [&](auto dim, auto cap, auto bias) {
     constexpr int D = decltype(dim)::value;
     constexpr bool CAP = decltype(cap)::value, BIAS = decltype(bias)::value;
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, a, o, lse,
+    auto go = [&](auto kernel, int threads) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, stream, a, o, lse,
                          heads_total, qtiles);
     };
-    switch (R) {
-      case 2: go(span_fwd_split_kernel<D, 2, CAP, BIAS>); break;
-      case 4: go(span_fwd_split_kernel<D, 4, CAP, BIAS>); break;
-      default: go(span_fwd_kernel<D, CAP, BIAS>); break;
+    switch (kind) {
+      case Kind::k64: go(span_fwd_split_kernel<D, 2, CAP, BIAS>, 512); break;
+      case Kind::k128: go(span_fwd_kernel<D, 8, 4, CAP, BIAS>, 512); break;
+      case Kind::k128Narrow: go(span_fwd_kernel<D, 4, 4, CAP, BIAS>, 256); break;
+      case Kind::k128Running:
+        if constexpr (CAP) go(span_fwd_split_kernel<D, 4, CAP, BIAS>, 512);
+        break;
     }
   };
   auto by_dim = [&](auto dim) {

@@ -282,7 +282,7 @@ def test_attn_spans():
 
 
 def test_scores_far_apart_in_wide_workgroups():
-    """Rows enough for 256 of them a workgroup: P outgrows the reference, within fp32's range and
+    """Rows enough for the wider workgroups: P outgrows the reference, within fp32's range and
     past it, and falls below it."""
     q, k, v, do = _inputs(1, 1500, 48, 2, 64, seed=16)
     for span, kind, sign in ((40, "causal", 1), (40, "wild", -1), (250, "docs", 1), (250, "wild", 1),
@@ -302,7 +302,7 @@ def test_scores_far_apart_in_wide_workgroups():
 @pytest.mark.parametrize("cap", [None, 30.0, 100.0])
 @pytest.mark.parametrize("d", [80, 128])
 def test_unseen_values_in_wide_workgroups(cap, d):
-    """As test_unseen_values_do_not_count, with 256 rows a workgroup: to the forward's bound, since
+    """As test_unseen_values_do_not_count, in the wider workgroups: to the forward's bound, since
     the second pass over such a workgroup adds up in another order."""
     b, S, n = 2, 900, 40
     q, k, v, _ = _inputs(b, S, n, 4, d, seed=12)
