@@ -301,31 +301,24 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
   };
   clear();
 
-  uint32_t gq[C::DMA_PER_WAVE], gd[C::DMA_PER_WAVE];
-#pragma unroll
-  for (int i = 0; i < C::DMA_PER_WAVE; ++i) {
-    gq[i] = dma_src_off<C::LW, D>((w * C::DMA_PER_WAVE + i) * 64 + lane, q_row_bytes);
-    gd[i] = dma_src_off<C::LW, D>((w * C::DMA_PER_WAVE + i) * 64 + lane, do_row_bytes);
-  }
-  int a_off[C::NS], b_off[kVRegs ? 1 : C::NS];
+  const CopySource<C::LW, D, C::DMA_PER_WAVE> src(w, lane);
+  // Rows of Q and dO; a row of the V tile lies as far from them as the wave's keys from
+  // its half.
+  int a_off[C::NS];
 #pragma unroll
   for (int s = 0; s < C::NS; ++s) {
     a_off[s] = T::off(32 * h + l32, 2 * s + hh);
     asm volatile("" : "+v"(a_off[s]));
-    if constexpr (!kVRegs) {
-      b_off[s] = kKvRegion + T::off(32 * kw + l32, 2 * s + hh);
-      asm volatile("" : "+v"(b_off[s]));
-    }
   }
-  int t_off[C::NE][2];
-#pragma unroll
-  for (int n = 0; n < C::NE; ++n)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      t_off[n][x] =
-          tr_piece_off<C::LW>(32 * h + 4 * hh + 8 * x, 32 * n + 16 * ((lane >> 4) & 1), lane);
-      asm volatile("" : "+v"(t_off[n][x]));
-    }
+  const int to_v = kKvRegion + 32 * (kw - h) * T::ROW_BYTES;
+  // Transposed rows 32h + 4hh (+ 16, and + 8 in the operand's second half) of columns
+  // 16((lane/16)%2): 32 n columns on, and 8 rows, the swizzle flips bits of the offset.
+  int t_base = tr_piece_off<C::LW>(32 * h + 4 * hh, 16 * ((lane >> 4) & 1), lane);
+  asm volatile("" : "+v"(t_base));
+  auto transposed = [&](const unsigned char *tile, int n, int s2) __attribute__((always_inline)) {
+    const int lo = t_base ^ (64 * n), hi = lo ^ 32, ro = s2 * 16 * T::ROW_BYTES;
+    return tr_operand(tile, lo + ro, hi + 8 * T::ROW_BYTES + ro);
+  };
   int aux_lane = kAuxRegion + 4 * 32 * h + 16 * hh;
   asm volatile("" : "+v"(aux_lane));
 
@@ -334,20 +327,14 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
 #pragma unroll
     for (int s = 0; s < C::NS; ++s) {
       asm volatile("" : "+v"(a_off[s]));
-      if constexpr (!kVRegs) asm volatile("" : "+v"(b_off[s]));
     }
-#pragma unroll
-    for (int n = 0; n < C::NE; ++n) {
-      asm volatile("" : "+v"(t_off[n][0]));
-      asm volatile("" : "+v"(t_off[n][1]));
-    }
+    asm volatile("" : "+v"(t_base));
     asm volatile("" : "+v"(aux_lane));
   };
 
   // Copies of step s of the head whose resources are at hand.  Wave 0 copies
   // the rows' -LSE and -D, wave 1 their spans: 512 bytes of either.
   u32x4 rq, rd, ra;
-  const uint32_t aux_lane_off = lane < 32 ? 16u * lane : kZeroOffset;
   float sl = 0.f;
   auto head_resources = [&](int hq) __attribute__((always_inline)) {
     rq = make_rsrc_words(a.s.q.p + ((size_t)beta * S + r_lo) * a.s.q.row_elems + (size_t)hq * D,
@@ -367,11 +354,11 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
 #pragma unroll
     for (int i = 0; i < C::DMA_PER_WAVE; ++i) {
       const uint32_t lds = stage + (w * C::DMA_PER_WAVE + i) * 1024;
-      copy16_to_lds(rq, gq[i] + qb, lds);
-      copy16_to_lds(rd, gd[i] + db, lds + kDoRegion);
+      copy16_to_lds(rq, src.off(i, q_row_bytes) + qb, lds);
+      copy16_to_lds(rd, src.off(i, do_row_bytes) + db, lds + kDoRegion);
     }
     if (w < 2)
-      copy16_to_lds(ra, aux_lane_off + s * kQM * 8,
+      copy16_to_lds(ra, (lane < 32 ? 16u * lane : kZeroOffset) + s * kQM * 8,
                            smem_lds + kAuxRegion + sq * C::AUX_BYTES + 1024 * w);
   };
   auto aux_rows = [&](int stg, int which) __attribute__((always_inline)) {
@@ -407,7 +394,7 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
         const bf16x8 ad = *reinterpret_cast<const bf16x8 *>(dOs + a_off[s]);
         bf16x8 bv;
         if constexpr (kVRegs) bv = vf[s];
-        else bv = *reinterpret_cast<const bf16x8 *>(smem + b_off[s]);
+        else bv = *reinterpret_cast<const bf16x8 *>(smem + (a_off[s] + to_v));
         sacc = mfma32x32x16(aq, kf[s], s == 0 ? neglse : sacc);
         pacc = mfma32x32x16(ad, bv, s == 0 ? negd : pacc);
       }
@@ -462,11 +449,10 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
     for (int n = 0; n < C::NE; ++n)
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
-        const int ro = s2 * 16 * T::ROW_BYTES;
-        bf16x8 av = tr_operand(dOs, t_off[n][0] + ro, t_off[n][1] + ro);
+        bf16x8 av = transposed(dOs, n, s2);
         if constexpr (CAREFUL) av = finite_operand(av, seen[s2], accv[n]);
         accv[n] = mfma32x32x16(av, bp[s2], accv[n]);
-        bf16x8 ak = tr_operand(Qs, t_off[n][0] + ro, t_off[n][1] + ro);
+        bf16x8 ak = transposed(Qs, n, s2);
         if constexpr (CAREFUL) ak = finite_operand(ak, seen[s2], acck[n]);
         acck[n] = mfma32x32x16(ak, bds[s2], acck[n]);
       }
@@ -755,11 +741,10 @@ __device__ __forceinline__ void dq_tile(const BwdArgs &a, int L, unsigned char *
       float base = BIAS ? fmaf(-slp, ahead, nlse) : nlse;
       constexpr uint32_t kOnes = 0x3F803F80u;
       u32x4 seen[2] = {{kOnes, kOnes, kOnes, kOnes}, {kOnes, kOnes, kOnes, kOnes}};
-      f32x16 add;  // with a cap
-      if constexpr (CAP) {
+      f32x16 add;  // with a cap and a bias
+      if constexpr (CAP && BIAS) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          add[r] = (BIAS ? fmaf(slp, (float)(8 * (r >> 2) + (r & 3)), base) : base) + cap2;
+        for (int r = 0; r < 16; ++r) add[r] = fmaf(slp, (float)(8 * (r >> 2) + (r & 3)), base) + cap2;
       }
       if (edge) {  // wave-uniform; as in the key pass
         asm volatile("" ::: "memory");
@@ -771,11 +756,13 @@ __device__ __forceinline__ void dq_tile(const BwdArgs &a, int L, unsigned char *
           const int jo = 8 * (r >> 2) + (r & 3);
           const bool vis = (uint32_t)(past + jo) < (uint32_t)(hi - lo);
           const float dist = BIAS ? fabsf(ahead - (float)jo) : 0.f;
-          if constexpr (CAP) {
+          if constexpr (CAP && BIAS) {
             add[r] = vis ? fmaf(-sl, dist, nlse + cap2) : -INFINITY;
             sacc[r] = vis ? sacc[r] : 0.f;
-          } else {
+          } else if constexpr (BIAS) {
             sacc[r] = vis ? fmaf(-sl * rc, dist, sacc[r]) : -INFINITY;
+          } else {  // with a cap P is at most 1 there: no LSE is below -cap
+            sacc[r] = vis ? sacc[r] : -INFINITY;
           }
           pacc[r] = vis ? pacc[r] : 0.f;
           if (CAREFUL && !vis) seen[r / 8][r % 8 / 2] &= r % 2 ? 0xFFFFu : 0xFFFF0000u;
@@ -786,7 +773,7 @@ __device__ __forceinline__ void dq_tile(const BwdArgs &a, int L, unsigned char *
       for (int r = 0; r < 16; ++r) {
         if constexpr (CAP) {
           const float rr = cap_r(sacc[r], c1);
-          const float p = fast_exp2(fmaf(rr, -2.f * cap2, add[r]));
+          const float p = fast_exp2(fmaf(rr, -2.f * cap2, BIAS ? add[r] : base + cap2));
           pacc[r] = p * pacc[r] * fmaf(-rr, rr, rr);
         } else {
           const int jo = 8 * (r >> 2) + (r & 3);
@@ -951,6 +938,19 @@ SpanCut span_cut(const SpanArgs &s) {
   return c;
 }
 
+// Row groups of the dQ pass: the causal backward's rule, but with spans 128 rows a
+// workgroup up to 256K query rows: documents make workgroups of very different
+// lengths, and twice as many of half the length even out better (16K tokens of packed
+// documents, 8 heads on 2 of 128: FIG).
+int row_groups(const SpanArgs &s) {
+  const int R = dq_row_groups(shape_of(s, (size_t)-1));
+  return R == 8 && s.spans && (long long)s.b * s.Hl * s.S <= 262144 ? 4 : R;
+}
+long long dq_blocks_of(const SpanArgs &s) {
+  const int rows = 32 * row_groups(s);
+  return (long long)((s.S + rows - 1) / rows) * s.b * s.Hl;
+}
+
 // Workgroups of the key pass: (key tile, row chunk) pairs with rows at or after the
 // keys first, then, with spans, those of rows before the keys.
 long long key_blocks(const SpanArgs &s, const SpanCut &ck) {
@@ -964,7 +964,7 @@ long long key_blocks(const SpanArgs &s, const SpanCut &ck) {
 size_t span_bwd_workspace_bytes(const SpanArgs &s) { return span_cut(s).bytes; }
 
 bool span_bwd_fits(const SpanArgs &s) {
-  return (bwd_dq_blocks(shape_of(s, (size_t)-1)) + key_blocks(s, span_cut(s))) * kThreads <=
+  return (dq_blocks_of(s) + key_blocks(s, span_cut(s))) * kThreads <=
          0xFFFFFFFFll;
 }
 
@@ -994,9 +994,8 @@ hipError_t launch_span_bwd(const SpanArgs &s, const uint16_t *o, const float *ls
   }
   const int T128 = ck.chunk_rows / kKN;
   a.causal_units = (uint32_t)kv_units(ck.nchunks, T128);
-  const AttnShape shape = shape_of(s, (size_t)-1);
-  const int R = dq_row_groups(shape);
-  a.dq_blocks = (uint32_t)bwd_dq_blocks(shape);
+  const int R = row_groups(s);
+  a.dq_blocks = (uint32_t)dq_blocks_of(s);
   const uint32_t kv_blocks = (uint32_t)key_blocks(s, ck);
   {
     const int n_rep = s.Hl / s.Hkl;

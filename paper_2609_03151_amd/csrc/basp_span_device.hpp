@@ -18,6 +18,31 @@ __device__ __forceinline__ void copy16_to_lds(u32x4 rsrc, uint32_t off, uint32_t
                : "memory");
 }
 
+// Where the 16 bytes come from that a lane copies into an LdsTile<LW> of D-element rows
+// by the i-th of N copies of its wave (dma_src_off of chunk slot (N wave + i) 64 + lane):
+// each copy is 64 / (LW / 8) rows further on, where the swizzle flips one bit of the
+// chunk's number.  Formed anew for each copy from two registers: offsets kept for
+// both tensors take up to 16, and one register too many sends a loop's values to
+// scratch memory, whose loads wait for every copy in flight.
+template <int LW, int D, int N>
+struct CopySource {
+  static constexpr int CPR = LW / 8, ROWS = 64 / CPR, FLIP = LW == 128 ? 1 : 2;
+  static_assert(N <= (LW == 128 ? 4 : 2), "the flips are those of the swizzle");
+  uint32_t row, col;
+  __device__ __forceinline__ CopySource(int wave, int lane) {
+    const int pos = wave * N * 64 + lane;
+    row = pos / CPR;
+    col = ((pos % CPR) ^ LdsTile<LW>::swz(pos / CPR)) << 4;
+  }
+  __device__ __forceinline__ uint32_t off(int i, uint32_t row_bytes) const {
+    uint32_t r = row, c = col;
+    asm volatile("" : "+v"(r), "+v"(c));  // not kept over the loop
+    c ^= (uint32_t)(FLIP * i) << 4;
+    const uint32_t x = __umul24(r + ROWS * i, row_bytes) + c;
+    return D < LW && c >= D * 2 ? kZeroOffset : x;
+  }
+};
+
 // lo and hi of a row, inside [0, S]; empty spans as lo = hi = 0.
 __device__ __forceinline__ void span_of(const int *spans, size_t beta, int S, int row, int &lo,
                                         int &hi) {
