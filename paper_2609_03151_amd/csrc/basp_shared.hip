@@ -8,11 +8,12 @@
 // values, each read once, up to some 200 rows a kv head, by the matrix cores (and
 // with a cap the vector units) past that.
 //
-//   shared_plan   which sequences share, and where their rows go
-//   shared_main   prefix workgroups: 64 rows of a group and kv head times a split of
-//                 the prefix's keys, as the causal forward's (S^T = K Q^T, O^T = V^T P^T
-//                 on v_mfma_f32_32x32x16_bf16, two row groups times two key parts, K and
-//                 V through LDS, widened to bf16 on the way from 8 bits).
+//   shared_plan   which sequences share, and where their rows go (many sequences; else each
+//                 workgroup of the next kernel finds out by itself)
+//   shared_main   prefix workgroups: 64 or 128 rows of a group and kv head times a
+//                 split of the prefix's keys, as the causal forward's (S^T = K Q^T, O^T =
+//                 V^T P^T on v_mfma_f32_32x32x16_bf16, K and V through LDS, widened to bf16
+//                 on the way from 8 bits).
 //                 Own workgroups: every sequence's other keys, dealt out evenly over
 //                 the workgroups as basp_decode.hip does.
 //   shared_join   a row's partial results of both kinds, by their maxima and sums
@@ -36,11 +37,13 @@ constexpr int kPlanThreads = 1024;
 struct Plan {
   int *total;    // chunks there are
   int *start;    // [b] a sequence's first own key: its group's prefix length, or 0
-  int *row;      // [b] its first prefix row, in chunks of kSharedRows; -1: it shares nothing
+  int *row;      // [b] its first prefix row, in chunks of SharedCut.rows; -1: it shares nothing
   int *member;   // [b] sequences that share, group by group, from its first sequence on
   int *units;    // [b + 1] units of the sequences before, times their heads
   int *group_n, *group_chunk;  // [n_groups]
-  int4 *chunk;   // first member's place, members, prefix length, row of the first
+  // Of a chunk of rows: its group's first place in `member` and the members' number, the
+  // prefix's length, the chunk's first row in the group; then the first member.
+  int4 *chunk;
 };
 __device__ __forceinline__ Plan plan_at(const SharedArgs &a, const SharedCut &c) {
   char *ws = static_cast<char *>(a.d.workspace);
@@ -116,7 +119,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
   for (int g0 = 0; g0 < a.n_groups; g0 += kPlanThreads) {
     const int g = g0 + tid;
     const long long rows = g < a.n_groups ? (long long)p.group_n[g] * rep : 0;
-    const int mine = (int)((rows + kSharedRows - 1) / kSharedRows);
+    const int mine = (int)((rows + c.rows - 1) / c.rows);
     int total;
     const int at = chunks + before(mine, sums, total);
     if (g < a.n_groups) {
@@ -138,10 +141,13 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
     for (int i = lane; i < n; i += 64) {
       const int s = p.member[g0 + i];
       p.start[s] = prefix;
-      p.row[s] = at * kSharedRows + i * rep;
+      p.row[s] = at * c.rows + i * rep;
     }
-    const int mine = (int)(((long long)n * rep + kSharedRows - 1) / kSharedRows);
-    for (int i = lane; i < mine; i += 64) p.chunk[at + i] = int4{g0, n, prefix, i * kSharedRows};
+    const int mine = (int)(((long long)n * rep + c.rows - 1) / c.rows);
+    for (int i = lane; i < mine; i += 64) {
+      p.chunk[2 * (at + i)] = int4{g0, n, prefix, i * c.rows};
+      p.chunk[2 * (at + i) + 1] = int4{p.member[g0], 0, 0, 0};
+    }
   }
   __syncthreads();
   int units = 0;
@@ -156,10 +162,133 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedA
   if (tid == 0) p.units[b] = units;
 }
 
+// What a main workgroup goes by: the plan in the workspace, or its own in LDS.
+struct View {
+  const int *start, *member, *units;
+  int4 rec;  // of its chunk
+  int lead;
+  bool chunk;  // there is one
+};
+struct Local {
+  int start[kLocalSeqs], member[kLocalSeqs], units[kLocalSeqs + 1];
+  int g0[kLocalGroups], g1[kLocalGroups], prefix[kLocalGroups], n[kLocalGroups];
+  int first[kLocalGroups], chunk0[kLocalGroups];
+  int sums[2][kWaves], rec[4];
+};
+
+// The plan of one workgroup (a launch of its own costs 4.5 us and its round trips
+// through memory).  `chunk` < 0: an own workgroup, number g of G, which also leaves its
+// share of the sequences' prefix rows for the join.
+__device__ __forceinline__ View plan_here(const SharedArgs &a, const SharedCut &c, Local &p,
+                                          int chunk, int g, int G) {
+  const int b = a.d.s.b, rep = a.d.n_q / a.d.s.n_k, n_groups = a.n_groups;
+  const int tid = threadIdx.x, lane = tid % 64, wave = scalar(tid / 64);
+  constexpr int kTurns = kLocalSeqs / kThreads;
+  int len[kTurns];
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) {
+    const int s = tid + k * kThreads;
+    len[k] = s < b ? a.d.lens[s] : 0;
+  }
+  if (tid < n_groups) {
+    const int g0 = clamp(a.groups[tid], 0, b);
+    p.g0[tid] = g0;
+    p.g1[tid] = clamp(a.groups[tid + 1], g0, b);
+    p.prefix[tid] = a.prefix_lens[tid];
+    p.n[tid] = 0;
+  }
+  if (tid == 0) p.rec[1] = 0;
+  __syncthreads();
+  int of[kTurns];  // a sequence's group, if it is as long as its prefix
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) {
+    const int s = tid + k * kThreads;
+    of[k] = -1;
+    if (s < b && n_groups > 0) {
+      int lo = 0, hi = n_groups;  // the last group that starts at s or before
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (p.g0[mid] <= s) lo = mid;
+        else hi = mid;
+      }
+      if (s >= p.g0[lo] && s < p.g1[lo] && p.prefix[lo] > 0 && len[k] >= p.prefix[lo] &&
+          len[k] <= a.d.max_len) {
+        of[k] = lo;
+        atomicAdd(&p.n[lo], 1);
+      }
+    }
+  }
+  __syncthreads();
+  // Sums over the threads before this one, and of all, of two numbers.
+  auto before = [&](int x, int y, int &tx, int &ty, int &ax, int &ay) {
+    const int ix = wave_scan(x), iy = wave_scan(y);
+    __syncthreads();  // sums of the turn before are read
+    if (lane == 63) p.sums[0][wave] = ix, p.sums[1][wave] = iy;
+    __syncthreads();
+    tx = ix - x, ty = iy - y, ax = ay = 0;
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) tx += p.sums[0][w], ty += p.sums[1][w];
+      ax += p.sums[0][w], ay += p.sums[1][w];
+    }
+  };
+  int all_first, all_chunks;
+  {
+    const int n = tid < n_groups && p.n[tid] >= 2 ? p.n[tid] : 0;
+    const int mine = (n * rep + c.rows - 1) / c.rows;
+    int first, chunk0;
+    before(n, mine, first, chunk0, all_first, all_chunks);
+    if (tid < n_groups) p.first[tid] = first, p.chunk0[tid] = chunk0;
+    if (mine > 0 && chunk >= chunk0 && chunk < chunk0 + mine) {
+      p.rec[0] = first, p.rec[1] = n, p.rec[2] = p.prefix[tid];
+      p.rec[3] = (chunk - chunk0) * c.rows;
+    }
+  }
+  int members = 0, units = 0;
+  for (int k = 0; k * kThreads < b; ++k) {
+    const int s = tid + k * kThreads;
+    const int gr = s < b ? of[k] : -1, n = gr >= 0 ? p.n[gr] : 0;
+    const bool in = n >= 2;
+    const int start = in ? p.prefix[gr] : 0;
+    int at, u, am, au;
+    before(in, s < b ? units_of(len[k], start, a.d.max_len) * c.vheads : 0, at, u, am, au);
+    at += members, u += units;
+    members += am, units += au;
+    if (s < b) {
+      p.start[s] = start;
+      p.units[s] = u;
+      if (in) p.member[at] = s;
+      if (chunk < 0 && s % G == g) {
+        const int rank = in ? clamp(at - p.first[gr], 0, n - 1) : 0;
+        plan_at(a, c).row[s] = in ? p.chunk0[gr] * c.rows + rank * rep : -1;
+      }
+    }
+  }
+  if (tid == 0) p.units[b] = units;
+  __syncthreads();
+  View v{p.start, p.member, p.units, int4{p.rec[0], p.rec[1], p.rec[2], p.rec[3]}, 0, false};
+  v.chunk = chunk >= 0 && v.rec.y > 0;
+  v.lead = v.chunk ? p.member[v.rec.x] : 0;
+  return v;
+}
+
+// The plan kernel's, for one workgroup.
+__device__ __forceinline__ View plan_there(const SharedArgs &a, const SharedCut &c, int chunk) {
+  const Plan p = plan_at(a, c);
+  View v{p.start, p.member, p.units, int4{0, 0, 0, 0}, 0, false};
+  if (chunk >= 0 && chunk < *p.total) {
+    v.rec = p.chunk[2 * chunk];
+    v.lead = p.chunk[2 * chunk + 1].x;
+    v.chunk = true;
+  }
+  return v;
+}
+
 // ------------------------------------------------------------- prefix pass
-template <int D>
+// 64 rows: two row groups of 32 times two key parts of a tile; 128: four row groups.
+template <int D, int RG>
 struct PrefixCfg {
-  static constexpr int R = 2, P = 2;  // row groups, key parts
+  static constexpr int R = RG, P = kWaves / R;  // row groups, key parts
+  static constexpr int KM = kSharedTile / 32 / P;  // 32-key blocks per wave and tile
   static constexpr int DC = HeadDim<D>::DC;
   static constexpr int LW = HeadDim<D>::LW;
   static constexpr int TILE_BYTES = kSharedTile * LW * 2;
@@ -167,28 +296,31 @@ struct PrefixCfg {
   static constexpr int NS = D / 16;
   static constexpr int NE = DC / 32;
   static constexpr int PART_BYTES = NE * 4 * 1024 + 512;
-  static_assert(R * PART_BYTES <= LDS_BYTES, "the merge area fits the stages");
+  static_assert((P - 1) * R * PART_BYTES <= LDS_BYTES, "the merge area fits the stages");
 };
 
-// Chunks of 16 bytes of a tile's rows that a thread carries from the pages to LDS.
+// What a thread carries from the pages to LDS: 16 bytes of one row in each of N blocks
+// of 16 keys (a tile has four; a block lies in one page, so its address is a scalar).
+// Where a row is short, two or all of the blocks are carried at once, by other waves.
 template <int D, bool E4M3>
 struct Carry {
-  static constexpr int kPerRow = D * (E4M3 ? 1 : 2) / 16;
-  static constexpr int kChunks = kSharedTile * kPerRow;
-  static constexpr int N = (kChunks + kThreads - 1) / kThreads;
+  static constexpr int kRowBytes = D * (E4M3 ? 1 : 2), kPerRow = kRowBytes / 16;
+  static constexpr int kAtOnce = kPerRow <= 4 ? 4 : kPerRow <= 8 ? 2 : 1;
+  static constexpr int kPerBlock = kThreads / kAtOnce;  // threads
+  static constexpr int N = kSharedTile / 16 / kAtOnce;
   u32x4 k[N], v[N];
-  float ks[N], vs[N];
-  int id[N];  // page numbers of the next tile
-  bool bad[N];
+  uint32_t ks[N], vs[N];  // scale bytes
+  int id[N];              // page numbers of the next tile (wave-uniform)
+  bool bad[N];            // this tile's block lies on no valid page (wave-uniform)
 };
 
-template <int D, bool E4M3>
-__device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned char *smem) {
-  using C = PrefixCfg<D>;
+template <int D, bool E4M3, int RG>
+__device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned char *smem,
+                            Local &local) {
+  using C = PrefixCfg<D, RG>;
   using T = LdsTile<C::LW>;
   using W = Carry<D, E4M3>;
   constexpr int kVRegion = 2 * C::TILE_BYTES;
-  const Plan plan = plan_at(a, c);
   const CacheShape &cs = a.d.s;
   const int rep = a.d.n_q / cs.n_k;
   // Splits fastest, in eights where there are as many: workgroups go round the eight
@@ -196,12 +328,14 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
   const int x = blockIdx.x;
   const int split = scalar(x % c.splits), rest = scalar(x / c.splits);
   const int chunk = scalar(rest / cs.n_k), kvh = scalar(rest % cs.n_k);
-  if (chunk >= *plan.total) return;  // workgroup-uniform
-  const int4 rec = plan.chunk[chunk];
+  const View plan =
+      c.local ? plan_here(a, c, local, chunk, 0, 1) : plan_there(a, c, chunk);  // uniform
+  if (!plan.chunk) return;  // workgroup-uniform
+  const int4 rec = plan.rec;
+  const int lead = scalar(plan.lead);
   const int first = scalar(rec.x), members = scalar(rec.y), prefix = scalar(rec.z),
             row0 = scalar(rec.w);
   const int rows = members * rep - row0;  // of this chunk (and those after it)
-  const int lead = scalar(plan.member[first]);
   const int *table = a.d.table + (size_t)lead * cs.max_pages;
   const int tiles = (prefix + kSharedTile - 1) / kSharedTile;
   const int t0 = (int)((long long)split * tiles / c.splits);
@@ -241,66 +375,72 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
     for (int r = 0; r < 16; ++r) oacc[n][r] = 0.f;
 
   W x_;
-  auto load_pages = [&](int t) {
+  const int block = scalar(tid / W::kPerBlock);  // of those at once
+  const int mine = tid % W::kPerBlock, row = mine / W::kPerRow, cc = mine % W::kPerRow;
+  const bool carries = mine < 16 * W::kPerRow;
+  auto first_key = [&](int t, int j) { return t * kSharedTile + 16 * (W::kAtOnce * j + block); };
+  auto load_pages = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < W::N; ++j) {
-      const int ch = tid + kThreads * j, key0 = t * kSharedTile + ch / W::kPerRow;
-      const int key = key0 < prefix ? key0 : prefix - 1, pi = key >> cs.page_log2;
-      x_.id[j] = ch < W::kChunks && t < t1 && pi < cs.max_pages ? table[pi] : -1;
+      const int pi = first_key(t, j) >> cs.page_log2;
+      x_.id[j] = t < t1 && first_key(t, j) < prefix && pi < cs.max_pages ? scalar_load(table, pi) : -1;
     }
   };
-  auto load_rows = [&](int t) {  // of the pages at hand
+  auto load_rows = [&](int t) __attribute__((always_inline)) {  // of the pages at hand
 #pragma unroll
     for (int j = 0; j < W::N; ++j) {
-      const int ch = tid + kThreads * j, key0 = t * kSharedTile + ch / W::kPerRow;
-      if (ch >= W::kChunks) continue;
-      const int key = key0 < prefix ? key0 : prefix - 1;  // past the end: the last one again
-      const bool there = x_.id[j] >= 0 && x_.id[j] < cs.n_pages;
-      const size_t row = there ? (((size_t)x_.id[j] * cs.n_k + kvh) << cs.page_log2) +
-                                     (key & ((1 << cs.page_log2) - 1))
-                               : 0;
-      const size_t off = row * (D * (E4M3 ? 1 : 2)) + ch % W::kPerRow * 16;
-      x_.k[j] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.d.k_pages) + off);
-      x_.v[j] = *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.d.v_pages) + off);
-      if constexpr (E4M3) {
-        x_.ks[j] = __builtin_bit_cast(float, (uint32_t)a.d.k_scales[row] << 23);
-        x_.vs[j] = __builtin_bit_cast(float, (uint32_t)a.d.v_scales[row] << 23);
+      const int key = first_key(t, j), id = scalar(x_.id[j]);
+      const bool there = id >= 0 && id < cs.n_pages;
+      const size_t at = there ? (((size_t)id * cs.n_k + kvh) << cs.page_log2) +
+                                    (key & ((1 << cs.page_log2) - 1))
+                              : 0;
+      // keys past the end: the last row again, or (a whole block) any
+      const int last = there ? prefix - key - 1 : 0;
+      const uint32_t r = (uint32_t)(row < last ? row : last);
+      const uint32_t off = r * W::kRowBytes + cc * 16;
+      const gptr kb = scalar_base(static_cast<const char *>(a.d.k_pages) + at * W::kRowBytes);
+      const gptr vb = scalar_base(static_cast<const char *>(a.d.v_pages) + at * W::kRowBytes);
+      if (carries) {
+        x_.k[j] = load_at<u32x4>(kb, off);
+        x_.v[j] = load_at<u32x4>(vb, off);
+        if constexpr (E4M3) {
+          x_.ks[j] = load_at<uint8_t>(scalar_base(a.d.k_scales + at), r);
+          x_.vs[j] = load_at<uint8_t>(scalar_base(a.d.v_scales + at), r);
+        }
       }
-      x_.bad[j] = !there;
+      x_.bad[j] = !there && key < prefix;
     }
   };
-  auto widen8 = [&](uint32_t lo, uint32_t hi, float scale) {
-    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
+  auto widen8 = [&](uint32_t lo, uint32_t hi, uint32_t byte) __attribute__((always_inline)) {
+    const float scale = __builtin_bit_cast(float, byte << 23);
+    return u32x4{
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
   };
-  auto put = [&](int stage) {  // into LDS
+  const int to0 = T::off(row + 16 * block, E4M3 ? 2 * cc : cc);
+  const int to1 = E4M3 ? T::off(row + 16 * block, 2 * cc + 1) : 0;
+  auto put = [&](int stage) __attribute__((always_inline)) {  // into LDS
+    if (!carries) return;
     unsigned char *Ks = smem + stage * C::TILE_BYTES;
 #pragma unroll
     for (int j = 0; j < W::N; ++j) {
-      const int ch = tid + kThreads * j, r = ch / W::kPerRow, cc = ch % W::kPerRow;
-      if (ch >= W::kChunks) continue;
-      constexpr uint32_t kNan = 0x7FFF7FFFu;
+      const int at = j * 16 * W::kAtOnce * T::ROW_BYTES;
+      u32x4 k0 = x_.k[j], v0 = x_.v[j];
       if constexpr (E4M3) {
-        u32x4 k0 = widen8(x_.k[j].x, x_.k[j].y, x_.ks[j]), k1 = widen8(x_.k[j].z, x_.k[j].w, x_.ks[j]);
-        if (x_.bad[j]) k0 = u32x4{kNan, kNan, kNan, kNan};
-        *reinterpret_cast<u32x4 *>(Ks + T::off(r, 2 * cc)) = k0;
-        *reinterpret_cast<u32x4 *>(Ks + T::off(r, 2 * cc + 1)) = k1;
-        *reinterpret_cast<u32x4 *>(Ks + kVRegion + T::off(r, 2 * cc)) =
-            widen8(x_.v[j].x, x_.v[j].y, x_.vs[j]);
-        *reinterpret_cast<u32x4 *>(Ks + kVRegion + T::off(r, 2 * cc + 1)) =
-            widen8(x_.v[j].z, x_.v[j].w, x_.vs[j]);
-      } else {
-        u32x4 k0 = x_.k[j];
-        if (x_.bad[j]) k0 = u32x4{kNan, kNan, kNan, kNan};
-        *reinterpret_cast<u32x4 *>(Ks + T::off(r, cc)) = k0;
-        *reinterpret_cast<u32x4 *>(Ks + kVRegion + T::off(r, cc)) = x_.v[j];
+        *reinterpret_cast<u32x4 *>(Ks + to1 + at) = widen8(k0.z, k0.w, x_.ks[j]);
+        *reinterpret_cast<u32x4 *>(Ks + kVRegion + to1 + at) = widen8(v0.z, v0.w, x_.vs[j]);
+        k0 = widen8(k0.x, k0.y, x_.ks[j]);
+        v0 = widen8(v0.x, v0.y, x_.vs[j]);
       }
+      if (x_.bad[j]) k0 = u32x4{0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu};  // NaN
+      *reinterpret_cast<u32x4 *>(Ks + to0 + at) = k0;
+      *reinterpret_cast<u32x4 *>(Ks + kVRegion + to0 + at) = v0;
     }
   };
 
-  const int part_off = part * 32 * T::ROW_BYTES;
+  const int part_off = part * 32 * C::KM * T::ROW_BYTES;
   int k_off[C::NS], v_off[C::NE][2];
 #pragma unroll
   for (int s = 0; s < C::NS; ++s) k_off[s] = T::off(l32, 2 * s + hh) + part_off;
@@ -312,23 +452,29 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
                     tr_piece_off<C::LW>(4 * hh + 8 * y, 32 * n + 16 * ((lane >> 4) & 1), lane);
   auto tile = [&](int t, int stage) __attribute__((always_inline)) {
     const unsigned char *Ks = smem + stage * C::TILE_BYTES;
-    f32x16 sc;
 #pragma unroll
-    for (int s = 0; s < C::NS; ++s)
-      sc = mfma32x32x16(*reinterpret_cast<const bf16x8 *>(Ks + k_off[s]), qf[s],
-                        s == 0 ? f32x16{} : sc);
-    // sc[r] = (q . k) of key jl + 8(r/4) + r%4 for this lane's row
-    const int jl = t * kSharedTile + 32 * part + 4 * hh;
-    const float away = at - (float)jl;
-    if (capped) {
+    for (int m = 0; m < C::KM; ++m) {
+      const int mo = m * 32 * T::ROW_BYTES;
+      f32x16 sc;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = fmaf(cap_r(sc[r], c1), -2.f * cap2, cap2);
-    } else {
+      for (int s = 0; s < C::NS; ++s)
+        sc = mfma32x32x16(*reinterpret_cast<const bf16x8 *>(Ks + k_off[s] + mo), qf[s],
+                          s == 0 ? f32x16{} : sc);
+      // sc[r] = (q . k) of key jl + 8(r/4) + r%4 for this lane's row
+      const int jl = t * kSharedTile + 32 * (C::KM * part + m) + 4 * hh;
+      const float away = at - (float)jl;
+      if (capped) {  // workgroup-uniform, as the next
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] *= c2;
+        for (int r = 0; r < 16; ++r) sc[r] = fmaf(cap_r(sc[r], c1), -2.f * cap2, cap2);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] *= c2;
     }
+    if (a.slopes) {
+      const float base = -sl * away;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = fmaf(-sl, away - (float)(8 * (r >> 2) + (r & 3)), sc[r]);
+      for (int r = 0; r < 16; ++r) sc[r] += fmaf(sl, (float)(8 * (r >> 2) + (r & 3)), base);
+    }
     if (jl - 4 * hh + 32 > prefix) {  // wave-uniform: the last tile
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -371,63 +517,75 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
     for (int n = 0; n < C::NE; ++n)
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
-        const int ro = s2 * 16 * T::ROW_BYTES;
+        const int ro = mo + s2 * 16 * T::ROW_BYTES;
         oacc[n] = mfma32x32x16(tr_operand(Ks, v_off[n][0] + ro, v_off[n][1] + ro), pf[s2], oacc[n]);
       }
+    }
   };
   // One tile of rows and the next one's page numbers in flight over a tile's
   // products; two stages, so that one barrier a tile is enough.
+  __syncthreads();  // the plan in LDS has been read
   load_pages(t0);
   if (t0 < t1) load_rows(t0);
   load_pages(t0 + 1);
-  for (int t = t0; t < t1; ++t) {
-    put((t - t0) & 1);
+  auto turn = [&](int t, int stage) __attribute__((always_inline)) {
+    put(stage);
     if (t + 1 < t1) {
       load_rows(t + 1);
       load_pages(t + 2);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     barrier_no_fence();
-    tile(t, (t - t0) & 1);
+    tile(t, stage);
+  };
+  for (int t = t0; t < t1; t += 2) {
+    turn(t, 0);
+    if (t + 1 < t1) turn(t + 1, 1);
   }
 
-  // The two parts of a row group, and out.
-  float l_tot = pair_sum(l_run);
-  __syncthreads();
+  // The parts of a row group brought together, and out.
+  float l_tot = pair_sum(l_run), m = m_ref, w0 = 1.f, w1 = 0.f;
   unsigned char *area = smem + rg * C::PART_BYTES;
-  constexpr int kScalars = C::NE * 4 * 1024;
-  if (part == 1) {
+  if constexpr (C::P == 2) {
+    constexpr int kScalars = C::NE * 4 * 1024;
+    __syncthreads();
+    if (part == 1) {
 #pragma unroll
-    for (int n = 0; n < C::NE; ++n)
+      for (int n = 0; n < C::NE; ++n)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4 *>(area + (n * 4 + g) * 1024 + 16 * lane) =
-            f32x4{oacc[n][4 * g], oacc[n][4 * g + 1], oacc[n][4 * g + 2], oacc[n][4 * g + 3]};
-    *reinterpret_cast<float *>(area + kScalars + 4 * lane) = m_ref;
-    *reinterpret_cast<float *>(area + kScalars + 256 + 4 * lane) = l_tot;
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4 *>(area + (n * 4 + g) * 1024 + 16 * lane) =
+              f32x4{oacc[n][4 * g], oacc[n][4 * g + 1], oacc[n][4 * g + 2], oacc[n][4 * g + 3]};
+      *reinterpret_cast<float *>(area + kScalars + 4 * lane) = m_ref;
+      *reinterpret_cast<float *>(area + kScalars + 256 + 4 * lane) = l_tot;
+    }
+    __syncthreads();
+    if (part == 1) return;
+    const float m1 = *reinterpret_cast<const float *>(area + kScalars + 4 * lane);
+    const float l1 = *reinterpret_cast<const float *>(area + kScalars + 256 + 4 * lane);
+    m = fmaxf(m_ref, m1);
+    const float ref = m == -INFINITY ? 0.f : m;
+    w0 = fast_exp2(m_ref - ref), w1 = fast_exp2(m1 - ref);
+    l_tot = l_tot * w0 + l1 * w1;
   }
-  __syncthreads();
-  if (part == 1 || !live) return;
-  const float m1 = *reinterpret_cast<const float *>(area + kScalars + 4 * lane);
-  const float l1 = *reinterpret_cast<const float *>(area + kScalars + 256 + 4 * lane);
-  const float m = fmaxf(m_ref, m1), ref = m == -INFINITY ? 0.f : m;
-  const float w0 = fast_exp2(m_ref - ref), w1 = fast_exp2(m1 - ref);
+  if (!live) return;
   char *ws = static_cast<char *>(a.d.workspace);
-  const size_t slot = ((size_t)(chunk * cs.n_k + kvh) * c.splits + split) * kSharedRows + i;
+  const size_t slot = ((size_t)(chunk * cs.n_k + kvh) * c.splits + split) * c.rows + i;
   float *po = reinterpret_cast<float *>(ws + c.part_o) + slot * D;
 #pragma unroll
   for (int n = 0; n < C::NE; ++n)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       if (32 * n + 8 * g >= D) continue;  // padding columns
-      const f32x4 z = *reinterpret_cast<const f32x4 *>(area + (n * 4 + g) * 1024 + 16 * lane);
-      f32x4 y;
+      f32x4 y = {oacc[n][4 * g], oacc[n][4 * g + 1], oacc[n][4 * g + 2], oacc[n][4 * g + 3]};
+      if constexpr (C::P == 2) {
+        const f32x4 z = *reinterpret_cast<const f32x4 *>(area + (n * 4 + g) * 1024 + 16 * lane);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = oacc[n][4 * g + e] * w0 + z[e] * w1;
+        for (int e = 0; e < 4; ++e) y[e] = y[e] * w0 + z[e] * w1;
+      }
       *reinterpret_cast<f32x4 *>(po + 32 * n + 8 * g + 4 * hh) = y;
     }
-  if (hh == 0)
-    reinterpret_cast<f32x2 *>(ws + c.part_ml)[slot] = f32x2{m, l_tot * w0 + l1 * w1};
+  if (hh == 0) reinterpret_cast<f32x2 *>(ws + c.part_ml)[slot] = f32x2{m, l_tot};
 }
 
 // ------------------------------------------------------------ the own keys
@@ -439,11 +597,12 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
 // first % 2 of workgroup first / 2, the others in slot 0 of the next ones.
 template <int D, bool E4M3, int RG>
 __device__ void own_unit(const SharedArgs &a, const SharedCut &c, int g, unsigned char *smem,
-                         int *found) {
+                         int *found, Local &local) {
   using B = Block<D, E4M3>;
   constexpr int kRows = 16 * RG;
   const DecodeArgs &d = a.d;
-  const Plan plan = plan_at(a, c);
+  const View plan =
+      c.local ? plan_here(a, c, local, -1, g, c.own.groups) : plan_there(a, c, -1);  // uniform
   const int rep = scalar(d.n_q / d.s.n_k), row_groups = c.own.row_groups, R = c.vheads;
   const int b = d.s.b, G = c.own.groups;
   const int wave = scalar(threadIdx.x / 64);
@@ -629,17 +788,20 @@ __device__ void own_unit(const SharedArgs &a, const SharedCut &c, int g, unsigne
   }
 }
 
-template <int D, bool E4M3, int RG>
+template <int D, bool E4M3, int PR, int RG>
 __global__ __launch_bounds__(kThreads, 2) void shared_main_kernel(const SharedArgs a,
                                                                   const SharedCut c) {
   constexpr int kOwn = kWaves * 16 * RG * ((D + 4) + 2) * 4;
-  constexpr int kLds = kOwn > PrefixCfg<D>::LDS_BYTES ? kOwn : PrefixCfg<D>::LDS_BYTES;
+  // The plan behind what the own keys take, among what the prefix's tiles take later.
+  constexpr int kPrefix = PrefixCfg<D, PR>::LDS_BYTES, kPlanned = kOwn + (int)sizeof(Local);
+  constexpr int kLds = kPlanned > kPrefix ? kPlanned : kPrefix;
   __shared__ __attribute__((aligned(16))) unsigned char smem[kLds];
   __shared__ int found;
+  Local &local = *reinterpret_cast<Local *>(smem + kOwn);
   if ((int)blockIdx.x < c.prefix_blocks)  // workgroup-uniform
-    prefix_unit<D, E4M3>(a, c, smem);
+    prefix_unit<D, E4M3, PR>(a, c, smem, local);
   else
-    own_unit<D, E4M3, RG>(a, c, (int)blockIdx.x - c.prefix_blocks, smem, &found);
+    own_unit<D, E4M3, RG>(a, c, (int)blockIdx.x - c.prefix_blocks, smem, &found, local);
 }
 
 // ------------------------------------------------------------------ the join
@@ -660,13 +822,13 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(const SharedArgs 
   const int n = own + shared;
   if (n == 0) return;
   const int at_p = prow + hr;
-  const size_t base = ((size_t)(at_p / kSharedRows * d.s.n_k + kvh) * c.splits) * kSharedRows +
-                      at_p % kSharedRows;
+  const size_t base =
+      ((size_t)(at_p / c.rows * d.s.n_k + kvh) * c.splits) * c.rows + at_p % c.rows;
   const f32x2 *part_ml = reinterpret_cast<const f32x2 *>(ws + c.part_ml);
   const float *part_o = reinterpret_cast<const float *>(ws + c.part_o);
   auto find = [&](int i, const f32x2 *&ml, const float *&o) {
     if (i < shared) {
-      const size_t x = base + (size_t)i * kSharedRows;
+      const size_t x = base + (size_t)i * c.rows;
       ml = part_ml + x, o = part_o + x * D;
     } else if (open.count < 0) {
       ml = reinterpret_cast<const f32x2 *>(ws + c.row_ml) + row;
@@ -736,16 +898,20 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(const SharedArgs 
 
 template <int D, bool E4M3>
 void main_typed(const SharedArgs &a, const SharedCut &c, hipStream_t stream) {
-  const dim3 grid(c.prefix_blocks + c.own.groups);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(c.prefix_blocks + c.own.groups), dim3(kThreads), 0, stream, a,
+                       c);
+  };
   if (c.own.rows == 16)
-    hipLaunchKernelGGL((shared_main_kernel<D, E4M3, 1>), grid, dim3(kThreads), 0, stream, a, c);
+    c.rows == 64 ? go(shared_main_kernel<D, E4M3, 2, 1>) : go(shared_main_kernel<D, E4M3, 4, 1>);
   else
-    hipLaunchKernelGGL((shared_main_kernel<D, E4M3, 2>), grid, dim3(kThreads), 0, stream, a, c);
+    c.rows == 64 ? go(shared_main_kernel<D, E4M3, 2, 2>) : go(shared_main_kernel<D, E4M3, 4, 2>);
 }
 
 template <int D>
 hipError_t launch_dim(const SharedArgs &a, const SharedCut &c, hipStream_t stream) {
-  hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, c);
+  if (!c.local)
+    hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a, c);
   if (a.d.s.e4m3) main_typed<D, true>(a, c, stream);
   else main_typed<D, false>(a, c, stream);
   hipLaunchKernelGGL((shared_join_kernel<D>), dim3((unsigned)(a.d.s.b * a.d.n_q)), dim3(kThreads),

@@ -15,13 +15,18 @@ struct SharedArgs {
   float cap;                // 0: none
 };
 
-// Rows (a query head of a sequence that shares) that a workgroup of the prefix pass
-// takes, and the keys of its tiles.
-constexpr int kSharedRows = 64, kSharedTile = 64;
+// Keys of a tile of the prefix pass.
+constexpr int kSharedTile = 64;
+
+// Up to so many sequences and groups every workgroup plans by itself, in LDS; past them a
+// kernel of its own does it first.
+constexpr int kLocalSeqs = 512, kLocalGroups = 128;
 
 // How a call is cut, and where things lie in the workspace (byte offsets).
 struct SharedCut {
-  int chunks;      // of kSharedRows rows: at most, in all groups
+  bool local;      // no plan kernel
+  int rows;        // (a query head of a sequence that shares) of a prefix workgroup: 64 or 128
+  int chunks;      // of so many rows: at most, in all groups
   int splits;      // of a prefix's keys
   int prefix_blocks;
   DecodeCut own;   // of the sequences' own keys
@@ -31,33 +36,41 @@ struct SharedCut {
 
 inline SharedCut shared_cut(int b, int n_q, int n_k, int d, int max_len, int n_groups) {
   SharedCut c;
+  c.local = b <= kLocalSeqs && n_groups <= kLocalGroups;
   const long long rep = n_q / n_k;
   // a group's rows in whole chunks; no group that shares has fewer than two sequences
   const long long sharing = n_groups < b / 2 ? n_groups : b / 2;
-  c.chunks = (int)(sharing == 0 ? 0 : sharing + b * rep / kSharedRows);
-  // Enough workgroups for two per CU, of two tiles or more.
+  // A tile's way through LDS is paid once for 64 or 128 rows; a workgroup leaves O of all of
+  // them (us: 128 rows of a kv head 21.7 with 64, 26.2 with 128; 512 rows 39.7, 35.5).
+  c.rows = b * rep > 192 * sharing ? 128 : 64;
+  c.chunks = (int)((b * rep + sharing * (c.rows - 1)) / c.rows);
+  if (sharing == 0) c.chunks = 0;
   const long long per_split = (long long)c.chunks * n_k;
-  long long splits = per_split == 0 ? 0 : (512 + per_split - 1) / per_split;
+  // A workgroup of either kind per CU, which has room for two: twice as many for the
+  // prefix leave twice the partial results (32 sequences on one prompt of 16K tokens 21.7
+  // us, 31.8 with 512; 64 on one of 32K 35.5, 47.0).
+  long long splits = per_split == 0 ? 0 : (256 + per_split - 1) / per_split;
   const long long most = ((long long)max_len + 2 * kSharedTile - 1) / (2 * kSharedTile);
   if (splits > most) splits = most;
   if (splits > 8) splits = splits / 8 * 8;
   c.splits = (int)splits;
   c.prefix_blocks = (int)(per_split * splits);
   c.own = decode_cut(b, n_q, n_k, d, max_len);
+  if (c.own.groups > (sharing ? 256 : 512)) c.own.groups = sharing ? 256 : 512;
   c.vheads = n_k * c.own.row_groups;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t row = (size_t)d * sizeof(float), ml = 2 * sizeof(float);
   // total chunks; then start, row, members, units so far [b + 1]; of a group rows and chunks
   c.ints = 0;
   c.records = up((4 * (size_t)b + 2 + 2 * (size_t)n_groups) * sizeof(int));
-  c.open = up(c.records + (size_t)c.chunks * 4 * sizeof(int));
+  c.open = up(c.records + (size_t)c.chunks * 8 * sizeof(int));
   c.own_ml = up(c.open + (size_t)b * c.vheads * sizeof(DecodeOpen));
   c.own_o = up(c.own_ml + (size_t)c.own.groups * 2 * c.own.rows * ml);
   c.row_ml = up(c.own_o + (size_t)c.own.groups * 2 * c.own.rows * row);
   c.row_o = up(c.row_ml + (sharing ? (size_t)b * n_q * ml : 0));
   c.part_ml = up(c.row_o + (sharing ? (size_t)b * n_q * row : 0));
-  c.part_o = up(c.part_ml + (size_t)c.prefix_blocks * kSharedRows * ml);
-  c.bytes = c.part_o + (size_t)c.prefix_blocks * kSharedRows * row;
+  c.part_o = up(c.part_ml + (size_t)c.prefix_blocks * c.rows * ml);
+  c.bytes = c.part_o + (size_t)c.prefix_blocks * c.rows * row;
   return c;
 }
 

@@ -941,7 +941,7 @@ SpanCut span_cut(const SpanArgs &s) {
 // Row groups of the dQ pass: the causal backward's rule, but with spans 128 rows a
 // workgroup up to 256K query rows: documents make workgroups of very different
 // lengths, and twice as many of half the length even out better (16K tokens of packed
-// documents, 8 heads on 2 of 128: FIG).
+// documents, 8 heads on 2 of 128: 476 -> 464 us).
 int row_groups(const SpanArgs &s) {
   const int R = dq_row_groups(shape_of(s, (size_t)-1));
   return R == 8 && s.spans && (long long)s.b * s.Hl * s.S <= 262144 ? 4 : R;
