@@ -39,6 +39,10 @@ between the pack and attention, and the backward goes through both:
 buffers in place has no such step: there the owner of a shard calls
 qk_norm_rope on it before the exchange.
 
+With a `ScoreRule` attention is that of packed documents, prefixes and padding, with scores
+capped and biased by distance, forward (`attn_span_fwd`), backward (`attn_span_bwd`) and in
+`decode`.  It needs the rank's tensors packed, as the norm does.
+
 After a forward, either one, `fill_cache` puts the prompt's K and V into a paged
 cache, and `decode` takes the share on by one token per sequence.
 """
@@ -50,7 +54,8 @@ import torch
 
 from . import (attn_bwd, attn_bwd_sharded, attn_bwd_sharded_workspace_bytes,
                attn_bwd_workspace_bytes, attn_fwd,
-               attn_fwd_sharded, heads_per_member, pack, pack_qkv, qk_norm_rope, qk_norm_rope_bwd,
+               attn_fwd_sharded, attn_span_bwd, attn_span_bwd_workspace_bytes, attn_span_fwd,
+               heads_per_member, pack, pack_qkv, qk_norm_rope, qk_norm_rope_bwd,
                qk_norm_rope_bwd_workspace_bytes, unpack, unpack_add, unpack_grads)
 
 
@@ -66,9 +71,21 @@ class QkNormRope:
     interleaved: bool = False
 
 
+@dataclass
+class ScoreRule:
+    """What a layer's attention does to its scores: which keys each token sees (`attn_spans`, int32
+    [b, S, 2]; None: causal), the cap (None: none), and the slopes of all H query heads (fp32 [H];
+    None: no bias), of which a rank takes its own.  `decode` has the cap and slopes; its tokens see all
+    cached ones, whatever the spans."""
+    spans: torch.Tensor | None = None
+    cap: float | None = None
+    slopes: torch.Tensor | None = None
+
+
 class RankShare:
     def __init__(self, q_shards, k_shards, v_shards, do_shards, G: int, rank: int,
-                 scale: float | None = None, norm_rope: QkNormRope | None = None):
+                 scale: float | None = None, norm_rope: QkNormRope | None = None,
+                 rule: ScoreRule | None = None):
         self.G, self.rank = G, rank
         self.q_shards, self.k_shards, self.v_shards = q_shards, k_shards, v_shards
         self.do_shards = do_shards
@@ -114,6 +131,14 @@ class RankShare:
                 self.dq_weight = torch.empty_like(norm_rope.q_weight)
                 self.dk_weight = torch.empty_like(norm_rope.k_weight)
                 ws = max(ws, qk_norm_rope_bwd_workspace_bytes(b, S, self.Hl, self.Hkl, d))
+        self.rule = rule
+        self.slopes = None
+        if rule is not None:
+            if rule.slopes is not None:
+                if rule.slopes.shape != (H,):
+                    raise ValueError(f"slopes must be those of all {H} query heads")
+                self.slopes = rule.slopes[rank * self.Hl:(rank + 1) * self.Hl].contiguous()
+            ws = max(ws, attn_span_bwd_workspace_bytes(b, S, self.Hl, self.Hkl, d))
         self.workspace = torch.empty(max(ws, 16), dtype=torch.uint8, device=dev)
         # where the last forward's K and V are: "local" (k, v), "shards", or in neither
         self._kv = None
@@ -130,7 +155,14 @@ class RankShare:
                      interleaved=n.interleaved, q_out=self.q, k_out=self.k)
         self._kv = "local"
 
+    def _rule(self):
+        return {"scale": self.scale, "cap": self.rule.cap, "slopes": self.slopes}
+
     def attn_fwd(self):
+        if self.rule is not None:
+            attn_span_fwd(self.q, self.k, self.v, self.rule.spans, out=self.o, lse=self.lse,
+                          **self._rule())
+            return
         attn_fwd(self.q, self.k, self.v, G=self.G, scale=self.scale, out=self.o, lse=self.lse,
                  H_kv=self.H_kv)
 
@@ -141,6 +173,11 @@ class RankShare:
         pack(self.do_shards, self.rank, out=self.do)
 
     def attn_bwd(self):
+        if self.rule is not None:
+            attn_span_bwd(self.q, self.k, self.v, self.o, self.lse, self.do, self.rule.spans,
+                          dq=self.dq, dk=self.dk, dv=self.dv, workspace=self.workspace,
+                          **self._rule())
+            return
         attn_bwd(self.q, self.k, self.v, self.o, self.lse, self.do, G=self.G, scale=self.scale,
                  dq=self.dq, dk=self.dk, dv=self.dv, workspace=self.workspace, H_kv=self.H_kv)
 
@@ -196,17 +233,24 @@ class RankShare:
         for k, v, at in zip(self.k_shards, self.v_shards, start):
             cache.write(k[:, :, h:h + self.Hkl], v[:, :, h:h + self.Hkl], block_table, at)
 
-    def decode(self, cache, q, k, v, block_table, lens, max_len: int | None = None, workspace=None):
+    def decode(self, cache, q, k, v, block_table, lens, max_len: int | None = None, workspace=None,
+               groups=None, prefix_lens=None):
         """One new token per sequence: q [n, 1, H/G, d] and k, v [n, 1, Hkl, d], the rank's heads of
         its projections, at position lens[s] - 1.  Norm and rotation if the share has them, the
-        token's K and V into the cache, and attention over the lens[s] tokens: returns (O [n,
-        H/G, d], LSE [n, H/G]).  A length of 0 is a slot without a sequence."""
+        token's K and V into the cache, and attention over the lens[s] tokens, with the share's cap
+        and slopes if it has them: returns (O [n, H/G, d], LSE [n, H/G]).  A length of 0 is a slot
+        without a sequence.  ``groups``, ``prefix_lens``: sequences that share a prefix, in pages
+        that no new token goes to (`attn_decode_shared`)."""
         at = lens - 1
         n = self.norm_rope
         if n is not None:
             q, k = qk_norm_rope(q, k, n.q_weight, n.k_weight, n.cos, n.sin, eps=n.eps,
                                 interleaved=n.interleaved, positions=at.view(-1, 1))
         cache.write(k, v, block_table, at)
+        if self.rule is not None or groups is not None or prefix_lens is not None:
+            rule = {"scale": self.scale} if self.rule is None else self._rule()
+            return cache.attend_shared(q[:, 0], block_table, lens, groups, prefix_lens,
+                                       max_len=max_len, workspace=workspace, **rule)
         return cache.attend(q[:, 0], block_table, lens, scale=self.scale, max_len=max_len,
                             workspace=workspace)
 
@@ -215,6 +259,8 @@ class RankShare:
         if self.norm_rope is not None:
             raise ValueError("attention in place takes normalised, rotated shards: call qk_norm_rope "
                              "on them before the exchange")
+        if self.rule is not None:
+            raise ValueError("attention in place is causal: a share with a ScoreRule packs")
 
     def forward_sharded(self):
         self._check_in_place()
