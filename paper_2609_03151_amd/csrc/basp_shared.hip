@@ -38,11 +38,11 @@ struct Plan {
   int *total;    // chunks there are
   int *start;    // [b] a sequence's first own key: its group's prefix length, or 0
   int *row;      // [b] its first prefix row, in chunks of SharedCut.rows; -1: it shares nothing
-  int *member;   // [b] sequences that share, group by group, from its first sequence on
+  int *member;   // [b] sequences that share, group by group
   int *units;    // [b + 1] units of the sequences before, times their heads
-  int *group_n, *group_chunk;  // [n_groups]
+  int *group_n, *group_first, *group_chunk;  // [n_groups] members, places in `member`, chunks
   // Of a chunk of rows: its group's first place in `member` and the members' number, the
-  // prefix's length, the chunk's first row in the group; then the first member.
+  // prefix's length, the chunk's first row in the group.
   int4 *chunk;
 };
 __device__ __forceinline__ Plan plan_at(const SharedArgs &a, const SharedCut &c) {
@@ -55,7 +55,8 @@ __device__ __forceinline__ Plan plan_at(const SharedArgs &a, const SharedCut &c)
   p.member = p.row + b;
   p.units = p.member + b;
   p.group_n = p.units + b + 1;
-  p.group_chunk = p.group_n + a.n_groups;
+  p.group_first = p.group_n + a.n_groups;
+  p.group_chunk = p.group_first + a.n_groups;
   p.chunk = reinterpret_cast<int4 *>(ws + c.records);
   return p;
 }
@@ -67,97 +68,91 @@ __device__ __forceinline__ int units_of(int len, int start, int max_len) {
 
 __device__ __forceinline__ int clamp(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-// Sum over the workgroup of x of the threads before this one; `total`: of all.
-__device__ __forceinline__ int before(int x, int *sums, int &total) {
+// Sums of x and y over the threads before this one, and over all WAVES waves.
+template <int WAVES>
+__device__ __forceinline__ void before(int x, int y, int (*sums)[WAVES], int &tx, int &ty, int &ax,
+                                       int &ay) {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int incl = wave_scan(x);
+  const int ix = wave_scan(x), iy = wave_scan(y);
   __syncthreads();  // sums of the turn before are read
-  if (lane == 63) sums[wave] = incl;
+  if (lane == 63) sums[0][wave] = ix, sums[1][wave] = iy;
   __syncthreads();
-  int at = incl - x;
-  total = 0;
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    if (w < wave) at += sums[w];
-    total += sums[w];
+  tx = ix - x, ty = iy - y, ax = ay = 0;
+  for (int w = 0; w < WAVES; ++w) {
+    if (w < wave) tx += sums[0][w], ty += sums[1][w];
+    ax += sums[0][w], ay += sums[1][w];
   }
-  return at;
+}
+
+// The group that sequence s is in and whose prefix it is at least as long as, or -1. `bound`:
+// groups' first sequences, then b; one group whatever their order.
+template <class Bound, class Prefix>
+__device__ __forceinline__ int group_of(int s, int len, int n_groups, int max_len, Bound bound,
+                                        Prefix prefix) {
+  if (n_groups == 0 || len <= 0 || len > max_len) return -1;
+  int lo = 0, hi = n_groups;  // the last group that starts at s or before
+  while (hi - lo > 1) {
+    const int mid = lo + (hi - lo) / 2;
+    if (bound(mid) <= s) lo = mid;
+    else hi = mid;
+  }
+  if (s < bound(lo) || s >= bound(lo + 1)) return -1;
+  const int p = prefix(lo);
+  return p > 0 && len >= p ? lo : -1;
 }
 
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedArgs a,
                                                                    const SharedCut c) {
   const Plan p = plan_at(a, c);
-  const int b = a.d.s.b, rep = a.d.n_q / a.d.s.n_k;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  __shared__ int sums[kPlanThreads / 64], room;
-  if (tid == 0) room = c.chunks;
+  const int b = a.d.s.b, rep = a.d.n_q / a.d.s.n_k, n_groups = a.n_groups;
+  const int tid = threadIdx.x;
+  __shared__ int sums[2][kPlanThreads / 64];
+  for (int g = tid; g < n_groups; g += kPlanThreads)
+    __hip_atomic_store(p.group_n + g, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
   for (int s = tid; s < b; s += kPlanThreads) {
-    p.start[s] = 0;
-    p.row[s] = -1;
+    const int g = group_of(
+        s, a.d.lens[s], n_groups, a.d.max_len, [&](int i) { return a.groups[i]; },
+        [&](int i) { return a.prefix_lens[i]; });
+    p.row[s] = g;  // until the last pass
+    if (g >= 0) atomicAdd(p.group_n + g, 1);
   }
   __syncthreads();
-  auto group = [&](int g, int &g0, int &g1, int &prefix) {
-    g0 = clamp(a.groups[g], 0, b);
-    g1 = clamp(a.groups[g + 1], g0, b);
-    prefix = a.prefix_lens[g];
+  auto members_of = [&](int g) {  // at least two share, or nobody does
+    const int n =
+        __hip_atomic_load(p.group_n + g, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return n < 2 ? 0 : n;
   };
-  // Members of each group: a sequence as long as the prefix, or longer.
-  for (int g = wave; g < a.n_groups; g += kPlanThreads / 64) {
-    int g0, g1, prefix, n = 0;
-    group(g, g0, g1, prefix);
-    if (prefix > 0)
-      for (int s0 = g0; s0 < g1; s0 += 64) {
-        const int s = s0 + lane, len = s < g1 ? a.d.lens[s] : 0;
-        const bool in = len >= prefix && len <= a.d.max_len;
-        const uint64_t mask = __builtin_amdgcn_ballot_w64(in);
-        if (in) p.member[g0 + n + __builtin_popcountll(mask & ((1ull << lane) - 1))] = s;
-        n += __builtin_popcountll(mask);
-      }
-    if (lane == 0) p.group_n[g] = n < 2 ? 0 : n;
+  int members = 0, chunks = 0, x, y, ax, ay;
+  for (int g0 = 0; g0 < n_groups; g0 += kPlanThreads) {
+    const int g = g0 + tid, n = g < n_groups ? members_of(g) : 0;
+    const int mine = (n * rep + c.rows - 1) / c.rows;
+    before<kPlanThreads / 64>(n, mine, sums, x, y, ax, ay);
+    x += members, y += chunks;
+    members += ax, chunks += ay;
+    if (g >= n_groups) continue;
+    p.group_first[g] = x;
+    p.group_chunk[g] = y;
+    for (int i = 0; i < mine; ++i) p.chunk[y + i] = int4{x, n, a.prefix_lens[g], i * c.rows};
   }
+  if (tid == 0) *p.total = chunks;
   __syncthreads();
-  int chunks = 0;
-  for (int g0 = 0; g0 < a.n_groups; g0 += kPlanThreads) {
-    const int g = g0 + tid;
-    const long long rows = g < a.n_groups ? (long long)p.group_n[g] * rep : 0;
-    const int mine = (int)((rows + c.rows - 1) / c.rows);
-    int total;
-    const int at = chunks + before(mine, sums, total);
-    if (g < a.n_groups) {
-      // groups that overlap may have more rows than there is room for
-      if (at + mine > c.chunks) {
-        p.group_n[g] = 0;
-        atomicMin(&room, at);
-      }
-      p.group_chunk[g] = at;
-    }
-    chunks += total;
-  }
-  __syncthreads();
-  if (tid == 0) *p.total = chunks < room ? chunks : room;
-  for (int g = wave; g < a.n_groups; g += kPlanThreads / 64) {
-    int g0, g1, prefix;
-    group(g, g0, g1, prefix);
-    const int n = p.group_n[g], at = p.group_chunk[g];
-    for (int i = lane; i < n; i += 64) {
-      const int s = p.member[g0 + i];
-      p.start[s] = prefix;
-      p.row[s] = at * c.rows + i * rep;
-    }
-    const int mine = (int)(((long long)n * rep + c.rows - 1) / c.rows);
-    for (int i = lane; i < mine; i += 64) {
-      p.chunk[2 * (at + i)] = int4{g0, n, prefix, i * c.rows};
-      p.chunk[2 * (at + i) + 1] = int4{p.member[g0], 0, 0, 0};
-    }
-  }
-  __syncthreads();
+  members = 0;
   int units = 0;
   for (int s0 = 0; s0 < b; s0 += kPlanThreads) {
-    const int s = s0 + tid;
-    const int mine = s < b ? units_of(a.d.lens[s], p.start[s], a.d.max_len) * c.vheads : 0;
-    int total;
-    const int at = units + before(mine, sums, total);
-    if (s < b) p.units[s] = at;
-    units += total;
+    const int s = s0 + tid, g = s < b ? p.row[s] : -1, n = g >= 0 ? members_of(g) : 0;
+    const bool in = n > 0;
+    const int start = in ? a.prefix_lens[g] : 0;
+    before<kPlanThreads / 64>(
+        in, s < b ? units_of(a.d.lens[s], start, a.d.max_len) * c.vheads : 0, sums, x, y, ax, ay);
+    x += members, y += units;
+    members += ax, units += ay;
+    if (s >= b) continue;
+    p.start[s] = start;
+    p.units[s] = y;
+    if (in) p.member[x] = s;
+    const int rank = in ? clamp(x - p.group_first[g], 0, n - 1) : 0;
+    p.row[s] = in ? p.group_chunk[g] * c.rows + rank * rep : -1;
   }
   if (tid == 0) p.units[b] = units;
 }
@@ -171,7 +166,7 @@ struct View {
 };
 struct Local {
   int start[kLocalSeqs], member[kLocalSeqs], units[kLocalSeqs + 1];
-  int g0[kLocalGroups], g1[kLocalGroups], prefix[kLocalGroups], n[kLocalGroups];
+  int bound[kLocalGroups + 1], prefix[kLocalGroups], n[kLocalGroups];
   int first[kLocalGroups], chunk0[kLocalGroups];
   int sums[2][kWaves], rec[4];
 };
@@ -182,7 +177,7 @@ struct Local {
 __device__ __forceinline__ View plan_here(const SharedArgs &a, const SharedCut &c, Local &p,
                                           int chunk, int g, int G) {
   const int b = a.d.s.b, rep = a.d.n_q / a.d.s.n_k, n_groups = a.n_groups;
-  const int tid = threadIdx.x, lane = tid % 64, wave = scalar(tid / 64);
+  const int tid = threadIdx.x;
   constexpr int kTurns = kLocalSeqs / kThreads;
   int len[kTurns];
 #pragma unroll
@@ -191,52 +186,28 @@ __device__ __forceinline__ View plan_here(const SharedArgs &a, const SharedCut &
     len[k] = s < b ? a.d.lens[s] : 0;
   }
   if (tid < n_groups) {
-    const int g0 = clamp(a.groups[tid], 0, b);
-    p.g0[tid] = g0;
-    p.g1[tid] = clamp(a.groups[tid + 1], g0, b);
+    p.bound[tid] = a.groups[tid];
     p.prefix[tid] = a.prefix_lens[tid];
     p.n[tid] = 0;
   }
+  if (n_groups > 0 && tid == n_groups) p.bound[tid] = a.groups[tid];
   if (tid == 0) p.rec[1] = 0;
   __syncthreads();
   int of[kTurns];  // a sequence's group, if it is as long as its prefix
 #pragma unroll
   for (int k = 0; k < kTurns; ++k) {
-    const int s = tid + k * kThreads;
-    of[k] = -1;
-    if (s < b && n_groups > 0) {
-      int lo = 0, hi = n_groups;  // the last group that starts at s or before
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (p.g0[mid] <= s) lo = mid;
-        else hi = mid;
-      }
-      if (s >= p.g0[lo] && s < p.g1[lo] && p.prefix[lo] > 0 && len[k] >= p.prefix[lo] &&
-          len[k] <= a.d.max_len) {
-        of[k] = lo;
-        atomicAdd(&p.n[lo], 1);
-      }
-    }
+    of[k] = group_of(
+        tid + k * kThreads, len[k], n_groups, a.d.max_len, [&](int i) { return p.bound[i]; },
+        [&](int i) { return p.prefix[i]; });
+    if (of[k] >= 0) atomicAdd(&p.n[of[k]], 1);
   }
   __syncthreads();
-  // Sums over the threads before this one, and of all, of two numbers.
-  auto before = [&](int x, int y, int &tx, int &ty, int &ax, int &ay) {
-    const int ix = wave_scan(x), iy = wave_scan(y);
-    __syncthreads();  // sums of the turn before are read
-    if (lane == 63) p.sums[0][wave] = ix, p.sums[1][wave] = iy;
-    __syncthreads();
-    tx = ix - x, ty = iy - y, ax = ay = 0;
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) tx += p.sums[0][w], ty += p.sums[1][w];
-      ax += p.sums[0][w], ay += p.sums[1][w];
-    }
-  };
   int all_first, all_chunks;
   {
     const int n = tid < n_groups && p.n[tid] >= 2 ? p.n[tid] : 0;
     const int mine = (n * rep + c.rows - 1) / c.rows;
     int first, chunk0;
-    before(n, mine, first, chunk0, all_first, all_chunks);
+    before<kWaves>(n, mine, p.sums, first, chunk0, all_first, all_chunks);
     if (tid < n_groups) p.first[tid] = first, p.chunk0[tid] = chunk0;
     if (mine > 0 && chunk >= chunk0 && chunk < chunk0 + mine) {
       p.rec[0] = first, p.rec[1] = n, p.rec[2] = p.prefix[tid];
@@ -250,7 +221,8 @@ __device__ __forceinline__ View plan_here(const SharedArgs &a, const SharedCut &
     const bool in = n >= 2;
     const int start = in ? p.prefix[gr] : 0;
     int at, u, am, au;
-    before(in, s < b ? units_of(len[k], start, a.d.max_len) * c.vheads : 0, at, u, am, au);
+    before<kWaves>(in, s < b ? units_of(len[k], start, a.d.max_len) * c.vheads : 0, p.sums, at, u, am,
+                   au);
     at += members, u += units;
     members += am, units += au;
     if (s < b) {
@@ -276,8 +248,8 @@ __device__ __forceinline__ View plan_there(const SharedArgs &a, const SharedCut 
   const Plan p = plan_at(a, c);
   View v{p.start, p.member, p.units, int4{0, 0, 0, 0}, 0, false};
   if (chunk >= 0 && chunk < *p.total) {
-    v.rec = p.chunk[2 * chunk];
-    v.lead = p.chunk[2 * chunk + 1].x;
+    v.rec = p.chunk[chunk];
+    v.lead = p.member[v.rec.x];
     v.chunk = true;
   }
   return v;
@@ -394,7 +366,7 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
       const size_t at = there ? (((size_t)id * cs.n_k + kvh) << cs.page_log2) +
                                     (key & ((1 << cs.page_log2) - 1))
                               : 0;
-      // keys past the end: the last row again, or (a whole block) any
+      // keys past the end: the last row again, or (a whole block) any; put() clears V
       const int last = there ? prefix - key - 1 : 0;
       const uint32_t r = (uint32_t)(row < last ? row : last);
       const uint32_t off = r * W::kRowBytes + cc * 16;
@@ -421,9 +393,18 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
   };
   const int to0 = T::off(row + 16 * block, E4M3 ? 2 * cc : cc);
   const int to1 = E4M3 ? T::off(row + 16 * block, 2 * cc + 1) : 0;
-  auto put = [&](int stage) __attribute__((always_inline)) {  // into LDS
+  auto put = [&](int t, int stage) __attribute__((always_inline)) {  // into LDS
     if (!carries) return;
     unsigned char *Ks = smem + stage * C::TILE_BYTES;
+    if ((t + 1) * kSharedTile > prefix) {  // workgroup-uniform: the last tile
+      // V of keys past the end must not meet their weight of 0 as infinities or NaN
+#pragma unroll
+      for (int j = 0; j < W::N; ++j)
+        if (first_key(t, j) + row >= prefix) {
+          x_.v[j] = u32x4{0, 0, 0, 0};
+          if constexpr (E4M3) x_.vs[j] = 127;
+        }
+    }
 #pragma unroll
     for (int j = 0; j < W::N; ++j) {
       const int at = j * 16 * W::kAtOnce * T::ROW_BYTES;
@@ -529,7 +510,7 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
   if (t0 < t1) load_rows(t0);
   load_pages(t0 + 1);
   auto turn = [&](int t, int stage) __attribute__((always_inline)) {
-    put(stage);
+    put(t, stage);
     if (t + 1 < t1) {
       load_rows(t + 1);
       load_pages(t + 2);

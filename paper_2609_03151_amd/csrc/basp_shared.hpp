@@ -60,10 +60,10 @@ inline SharedCut shared_cut(int b, int n_q, int n_k, int d, int max_len, int n_g
   c.vheads = n_k * c.own.row_groups;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t row = (size_t)d * sizeof(float), ml = 2 * sizeof(float);
-  // total chunks; then start, row, members, units so far [b + 1]; of a group rows and chunks
+  // total chunks; then start, row, member, units [b + 1]; of a group members, first, chunk
   c.ints = 0;
-  c.records = up((4 * (size_t)b + 2 + 2 * (size_t)n_groups) * sizeof(int));
-  c.open = up(c.records + (size_t)c.chunks * 8 * sizeof(int));
+  c.records = up((4 * (size_t)b + 2 + 3 * (size_t)n_groups) * sizeof(int));
+  c.open = up(c.records + (size_t)c.chunks * 4 * sizeof(int));
   c.own_ml = up(c.open + (size_t)b * c.vheads * sizeof(DecodeOpen));
   c.own_o = up(c.own_ml + (size_t)c.own.groups * 2 * c.own.rows * ml);
   c.row_ml = up(c.own_o + (size_t)c.own.groups * 2 * c.own.rows * row);

@@ -242,6 +242,35 @@ def test_values_that_are_not_finite():
     assert not o2[bad].isfinite().any() and torch.equal(o2[~bad], o[~bad])
 
 
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("prefix", [1, 20, 40, 300, 331])
+def test_keys_past_a_prefix(prefix, dtype):
+    """Whatever lies in pages of nobody, the first among them; and an infinite value at a prefix's
+    last key, which is read again for the keys past it, reaches its element alone."""
+    c = Case([4], [prefix], [10, 0, -1, 70], 4, 2, 64, 16, dtype, seed=prefix)
+    names = c.table[c.table >= 0]
+    free = next(p for p in range(c.cache.k_pages.shape[0]) if not (names == p).any())
+    pools = [c.cache.k_pages, c.cache.v_pages]
+    pools += [c.cache.k_scales, c.cache.v_scales] if dtype == E4M3 else []
+    for pool in pools:
+        raw = pool.view(torch.uint8 if pool.element_size() == 1 else torch.int16)
+        raw[free] = raw[0]
+    c.table.copy_(torch.where(c.table == 0, free, c.table))
+    for pool in pools:
+        raw = pool.view(torch.uint8 if pool.element_size() == 1 else torch.int16)
+        raw[0] = 0x7F if pool.element_size() == 1 else 0x7FC0
+    c.check()
+    if dtype == E4M3:
+        return
+    t = prefix - 1
+    for s in (0, 1, 3):  # 2 ends before it
+        c.cache.v_pages[c.table[s, t // 16], 1, t % 16, 11] = math.inf
+    o, _ = c.run()
+    assert not o[[0, 1, 3], 2:, 11].isfinite().any()
+    assert o[2].isfinite().all() and o[:, :, :11].isfinite().all() and o[:, :2].isfinite().all()
+    assert o[:, :, 12:].isfinite().all()
+
+
 def test_group_ends_out_of_range():
     """Ends before the first sequence and past the last are taken for these."""
     c = Case([3, 4], [200, 100], [1, 2, 3, 4, 5, 6, 7], 4, 1, 64, 16, BF16, seed=6)
@@ -253,6 +282,24 @@ def test_group_ends_out_of_range():
     plain = c.run(groups=False)
     c.prefix.copy_(ints([-3, 2 ** 31 - 1]))
     for x, y in zip(c.run(), plain):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("per,b", [(4, 8), (300, 600)])
+def test_groups_out_of_order(per, b):
+    """Ends that do not ascend: other results, nothing outside the buffers, nothing left behind."""
+    g = b // per
+    c = Case([per] * g, [50] * g, [s % 7 for s in range(b)], 2, 1, 64, 16, BF16, seed=b)
+    want = c.run()
+    good = c.groups.clone()
+    need = basp.attn_decode_shared_workspace_bytes(b, 2, 1, 64, c.max_len, g)
+    ws = torch.full((need + 512,), 255, device="cuda", dtype=torch.uint8)
+    for ends in ([b, 0, per], [0, b, per], [per, 2 * per, 0], [0, b, b], [0, 0, per]):
+        c.groups.copy_(ints(ends))
+        c.run(workspace=ws[256:256 + need])
+        assert (ws[:256] == 255).all() and (ws[-256:] == 255).all()
+    c.groups.copy_(good)
+    for x, y in zip(c.run(workspace=ws[256:256 + need]), want):
         assert torch.equal(x, y)
 
 
