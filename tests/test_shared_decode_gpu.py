@@ -364,3 +364,36 @@ def test_empty():
     c.check(groups=False)
     o, _ = c.cache.attend_shared(c.q, c.table, c.lens, ints([0]), ints([]), scale=0.1)
     assert torch.equal(o, c.run(groups=False)[0])
+
+
+def test_pools_past_4_gib():
+    """Pages all over pools of 5 GB each."""
+    c = Case([5, 3], [1000, 300], [100, 3, 200, 1, 0, 9, 30, 77], 8, 2, 128, 64, BF16, seed=10,
+             spare=160000)
+    assert c.cache.k_pages.numel() * 2 > 2 ** 32
+    assert c.table.max() * 2 * 64 * 128 * 2 > 2 ** 32
+    c.check(cap=20.0, slopes=_slopes(8))
+
+
+@pytest.mark.parametrize("groups", [2, 300])
+def test_two_calls_at_once(groups):
+    """Calls on two streams side by side, a workspace each, one of them a graph's: the bits of one
+    after the other."""
+    cases = [Case([3] * groups, [200] * groups, [i + s % 40 for s in range(3 * groups)], 4, 2, 64, 16,
+                  BF16, seed=i) for i in (1, 2)]
+    want = [[x.clone() for x in c.run(cap=9.0)] for c in cases]
+    spaces = [torch.empty(basp.attn_decode_shared_workspace_bytes(c.b, 4, 2, 64, c.max_len, groups),
+                          device="cuda", dtype=torch.uint8) for c in cases]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = cases[1].run(cap=9.0, workspace=spaces[1])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(streams[1]):
+            graph.replay()
+        with torch.cuda.stream(streams[0]):
+            got = cases[0].run(cap=9.0, workspace=spaces[0])
+        torch.cuda.synchronize()
+        for x, y in zip((*got, *out), (*want[0], *want[1])):
+            assert torch.equal(x, y)
