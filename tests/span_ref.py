@@ -65,6 +65,11 @@ def fwd_ref(q, k, v, spans, scale, cap, slopes):
     O = torch.matmul(p, V)
     # a weight: rounded, its exponent, and the reference's; the row's sum alike but unrounded
     bound = torch.matmul(p * (U16 + 2 * EXP + (2 * n + 16) * U32 + e + worst), V.abs()) * 1.01
+    if cap and cap <= 64:
+        # With the fixed reference O is divided by the sum L' of weights of which some are rounded:
+        # w_j = p_j (1 + d_j), |d_j| <= U16, so L' = L (1 + x) with |x| <= U16 sum p_j = U16, and
+        # sum w_j v_j / L' - O = (sum p_j d_j v_j - x O) / (1 + x): U16 |O| more.
+        bound = bound + U16 * 1.01 * O.abs()
     # weights below 2^-126 may be taken for 0: relative to the row's sum, which is 2^-8 at least with
     # a reference that follows the maximum to 2^8, and 2^(-1.45 cap) with the fixed one (cap <= 64)
     lost = 2.0 ** -116 if not cap or cap > 64 else 2.0 ** -33
