@@ -8,6 +8,7 @@ the library raises.
 
 Names follow the C ABI: ``pack``, ``unpack``, ``attn_fwd``, ``attn_bwd``,
 ``attn_bwd_workspace_bytes``, ``qk_norm_rope``, ``kv_write``, ``attn_decode``,
+``attn_span_fwd``, ``attn_span_bwd``, ``attn_decode_shared``,
 ``validate``, ``group_of``, ``status_str``.
 """
 from __future__ import annotations
