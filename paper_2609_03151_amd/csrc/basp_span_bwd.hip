@@ -5,7 +5,9 @@
 //   dV_j = sum_i P_ij dO_i,  dK_j = scale sum_i dS_ij q_i,  dQ_i = scale sum_j dS_ij k_j
 // (sums over the keys a row sees, and over the query heads of a kv head).  Bound
 // by the matrix cores: five products of 2 d operations a seen pair are needed,
-// seven are formed (S and dP in both passes).
+// seven are formed (S and dP in both passes).  On MI355X, 16K tokens, 8 heads on 2 of
+// 128: one document with a cap 2035 us, 675 TFLOP/s of the five; documents of some 2K with
+// a bias 420 us, 535 TFLOP/s.
 //
 // Kernels, all deterministic (no atomics):
 //   span_pre     per row and head -LSE and -D, of rows padded to 64; per row its span;
@@ -939,12 +941,12 @@ SpanCut span_cut(const SpanArgs &s) {
 }
 
 // Row groups of the dQ pass: the causal backward's rule, but with spans 128 rows a
-// workgroup up to 256K query rows: documents make workgroups of very different
-// lengths, and twice as many of half the length even out better (16K tokens of packed
-// documents, 8 heads on 2 of 128: 476 -> 464 us).
+// workgroup up to 96K query rows: documents make workgroups of very different
+// lengths, and twice as many of half the length even out better (42K rows, d = 80,
+// documents of 1200 tokens: 123 -> 115 us; 128K rows of documents of 2048: 419, 421).
 int row_groups(const SpanArgs &s) {
   const int R = dq_row_groups(shape_of(s, (size_t)-1));
-  return R == 8 && s.spans && (long long)s.b * s.Hl * s.S <= 262144 ? 4 : R;
+  return R == 8 && s.spans && (long long)s.b * s.Hl * s.S <= 98304 ? 4 : R;
 }
 long long dq_blocks_of(const SpanArgs &s) {
   const int rows = 32 * row_groups(s);
