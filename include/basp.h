@@ -601,7 +601,8 @@ int basp_attn_decode_shared(const void *q, const void *k_pages, const void *v_pa
  * products), softmax in fp32; deterministic.  tanh is off by at most 2^-21, so a capped
  * score by 2^-21 * cap; a bias and an LSE are fp32 numbers, off by 2^-24 of
  * themselves: rows all of whose keys are far away, |slope * distance| past 2^12, see that in
- * P.  A value, key, query or gradient outside every span that it would meet does not
+ * P.  Values of up to 2^96 in magnitude do not overflow on the way to O, whatever the scores.
+ * A value, key, query or gradient outside every span that it would meet does not
  * count, infinities and NaN too; inside one they make what they reach NaN: a value
  * its element of O, a score of plus infinity or NaN its row.
  * Conditions: d 64, 80, 96 or 128; scale 2^-40 to 2^40; 16-byte aligned q, k, v, o,

@@ -20,7 +20,9 @@ constexpr float kSpanLn2 = 0.69314718055994531f;
 
 // Up to this cap the exponents' reference needs no running maximum: a capped
 // score is at most cap and at least -cap, so with the largest bias of the row
-// as its reference P lies in 2^(+-92.4), and sums over 2^24 keys in fp32's range.
+// as its reference P lies in 2^(+-92.4), and sums of P over 2^24 keys in fp32's range.
+// Their products with V need not: rows whose sum is far from 1 are done again against
+// their maximum where it matters (basp_span_fwd.hip).
 constexpr float kSpanFixedCap = 64.f;
 
 // A tensor [b, S, n, d] whose tokens lie row_elems elements apart.

@@ -32,6 +32,10 @@ constexpr float kRescaleSlack = 8.f;  // log2 headroom before the reference max 
 // A lane's sum of a tile's P past which the pipelined loop moves the reference.
 constexpr float kFollowSum = 65536.f;
 constexpr int kFewKeys = 16;
+// With a fixed reference, the sums of a row's P between which its products with V stay
+// in fp32's range, since they are at most the sum times the largest |V| (2^104 / 2^24),
+// and those that come out 0 are less than 2^-86 a key.
+constexpr float kLowSum = 0x1p-40f, kHighSum = 0x1p24f;
 constexpr int kSchedMfma = 0x008;
 constexpr int kSchedDsRead = 0x100;
 
@@ -128,6 +132,7 @@ struct Work {
   SpanHull hull;         // of the wave's rows
   float sl, c, rc, c1, cap2;
   bool fixed;            // the reference stands still (kSpanFixedCap)
+  bool stays;            // this row's, where not all rows' do
   float m_ref, l_run;
   // With a fixed reference, where some row of the wave sees few keys (`few`): what rounding
   // P to bf16 on edges added to the row's sum.  Its largest P is not 1, and O is divided
@@ -218,6 +223,7 @@ __device__ __forceinline__ void enter(Work<C> &wk, bf16x8 (&qf)[C::NS], const Sp
   wk.fixed = CAP && a.cap <= kSpanFixedCap;
   wk.few = wk.fixed && __builtin_amdgcn_ballot_w64(wk.hi > wk.lo && wk.hi - wk.lo <= kFewKeys) != 0;
   wk.l_run = wk.l_fix = 0.f;
+  wk.stays = false;
   wk.m_ref = -INFINITY;
   if (wk.fixed) {  // the largest bias of the row, at its nearest or farthest key
     const int near = wk.row < wk.lo ? wk.lo - wk.row : wk.row >= wk.hi ? wk.row - wk.hi + 1 : 0;
@@ -397,6 +403,7 @@ __device__ __forceinline__ void one_tile(Work<C> &wk, const Offsets<C, D> &off,
       float mx = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+      if (CAP && CAREFUL && wk.stays) mx = -INFINITY;
       move_reference<C>(wk, oacc, pair_max(mx));
     }
     // A row of which no key has come yet: every score is -inf, P = 0.
@@ -409,7 +416,10 @@ __device__ __forceinline__ void one_tile(Work<C> &wk, const Offsets<C, D> &off,
     }
     wk.l_run += psum;
     const u32x4 p8[2] = {pack8(sc, 0), pack8(sc, 8)};
-    if (CAP && edge && wk.few) wk.l_fix += sum8(p8[0]) + sum8(p8[1]) - psum;  // wave-uniform
+    if (CAP && edge && wk.few) {  // wave-uniform
+      const float fix = sum8(p8[0]) + sum8(p8[1]) - psum;
+      wk.l_fix += CAREFUL && !wk.stays ? 0.f : fix;  // a reference that moves does not move it
+    }
     const bf16x8 pf[2] = {as_bf16x8(p8[0]), as_bf16x8(p8[1])};
 #pragma unroll
     for (int n = 0; n < C::NE; ++n)
@@ -434,15 +444,54 @@ __device__ __forceinline__ void one_tile(Work<C> &wk, const Offsets<C, D> &off,
 }
 
 // O of no finite value anywhere in the workgroup: infinities or NaN in V, which 0 * V
-// may have carried to rows that do not see them, or P past fp32's range.  All rows again,
-// tile by tile.
+// may have carried to rows that do not see them, or P, or its products, past fp32's range.
+// Or a row whose sum is low with a fixed reference (P of all its keys down to 2^-92): its
+// products with small values have come out 0.  All rows again, tile by tile, those whose
+// sum is far from 1 against their maximum (the others keep their reference, and so their
+// bits, whatever is in rows beside them).
 template <class C, int D, bool CAP, bool BIAS>
 __device__ __forceinline__ void again_if_needed(Work<C> &wk, const Offsets<C, D> &off,
                                                 const Copies<C, D> &copies,
                                                 const bf16x8 (&qf)[C::NS], f32x16 (&oacc)[C::NE],
-                                                const unsigned char *smem, int part) {
-  if (!__syncthreads_or(!finite<C::NE>(oacc, 0.f * wk.l_run))) return;
-  if (!wk.fixed) wk.m_ref = -INFINITY;
+                                                const unsigned char *smem,
+                                                uint32_t (&votes)[3][kMaxWaves], int part) {
+  const bool bad = !finite<C::NE>(oacc, 0.f * wk.l_run);
+  if constexpr (CAP) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool sees = wk.fixed && wk.hi > wk.lo;
+    const float l = pair_sum(wk.l_run);
+    const uint32_t any = __builtin_amdgcn_ballot_w64(bad) != 0;
+    const uint32_t low = (uint32_t)__builtin_amdgcn_ballot_w64(sees && l < kLowSum);
+    const uint32_t high = (uint32_t)__builtin_amdgcn_ballot_w64(sees && l > kHighSum);
+    if ((threadIdx.x & 63) == 0) votes[0][w] = any, votes[1][w] = low, votes[2][w] = high;
+    __syncthreads();
+    uint32_t wrong = 0, little = 0, mine = 0;
+#pragma unroll
+    for (int r = 0; r < C::R; ++r) {
+      uint32_t lows = ~0u, highs = 0;  // low in every part: in one, keys may well weigh nothing
+#pragma unroll
+      for (int p = 0; p < C::P; ++p) {
+        wrong |= votes[0][p * C::R + r];
+        lows &= votes[1][p * C::R + r];
+        highs |= votes[2][p * C::R + r];
+      }
+      little |= lows;
+      if (w % C::R == r) mine = lows | highs;
+    }
+    wrong = __builtin_amdgcn_readfirstlane(wrong);
+    little = __builtin_amdgcn_readfirstlane(little);
+    if (!wrong && !little) return;
+    if (wk.fixed) {
+      wk.stays = !((mine >> (threadIdx.x & 31)) & 1);
+      if (!wk.stays) wk.m_ref = -INFINITY;
+      wk.fixed = false;
+    } else {
+      wk.m_ref = -INFINITY;
+    }
+  } else {
+    if (!__syncthreads_or(bad)) return;
+    wk.m_ref = -INFINITY;
+  }
   wk.l_run = wk.l_fix = 0.f;
   clear<C::NE>(oacc);
   for (int u = 0; u < wk.nt; ++u) {
@@ -466,6 +515,7 @@ __global__ __launch_bounds__(512, 1) void span_fwd_split_kernel(const SpanArgs a
   // LDS: the K tiles of the ring stages, then their V tiles.
   __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
   __shared__ int hulls[2][kMaxWaves];
+  __shared__ uint32_t votes[3][kMaxWaves];
   constexpr int kSt = C::STAGES;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rg = w % R, part = w / R;  // row group, key part
@@ -503,7 +553,7 @@ __global__ __launch_bounds__(512, 1) void span_fwd_split_kernel(const SpanArgs a
           one_tile<C, D, CAP, BIAS, false>(wk, off, qf, oacc, smem + st * C::TILE_BYTES, u0 + st,
                                            part);
       }
-  again_if_needed<C, D, CAP, BIAS>(wk, off, copies, qf, oacc, smem, part);
+  again_if_needed<C, D, CAP, BIAS>(wk, off, copies, qf, oacc, smem, votes, part);
   float l_tot = pair_sum(wk.l_run), l_fix = CAP ? pair_sum(wk.l_fix) : 0.f;
   if (!merge_parts<C>(smem, rg, part, lane, wk.m_ref, l_tot, l_fix, oacc)) return;
   leave<C, D>(wk, a, o, lse, l_tot, l_fix, oacc);
@@ -528,6 +578,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void span_fwd_kernel(const S
   constexpr int kSt = C::STAGES, kPD = 2, kPf = 2;
   __shared__ __attribute__((aligned(16))) unsigned char smem[C::LDS_BYTES];
   __shared__ int hulls[2][kMaxWaves];
+  __shared__ uint32_t votes[3][kMaxWaves];
   const int hh = (threadIdx.x & 63) >> 5;
   Work<C> wk;
   bf16x8 qf[C::NS];
@@ -750,7 +801,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void span_fwd_kernel(const S
       }
     }
   }
-  again_if_needed<C, D, CAP, BIAS>(wk, off, copies, qf, oacc, smem, part);
+  again_if_needed<C, D, CAP, BIAS>(wk, off, copies, qf, oacc, smem, votes, part);
   float l_tot = pair_sum(wk.l_run), l_fix = CAP ? pair_sum(wk.l_fix) : 0.f;
   if constexpr (C::P > 1) {
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
