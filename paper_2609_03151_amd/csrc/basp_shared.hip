@@ -31,7 +31,6 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kUnit = kWaves * kBlockKeys;  // own keys: a block per wave
 static_assert(kUnit == kDecodeUnit, "the host's cut");
-constexpr float kFixedCap = 64.f;      // up to it P needs no running maximum (basp_span.hpp)
 constexpr float kRescaleSlack = 8.f;   // log2 headroom before the reference max moves
 constexpr int kPlanThreads = 1024;
 
@@ -337,10 +336,9 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
   const float at = live ? (float)(a.d.lens[seq] - 1) : 0.f;
   const float sl = a.slopes && live ? a.slopes[head] * kLog2e : 0.f;
   const float c2 = a.d.scale * kLog2e;
-  const bool capped = a.cap > 0.f, fixed = capped && a.cap <= kFixedCap;
+  const bool capped = a.cap > 0.f;
   const float c1 = capped ? 2.f * c2 / a.cap : 0.f, cap2 = a.cap * kLog2e;
   float m_ref = -INFINITY, l_run = 0.f;
-  if (fixed) m_ref = fmaxf(-sl * (at - (float)(prefix - 1)), -sl * at);
 
   f32x16 oacc[C::NE];
 #pragma unroll
@@ -463,22 +461,24 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
       for (int r = 0; r < 16; ++r)
         if (jl + 8 * (r >> 2) + (r & 3) >= prefix) sc[r] = -INFINITY;
     }
-    if (!fixed) {
-      float mx = -INFINITY;
+    // Against a running maximum with a cap too: that bounds the scores, but with a reference
+    // that stands still P lies in 2^(+-92) at a cap of 64, too wide for its products with V,
+    // and a weight alone in its row is rounded (64 sequences on one prompt of 32K, 8 heads on
+    // 1, a cap of 50: 37.2 us standing still, 35.8).
+    float mx = -INFINITY;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-      mx = pair_max(mx);
-      const bool grow = mx > m_ref + kRescaleSlack;
-      if (__builtin_amdgcn_ballot_w64(grow)) {  // wave-uniform, rare after the first tiles
-        asm volatile("" ::: "memory");
-        const float alpha = grow ? fast_exp2(m_ref - mx) : 1.f;
-        m_ref = grow ? mx : m_ref;
-        l_run *= alpha;
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+    mx = pair_max(mx);
+    const bool grow = mx > m_ref + kRescaleSlack;
+    if (__builtin_amdgcn_ballot_w64(grow)) {  // wave-uniform, rare after the first tiles
+      asm volatile("" ::: "memory");
+      const float alpha = grow ? fast_exp2(m_ref - mx) : 1.f;
+      m_ref = grow ? mx : m_ref;
+      l_run *= alpha;
 #pragma unroll
-        for (int n = 0; n < C::NE; ++n)
+      for (int n = 0; n < C::NE; ++n)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) oacc[n][r] *= alpha;
-      }
+        for (int r = 0; r < 16; ++r) oacc[n][r] *= alpha;
     }
     const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
     float psum = 0.f;
