@@ -42,7 +42,7 @@ struct SpanArgs {
 // The backward's: planes of -LSE and -D, the rows' hulls, which units of the key
 // pass saw anything, and their partial sums of dK and dV.
 size_t span_bwd_workspace_bytes(const SpanArgs &s);
-bool span_bwd_fits(const SpanArgs &s);  // its workgroups in one launch
+bool span_bwd_fits(const SpanArgs &s);  // its workgroups in one launch, a unit's steps in LDS
 hipError_t launch_span_bwd(const SpanArgs &s, const uint16_t *o, const float *lse,
                            const uint16_t *d_o, void *dq, void *dk, void *dv, bool grad_bf16,
                            void *workspace, hipStream_t stream);

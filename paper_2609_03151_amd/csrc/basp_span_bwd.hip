@@ -152,6 +152,13 @@ __global__ __launch_bounds__(kPreThreads) void span_pre_kernel(const BwdArgs a,
 }
 
 // ---------------------------------------------------------------- key pass
+// An entry of the list of steps is the step's number, and two bits for each of its
+// 32-row halves and 32-key blocks (bit 16 + 2 (4 half + block)): 0 nobody sees anything,
+// 1 mask, 2 everybody sees everything.
+// Steps of a chunk at most: a sixteenth of the longest sequence (a row of D elements takes
+// 2 D of its 2^31 bytes), rounded up to whole key tiles.
+constexpr int max_steps(int d) { return (1 << 20) / d + 2; }
+
 template <int D>
 struct KvCfg {
   static constexpr int DC = HeadDim<D>::DC;
@@ -167,27 +174,24 @@ struct KvCfg {
   static constexpr int KV_DMA_PER_WAVE = kKN * CPR / kThreads;  // for the V tile
   static constexpr bool V_REGS = D < 128;  // V of the wave's keys fits in registers
   // LDS: Q tiles of the two ring stages, their dO tiles, their AUX blocks,
-  // then (d = 128) the V tile.  After the last step the same bytes hold the
-  // second waves' partial sums.
+  // then (d = 128) the V tile, then the list of steps.  After the last step the same
+  // bytes hold the second waves' partial sums.
   static constexpr int DO_REGION = 2 * TILE_BYTES;
   static constexpr int AUX_REGION = 4 * TILE_BYTES;
   static constexpr int KV_REGION = AUX_REGION + 2 * AUX_BYTES;
   static constexpr int PART_BYTES = kWaves / 2 * 2 * NE * 4 * 1024;
-  static constexpr int RING_BYTES = KV_REGION + (V_REGS ? 0 : KT_BYTES);
+  static constexpr int LIST_REGION = KV_REGION + (V_REGS ? 0 : KT_BYTES);
+  static constexpr int RING_BYTES = LIST_REGION + max_steps(D) * 4;
   static constexpr int LDS_BYTES = RING_BYTES > PART_BYTES ? RING_BYTES : PART_BYTES;
+  static_assert(max_steps(D) <= 65536 && LDS_BYTES <= 163840 - 1024, "16 bits, 160 KB");
 };
-
-// Steps of a chunk at most; an entry of the list is the step's number, and two bits
-// for each of its 32-row halves and 32-key blocks (bit 16 + 2 (4 half + block)): 0
-// nobody sees anything, 1 mask, 2 everybody sees everything.
-constexpr int kMaxSteps = 1024;
-constexpr int kMaxChunkRows = kMaxSteps * kQM;
 
 template <int D, bool CAP, bool BIAS>
 __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char *smem,
-                                         uint32_t *list, int *counts) {
+                                         int *counts) {
   using C = KvCfg<D>;
   using T = LdsTile<C::LW>;
+  uint32_t *list = reinterpret_cast<uint32_t *>(smem + C::LIST_REGION);
   constexpr int kDoRegion = C::DO_REGION, kAuxRegion = C::AUX_REGION, kKvRegion = C::KV_REGION;
   const int S = a.s.S, Sp = a.Sp, Hl = a.s.Hl, Hkl = a.s.Hkl, n_rep = Hl / Hkl;
   const int kvheads_total = a.s.b * Hkl;
@@ -897,13 +901,12 @@ template <int D, int R, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 1) void span_main_kernel(const BwdArgs a) {
   constexpr int kKvLds = KvCfg<D>::LDS_BYTES, kDqLds = DqCfg<D, R>::LDS_BYTES;
   __shared__ __attribute__((aligned(16))) unsigned char smem[kKvLds > kDqLds ? kKvLds : kDqLds];
-  __shared__ uint32_t list[kMaxSteps];
   __shared__ int scratch[2 * kWaves];
   const uint32_t kv_blocks = gridDim.x - a.dq_blocks;
   const uint32_t first = a.keys_first ? kv_blocks : a.dq_blocks;
   const uint32_t i = blockIdx.x < first ? blockIdx.x : blockIdx.x - first;
   if ((blockIdx.x < first) == (a.keys_first != 0))  // workgroup-uniform
-    key_unit<D, CAP, BIAS>(a, (int)i, smem, list, scratch);
+    key_unit<D, CAP, BIAS>(a, (int)i, smem, scratch);
   else
     dq_tile<D, R, CAP, BIAS>(a, (int)i, smem, scratch);
 }
@@ -925,7 +928,7 @@ struct SpanCut {
 SpanCut span_cut(const SpanArgs &s) {
   const BwdChunks ck = bwd_chunks(shape_of(s, (size_t)-1));
   SpanCut c;
-  c.chunk_rows = ck.rows < kMaxChunkRows ? ck.rows : kMaxChunkRows;
+  c.chunk_rows = ck.rows;
   c.nchunks = (s.S + c.chunk_rows - 1) / c.chunk_rows;
   c.nsplits = ck.splits;
   c.ktiles = (s.S + kKN - 1) / kKN;
@@ -966,8 +969,9 @@ long long key_blocks(const SpanArgs &s, const SpanCut &ck) {
 size_t span_bwd_workspace_bytes(const SpanArgs &s) { return span_cut(s).bytes; }
 
 bool span_bwd_fits(const SpanArgs &s) {
-  return (dq_blocks_of(s) + key_blocks(s, span_cut(s))) * kThreads <=
-         0xFFFFFFFFll;
+  const SpanCut ck = span_cut(s);
+  return (dq_blocks_of(s) + key_blocks(s, ck)) * kThreads <= 0xFFFFFFFFll &&
+         ck.chunk_rows <= max_steps(s.d) * kQM;
 }
 
 hipError_t launch_span_bwd(const SpanArgs &s, const uint16_t *o, const float *lse,
