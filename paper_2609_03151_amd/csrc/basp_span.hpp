@@ -39,10 +39,78 @@ struct SpanArgs {
   float scale, cap;     // cap 0: none
 };
 
-// The backward's: planes of -LSE and -D, the rows' hulls, which units of the key
-// pass saw anything, and their partial sums of dK and dV.
-size_t span_bwd_workspace_bytes(const SpanArgs &s);
-bool span_bwd_fits(const SpanArgs &s);  // its workgroups in one launch, a unit's steps in LDS
+// ------------------------------------------------ how the backward is cut
+constexpr int kSpanThreads = 512;   // of a workgroup of either pass
+constexpr int kSpanStep = 64;       // rows of a step of the key pass
+constexpr int kSpanHullBytes = 16;  // of the hull of 32 rows' spans
+
+// Steps of a chunk at most: a sixteenth of the longest sequence (a row of d elements takes
+// 2 d of its 2^31 bytes), rounded up to whole key tiles.  A unit lists them in LDS.
+constexpr int span_max_steps(int d) { return (1 << 20) / d + 2; }
+
+inline AttnShape span_shape(const SpanArgs &s, size_t workspace_bytes) {
+  AttnShape x{s.b, s.S, s.Hl, s.Hkl, s.d, s.scale};
+  x.workspace_bytes = workspace_bytes;
+  return x;
+}
+
+// How the key pass is cut, and where things lie in the workspace.
+struct SpanCut {
+  int chunk_rows, nchunks, nsplits, ktiles, Sp;
+  size_t rows, hulls, touched, parts, bytes;  // byte offsets, aux at 0
+};
+
+inline SpanCut span_cut(const SpanArgs &s) {
+  auto align256 = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const BwdChunks ck = bwd_chunks(span_shape(s, (size_t)-1));
+  SpanCut c;
+  c.chunk_rows = ck.rows;
+  c.nchunks = (s.S + c.chunk_rows - 1) / c.chunk_rows;
+  c.nsplits = ck.splits;
+  c.ktiles = (s.S + kKvKeys - 1) / kKvKeys;
+  c.Sp = bwd_plane_rows(s.S);
+  c.rows = align256((size_t)s.b * s.Hl * c.Sp * 2 * sizeof(float));
+  c.hulls = align256(c.rows + (size_t)s.b * c.Sp * 2 * sizeof(int));
+  c.touched = align256(c.hulls + (size_t)s.b * c.Sp / 32 * kSpanHullBytes);
+  const size_t slots = (size_t)c.nchunks * c.nsplits;
+  c.parts = align256(c.touched + slots * s.b * s.Hkl * c.ktiles * sizeof(int));
+  c.bytes = c.parts;
+  if (slots > 1) c.bytes += 2 * slots * s.b * s.S * s.Hkl * s.d * sizeof(float);
+  return c;
+}
+
+// Row groups of the dQ pass: the causal backward's rule, but with spans 128 rows a
+// workgroup up to 96K query rows: documents make workgroups of very different
+// lengths, and twice as many of half the length even out better (42K rows, d = 80,
+// documents of 1200 tokens: 123 -> 115 us; 128K rows of documents of 2048: 419, 421).
+inline int span_row_groups(const SpanArgs &s) {
+  const int R = dq_row_groups(span_shape(s, (size_t)-1));
+  return R == 8 && s.spans && (long long)s.b * s.Hl * s.S <= 98304 ? 4 : R;
+}
+inline long long span_dq_blocks(const SpanArgs &s) {
+  const int rows = 32 * span_row_groups(s);
+  return (long long)((s.S + rows - 1) / rows) * s.b * s.Hl;
+}
+
+// Workgroups of the key pass: (key tile, row chunk) pairs with rows at or after the
+// keys first, then, with spans, those of rows before the keys.
+inline long long span_key_blocks(const SpanArgs &s, const SpanCut &ck) {
+  const long long pairs = kv_units(ck.nchunks, ck.chunk_rows / kKvKeys) +
+                          (s.spans ? (long long)ck.nchunks * ck.ktiles : 0);
+  return pairs * ck.nsplits * s.b * s.Hkl;
+}
+
+// Planes of -LSE and -D, the rows' spans and hulls, which units of the key pass saw
+// anything, and their partial sums of dK and dV.
+inline size_t span_bwd_workspace_bytes(const SpanArgs &s) { return span_cut(s).bytes; }
+
+// Its workgroups in one launch, and a unit's steps in LDS.
+inline bool span_bwd_fits(const SpanArgs &s) {
+  const SpanCut ck = span_cut(s);
+  return (span_dq_blocks(s) + span_key_blocks(s, ck)) * kSpanThreads <= 0xFFFFFFFFll &&
+         ck.chunk_rows <= span_max_steps(s.d) * kSpanStep;
+}
+
 hipError_t launch_span_bwd(const SpanArgs &s, const uint16_t *o, const float *lse,
                            const uint16_t *d_o, void *dq, void *dk, void *dv, bool grad_bf16,
                            void *workspace, hipStream_t stream);

@@ -30,10 +30,10 @@ namespace basp {
 namespace {
 
 constexpr int kPreThreads = 256;
-constexpr int kThreads = 512;
-constexpr int kWaves = 8;
+constexpr int kThreads = kSpanThreads;
+constexpr int kWaves = kThreads / 64;
 constexpr int kKN = kKvKeys;     // keys of a key pass unit: 32 per pair of waves
-constexpr int kQM = 64;          // rows of its step
+constexpr int kQM = kSpanStep;   // rows of its step
 constexpr int kSchedMfma = 0x008;
 constexpr int kSchedDsRead = 0x100;
 
@@ -49,6 +49,8 @@ __device__ __forceinline__ void sched_reads_ahead() {
   }
   __builtin_amdgcn_sched_group_barrier(kSchedMfma, A / R, 0);
 }
+
+static_assert(sizeof(SpanHull) == kSpanHullBytes, "the workspace's");
 
 struct BwdArgs {
   SpanArgs s;
@@ -155,10 +157,6 @@ __global__ __launch_bounds__(kPreThreads) void span_pre_kernel(const BwdArgs a,
 // An entry of the list of steps is the step's number, and two bits for each of its
 // 32-row halves and 32-key blocks (bit 16 + 2 (4 half + block)): 0 nobody sees anything,
 // 1 mask, 2 everybody sees everything.
-// Steps of a chunk at most: a sixteenth of the longest sequence (a row of D elements takes
-// 2 D of its 2^31 bytes), rounded up to whole key tiles.
-constexpr int max_steps(int d) { return (1 << 20) / d + 2; }
-
 template <int D>
 struct KvCfg {
   static constexpr int DC = HeadDim<D>::DC;
@@ -181,9 +179,9 @@ struct KvCfg {
   static constexpr int KV_REGION = AUX_REGION + 2 * AUX_BYTES;
   static constexpr int PART_BYTES = kWaves / 2 * 2 * NE * 4 * 1024;
   static constexpr int LIST_REGION = KV_REGION + (V_REGS ? 0 : KT_BYTES);
-  static constexpr int RING_BYTES = LIST_REGION + max_steps(D) * 4;
+  static constexpr int RING_BYTES = LIST_REGION + span_max_steps(D) * 4;
   static constexpr int LDS_BYTES = RING_BYTES > PART_BYTES ? RING_BYTES : PART_BYTES;
-  static_assert(max_steps(D) <= 65536 && LDS_BYTES <= 163840 - 1024, "16 bits, 160 KB");
+  static_assert(span_max_steps(D) <= 65536 && LDS_BYTES <= 163840 - 1024, "16 bits, 160 KB");
 };
 
 template <int D, bool CAP, bool BIAS>
@@ -911,68 +909,7 @@ __global__ __launch_bounds__(kThreads, 1) void span_main_kernel(const BwdArgs a)
     dq_tile<D, R, CAP, BIAS>(a, (int)i, smem, scratch);
 }
 
-AttnShape shape_of(const SpanArgs &s, size_t workspace_bytes) {
-  AttnShape x{s.b, s.S, s.Hl, s.Hkl, s.d, s.scale};
-  x.workspace_bytes = workspace_bytes;
-  return x;
-}
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// How the key pass is cut, and where things lie in the workspace.
-struct SpanCut {
-  int chunk_rows, nchunks, nsplits, ktiles, Sp;
-  size_t rows, hulls, touched, parts, bytes;  // byte offsets, aux at 0
-};
-
-SpanCut span_cut(const SpanArgs &s) {
-  const BwdChunks ck = bwd_chunks(shape_of(s, (size_t)-1));
-  SpanCut c;
-  c.chunk_rows = ck.rows;
-  c.nchunks = (s.S + c.chunk_rows - 1) / c.chunk_rows;
-  c.nsplits = ck.splits;
-  c.ktiles = (s.S + kKN - 1) / kKN;
-  c.Sp = bwd_plane_rows(s.S);
-  c.rows = align256((size_t)s.b * s.Hl * c.Sp * 2 * sizeof(float));
-  c.hulls = align256(c.rows + (size_t)s.b * c.Sp * 2 * sizeof(int));
-  c.touched = align256(c.hulls + (size_t)s.b * c.Sp / 32 * sizeof(SpanHull));
-  const size_t slots = (size_t)c.nchunks * c.nsplits;
-  c.parts = align256(c.touched + slots * s.b * s.Hkl * c.ktiles * sizeof(int));
-  c.bytes = c.parts;
-  if (slots > 1) c.bytes += 2 * slots * s.b * s.S * s.Hkl * s.d * sizeof(float);
-  return c;
-}
-
-// Row groups of the dQ pass: the causal backward's rule, but with spans 128 rows a
-// workgroup up to 96K query rows: documents make workgroups of very different
-// lengths, and twice as many of half the length even out better (42K rows, d = 80,
-// documents of 1200 tokens: 123 -> 115 us; 128K rows of documents of 2048: 419, 421).
-int row_groups(const SpanArgs &s) {
-  const int R = dq_row_groups(shape_of(s, (size_t)-1));
-  return R == 8 && s.spans && (long long)s.b * s.Hl * s.S <= 98304 ? 4 : R;
-}
-long long dq_blocks_of(const SpanArgs &s) {
-  const int rows = 32 * row_groups(s);
-  return (long long)((s.S + rows - 1) / rows) * s.b * s.Hl;
-}
-
-// Workgroups of the key pass: (key tile, row chunk) pairs with rows at or after the
-// keys first, then, with spans, those of rows before the keys.
-long long key_blocks(const SpanArgs &s, const SpanCut &ck) {
-  const long long pairs = kv_units(ck.nchunks, ck.chunk_rows / kKN) +
-                          (s.spans ? (long long)ck.nchunks * ck.ktiles : 0);
-  return pairs * ck.nsplits * s.b * s.Hkl;
-}
-
 }  // namespace
-
-size_t span_bwd_workspace_bytes(const SpanArgs &s) { return span_cut(s).bytes; }
-
-bool span_bwd_fits(const SpanArgs &s) {
-  const SpanCut ck = span_cut(s);
-  return (dq_blocks_of(s) + key_blocks(s, ck)) * kThreads <= 0xFFFFFFFFll &&
-         ck.chunk_rows <= max_steps(s.d) * kQM;
-}
 
 hipError_t launch_span_bwd(const SpanArgs &s, const uint16_t *o, const float *lse,
                            const uint16_t *d_o, void *dq, void *dk, void *dv, bool grad_bf16,
@@ -1000,9 +937,9 @@ hipError_t launch_span_bwd(const SpanArgs &s, const uint16_t *o, const float *ls
   }
   const int T128 = ck.chunk_rows / kKN;
   a.causal_units = (uint32_t)kv_units(ck.nchunks, T128);
-  const int R = row_groups(s);
-  a.dq_blocks = (uint32_t)dq_blocks_of(s);
-  const uint32_t kv_blocks = (uint32_t)key_blocks(s, ck);
+  const int R = span_row_groups(s);
+  a.dq_blocks = (uint32_t)span_dq_blocks(s);
+  const uint32_t kv_blocks = (uint32_t)span_key_blocks(s, ck);
   {
     const int n_rep = s.Hl / s.Hkl;
     const long long unit = (long long)(ck.chunk_rows / 64) * ((n_rep + ck.nsplits - 1) / ck.nsplits);
