@@ -189,7 +189,8 @@ struct State {
 struct KeyRule {
   bool capped;
   float c1, cap2;  // of cap_r; the cap in log2 units
-  float at;        // the query's position
+  int at;          // the query's position; distances are taken in whole numbers, since fp32 does
+                   // not hold positions past 2^24
   int lo;          // its first key
 };
 
@@ -203,6 +204,7 @@ __device__ __forceinline__ void weights(const Block<D, E4M3> &b, State<Block<D, 
   using B = Block<D, E4M3>;
   const int c = threadIdx.x % 64 / 16;
   float s[kTiles][4];
+  const float away = RULE ? (float)(rule.at - (t0 + 4 * c)) : 0.f;  // the lane's first key
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -225,7 +227,7 @@ __device__ __forceinline__ void weights(const Block<D, E4M3> &b, State<Block<D, 
         float x = acc[r];
         if constexpr (E4M3) x *= pow2_of_byte(b.ks[t], r);
         x = rule.capped ? fmaf(cap_r(x, rule.c1), -2.f * rule.cap2, rule.cap2) : x * scale2;
-        s[t][r] = fmaf(-sl, rule.at - (float)(t0 + 16 * t + 4 * c + r), x);
+        s[t][r] = fmaf(-sl, away - (float)(16 * t + r), x);
       } else {
         s[t][r] = acc[r] * scale2;
         if constexpr (E4M3) s[t][r] *= pow2_of_byte(b.ks[t], r);

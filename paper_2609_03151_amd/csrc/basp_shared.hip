@@ -333,7 +333,7 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
       qf[s] = as_bf16x8(v);
     }
   }
-  const float at = live ? (float)(a.d.lens[seq] - 1) : 0.f;
+  const int at = live ? a.d.lens[seq] - 1 : 0;
   const float sl = a.slopes && live ? a.slopes[head] * kLog2e : 0.f;
   const float c2 = a.d.scale * kLog2e;
   const bool capped = a.cap > 0.f;
@@ -443,7 +443,7 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
                           s == 0 ? f32x16{} : sc);
       // sc[r] = (q . k) of key jl + 8(r/4) + r%4 for this lane's row
       const int jl = t * kSharedTile + 32 * (C::KM * part + m) + 4 * hh;
-      const float away = at - (float)jl;
+      const float away = (float)(at - jl);
       if (capped) {  // workgroup-uniform, as the next
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = fmaf(cap_r(sc[r], c1), -2.f * cap2, cap2);
@@ -452,9 +452,9 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
         for (int r = 0; r < 16; ++r) sc[r] *= c2;
     }
     if (a.slopes) {
-      const float base = -sl * away;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] += fmaf(sl, (float)(8 * (r >> 2) + (r & 3)), base);
+      for (int r = 0; r < 16; ++r)
+        sc[r] = fmaf(-sl, away - (float)(8 * (r >> 2) + (r & 3)), sc[r]);
     }
     if (jl - 4 * hh + 32 > prefix) {  // wave-uniform: the last tile
 #pragma unroll
@@ -668,7 +668,7 @@ __device__ void own_unit(const SharedArgs &a, const SharedCut &c, int g, unsigne
     const int heads = rep - grp * kRows < kRows ? rep - grp * kRows : kRows;
     pg.table = d.table + (size_t)seq * d.s.max_pages;
     pg.kvh = kvh;
-    rule.at = (float)(len - 1);
+    rule.at = len - 1;
     rule.lo = start;
 
     int t = lo + wave * kBlockKeys;
