@@ -599,9 +599,9 @@ int basp_attn_decode_shared(const void *q, const void *k_pages, const void *v_pa
  * n_q a multiple of n_k, query head h takes kv head h / (n_q/n_k).
  * Products in bf16 with fp32 accumulation (P and dS rounded to bf16 for their
  * products), softmax in fp32; deterministic.  tanh is off by at most 2^-21, so a capped
- * score by 2^-21 * cap; a bias and an LSE are fp32 numbers, off by 2^-24 of
- * themselves: rows all of whose keys are far away, |slope * distance| past 2^12, see that in
- * P.  Values of up to 2^96 in magnitude do not overflow on the way to O, whatever the scores.
+ * score by 2^-21 * cap; a bias and an LSE are fp32 numbers, off by some 2^-24 of
+ * themselves (a bias, more than 32 tokens away, of that of a key 64 tokens farther): rows all
+ * of whose keys are far away, |slope * distance| past 2^12, see that in P.  Values of up to 2^96 in magnitude do not overflow on the way to O, whatever the scores.
  * A value, key, query or gradient outside every span that it would meet does not
  * count, infinities and NaN too; inside one they make what they reach NaN: a value
  * its element of O, a score of plus infinity or NaN its row.

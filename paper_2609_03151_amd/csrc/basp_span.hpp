@@ -43,6 +43,7 @@ struct SpanArgs {
 constexpr int kSpanThreads = 512;   // of a workgroup of either pass
 constexpr int kSpanStep = 64;       // rows of a step of the key pass
 constexpr int kSpanHullBytes = 16;  // of the hull of 32 rows' spans
+constexpr int kSpanPlanes = 4;      // numbers kept of a row and head, and of a row, with slopes
 
 // Steps of a chunk at most: a sixteenth of the longest sequence (a row of d elements takes
 // 2 d of its 2^31 bytes), rounded up to whole key tiles.  A unit lists them in LDS.
@@ -69,8 +70,8 @@ inline SpanCut span_cut(const SpanArgs &s) {
   c.nsplits = ck.splits;
   c.ktiles = (s.S + kKvKeys - 1) / kKvKeys;
   c.Sp = bwd_plane_rows(s.S);
-  c.rows = align256((size_t)s.b * s.Hl * c.Sp * 2 * sizeof(float));
-  c.hulls = align256(c.rows + (size_t)s.b * c.Sp * 2 * sizeof(int));
+  c.rows = align256((size_t)s.b * s.Hl * c.Sp * kSpanPlanes * sizeof(float));
+  c.hulls = align256(c.rows + (size_t)s.b * c.Sp * kSpanPlanes * sizeof(int));
   c.touched = align256(c.hulls + (size_t)s.b * c.Sp / 32 * kSpanHullBytes);
   const size_t slots = (size_t)c.nchunks * c.nsplits;
   c.parts = align256(c.touched + slots * s.b * s.Hkl * c.ktiles * sizeof(int));
@@ -100,7 +101,7 @@ inline long long span_key_blocks(const SpanArgs &s, const SpanCut &ck) {
   return pairs * ck.nsplits * s.b * s.Hkl;
 }
 
-// Planes of -LSE and -D, the rows' spans and hulls, which units of the key pass saw
+// Planes of -LSE (with slopes two) and -D, the rows' spans and hulls, which units of the key pass saw
 // anything, and their partial sums of dK and dV.
 inline size_t span_bwd_workspace_bytes(const SpanArgs &s) { return span_cut(s).bytes; }
 

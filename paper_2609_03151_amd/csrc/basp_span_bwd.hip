@@ -56,8 +56,8 @@ struct BwdArgs {
   SpanArgs s;
   const uint16_t *d_o;
   const float *lse;
-  float *aux;              // [b][Hl][Sp / 64][2][64]: -LSE, then -D, of 64 rows
-  int *rows;               // [b][Sp][2]: lo and hi, in order
+  float *aux;              // [b][Hl][Sp / 64][kPlanes][64]: what span_pre says of 64 rows
+  int *rows;               // [b][Sp][kPlanes]: lo and hi
   const SpanHull *hulls;   // [b][Sp / 32]
   int *touched;            // [slot][b][ktiles], or NULL: dk, dv written by the units
   void *dq, *dk, *dv;      // outputs
@@ -67,6 +67,12 @@ struct BwdArgs {
   int Sp, chunk_rows, nchunks, nsplits, ktiles;
   uint32_t dq_blocks, pre_rows_blocks, causal_units, keys_first;
 };
+
+// Planes of 64 rows: -LSE, then -D, and with slopes -LSE without the rows' part of the bias
+// and an empty one: a step's planes, and its spans, so are copies of a kilobyte (three
+// planes were some 5% slower at d = 96 and 64, for scalar registers that the sizes took).
+template <bool BIAS>
+constexpr int kPlanes = BIAS ? kSpanPlanes : 2;
 
 // Four consecutive gradients, in the output's type.
 __device__ __forceinline__ void store4(void *p, size_t elem, f32x4 x, int bf16) {
@@ -92,8 +98,10 @@ __device__ __forceinline__ void pack16(const f32x16 &x, bf16x8 (&out)[2]) {
 // padded rows, 16-byte loads of O and dO:
 //   -(LSE log2(e) + slope' (i % 64)) / c   (not divided with a cap), and -D_i
 // c = scale log2(e), slope' = slope log2(e): with the rows' part of the bias in it, the
-// key pass adds one number per step and key.  Rows that see nothing, and those past
-// S, have -inf: P = 0.  The other blocks: a wave per 64 rows, their spans and two hulls.
+// key pass adds one number per step and key where all keys lie before the rows.  Elsewhere
+// it starts from -LSE / c alone, of which steep slopes would leave nothing.  Rows that
+// see nothing, and those past S, have -inf: P = 0.  The other blocks: a wave per 64 rows,
+// their spans and two hulls.
 template <int D, bool CAP>
 __global__ __launch_bounds__(kPreThreads) void span_pre_kernel(const BwdArgs a,
                                                                const uint16_t *__restrict__ o,
@@ -108,7 +116,8 @@ __global__ __launch_bounds__(kPreThreads) void span_pre_kernel(const BwdArgs a,
     const int beta = (int)(step / per_seq), row = (int)(step % per_seq) * 64 + lane;
     int lo = 0, hi = 0;
     if (row < S) span_of(a.s.spans, beta, S, row, lo, hi);
-    *reinterpret_cast<u32x2 *>(a.rows + ((size_t)beta * Sp + row) * 2) =
+    *reinterpret_cast<u32x2 *>(a.rows + ((size_t)beta * Sp + row) *
+                                            (a.s.slopes ? kPlanes<true> : kPlanes<false>)) =
         u32x2{(uint32_t)lo, (uint32_t)hi};
     SpanHull h = hull_of(lo, hi, row < S);
 #pragma unroll
@@ -142,15 +151,17 @@ __global__ __launch_bounds__(kPreThreads) void span_pre_kernel(const BwdArgs a,
   int lo = 0, hi = 0;
   if (i < S) span_of(a.s.spans, beta, S, i, lo, hi);
   const size_t row = (size_t)beta * Hl + h;
-  float l = -INFINITY;
+  float l = -INFINITY, alone = -INFINITY;
   if (hi > lo) {
-    l = -a.lse[row * S + i] * kSpanLog2e;
+    l = alone = -a.lse[row * S + i] * kSpanLog2e;
     if (a.s.slopes) l = fmaf(-a.s.slopes[h] * kSpanLog2e, (float)(i % 64), l);
-    if (!CAP) l /= a.s.scale * kSpanLog2e;
+    if (!CAP) l /= a.s.scale * kSpanLog2e, alone /= a.s.scale * kSpanLog2e;
   }
-  float *aux = a.aux + (row * Sp + i / 64 * 64) * 2 + i % 64;
+  float *aux = a.aux + (row * Sp + i / 64 * 64) * (a.s.slopes ? kPlanes<true> : kPlanes<false>) +
+               i % 64;
   aux[0] = l;
   aux[64] = i < S ? -acc : 0.f;
+  if (a.s.slopes) aux[128] = alone;
 }
 
 // ---------------------------------------------------------------- key pass
@@ -163,7 +174,7 @@ struct KvCfg {
   static constexpr int LW = HeadDim<D>::LW;
   static constexpr int TILE_BYTES = kQM * LW * 2;   // a step's Q or dO rows
   static constexpr int KT_BYTES = kKN * LW * 2;     // the workgroup's V rows
-  // -LSE, then -D, of the step's rows, and from byte 1024 on their spans
+  // the planes of the step's rows, and from byte 1024 on their spans
   static constexpr int AUX_BYTES = 2048;
   static constexpr int NS = D / 16;
   static constexpr int NE = DC / 32;
@@ -336,8 +347,9 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
     asm volatile("" : "+v"(aux_lane));
   };
 
-  // Copies of step s of the head whose resources are at hand.  Wave 0 copies
-  // the rows' -LSE and -D, wave 1 their spans: 512 bytes of either.
+  // Copies of step s of the head whose resources are at hand.  Wave 0 copies the
+  // rows' planes, wave 1 their spans.
+  constexpr uint32_t kAuxBytes = 256 * kPlanes<BIAS>;
   u32x4 rq, rd, ra;
   float sl = 0.f;
   auto head_resources = [&](int hq) __attribute__((always_inline)) {
@@ -346,10 +358,11 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
     rd = make_rsrc_words(a.d_o + (((size_t)beta * S + r_lo) * Hl + hq) * D,
                          (uint32_t)(S - r_lo) * do_row_bytes);
     if (w == 0)
-      ra = make_rsrc_words(a.aux + (((size_t)beta * Hl + hq) * Sp + r_lo) * 2,
-                           (uint32_t)(Sp - r_lo) * 8);
+      ra = make_rsrc_words(a.aux + (((size_t)beta * Hl + hq) * Sp + r_lo) * kPlanes<BIAS>,
+                           (uint32_t)(Sp - r_lo) * 4 * kPlanes<BIAS>);
     else
-      ra = make_rsrc_words(a.rows + ((size_t)beta * Sp + r_lo) * 2, (uint32_t)(Sp - r_lo) * 8);
+      ra = make_rsrc_words(a.rows + ((size_t)beta * Sp + r_lo) * kPlanes<BIAS>,
+                           (uint32_t)(Sp - r_lo) * 4 * kPlanes<BIAS>);
   };
   auto load_step = [&](int st, uint32_t s) __attribute__((always_inline)) {
     const uint32_t sq = (uint32_t)st & 1;
@@ -362,7 +375,7 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
       copy16_to_lds(rd, src.off(i, do_row_bytes) + db, lds + kDoRegion);
     }
     if (w < 2)
-      copy16_to_lds(ra, (lane < 32 ? 16u * lane : kZeroOffset) + s * kQM * 8,
+      copy16_to_lds(ra, (16u * lane < kAuxBytes ? 16u * lane : kZeroOffset) + s * kAuxBytes,
                            smem_lds + kAuxRegion + sq * C::AUX_BYTES + 1024 * w);
   };
   auto aux_rows = [&](int stg, int which) __attribute__((always_inline)) {
@@ -391,7 +404,7 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
       const f32x16 negd = aux_rows(stg, 1);
       f32x16 neglse;
       if constexpr (CAP) neglse = f32x16{};
-      else neglse = aux_rows(stg, 0);
+      else neglse = aux_rows(stg, BIAS && edge ? 2 : 0);
 #pragma unroll
       for (int s = 0; s < C::NS; ++s) {
         const bf16x8 aq = *reinterpret_cast<const bf16x8 *>(Qs + a_off[s]);
@@ -408,21 +421,22 @@ __device__ __forceinline__ void key_unit(const BwdArgs &a, int L, unsigned char 
     u32x4 seen[2] = {{kOnes, kOnes, kOnes, kOnes}, {kOnes, kOnes, kOnes, kOnes}};
     {
       f32x16 neglse;
-      if constexpr (CAP) neglse = aux_rows(stg, 0);
+      if constexpr (CAP) neglse = aux_rows(stg, BIAS && edge ? 2 : 0);
       // row0: first row of the wave's half
       float base = BIAS ? sl * (float)(key - (row0 - 32 * h)) : 0.f;
       if (edge) {  // wave-uniform
         asm volatile("" ::: "memory");
-        const float ahead = (float)(row0 + 4 * hh - key), in64 = (float)(32 * h + 4 * hh);
-        const unsigned char *spans = smem + stg * C::AUX_BYTES + kAuxRegion + 1024 + 8 * 32 * h +
-                                     8 * 4 * hh;
+        const float ahead = (float)(row0 + 4 * hh - key);
+        constexpr int kRow = 4 * kPlanes<BIAS>;
+        const unsigned char *spans = smem + stg * C::AUX_BYTES + kAuxRegion + 1024 + kRow * 32 * h +
+                                     kRow * 4 * hh;
         base = 0.f;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int io = 8 * (r >> 2) + (r & 3);
-          const u32x2 span = *reinterpret_cast<const u32x2 *>(spans + 8 * io);
+          const u32x2 span = *reinterpret_cast<const u32x2 *>(spans + kRow * io);
           const bool vis = key - span.x < span.y - span.x;
-          const float bias = BIAS ? (in64 + (float)io) - fabsf(ahead + (float)io) : 0.f;
+          const float bias = BIAS ? -fabsf(ahead + (float)io) : 0.f;
           if constexpr (CAP) {
             neglse[r] = vis ? fmaf(sl, bias, neglse[r]) : -INFINITY;
             sacc[r] = vis ? sacc[r] : 0.f;
@@ -652,7 +666,8 @@ __device__ __forceinline__ void dq_tile(const BwdArgs &a, int L, unsigned char *
   if (row < S) {
     span_of(a.s.spans, beta, S, row, lo, hi);
     if (hi > lo) nlse = -a.lse[((size_t)beta * Hl + h) * S + row] * kSpanLog2e;
-    nd = a.aux[(((size_t)beta * Hl + h) * a.Sp + row / 64 * 64) * 2 + 64 + row % 64];
+    nd = a.aux[(((size_t)beta * Hl + h) * a.Sp + row / 64 * 64) * kPlanes<BIAS> + 64 +
+               row % 64];
   }
   float sl = 0.f;
   if constexpr (BIAS) sl = a.s.slopes[h] * kSpanLog2e;
