@@ -561,6 +561,9 @@ size_t basp_attn_decode_shared_workspace_bytes(int b, int n_q, int n_k, int d, i
  * tokens through the first such sequence's row of the table.  Shorter sequences of the
  * group and sequences in no group are read by themselves; results are then those of
  * basp_attn_decode, but for rounding (the weights of a shared prefix are one bf16).
+ * How the prefixes' keys are divided among workgroups goes by b, n_groups and max_len, not by
+ * their lengths: prefixes of like length are what it is made for.  One of 32K tokens named
+ * among 127 of 64 takes nine times as long as named alone, or as nothing named.
  * n_groups 0: groups and prefix_lens are not read.  Arrays that are not as described
  * give other results, no access outside the buffers.
  * Arguments, layouts, empty slots, bad pages, NaN and infinities as basp_attn_decode;
@@ -600,8 +603,8 @@ int basp_attn_decode_shared(const void *q, const void *k_pages, const void *v_pa
  * Products in bf16 with fp32 accumulation (P and dS rounded to bf16 for their
  * products), softmax in fp32; deterministic.  tanh is off by at most 2^-21, so a capped
  * score by 2^-21 * cap; a bias and an LSE are fp32 numbers, off by some 2^-24 of
- * themselves (a bias, more than 32 tokens away, of that of a key 64 tokens farther): rows all
- * of whose keys are far away, |slope * distance| past 2^12, see that in P.  Values of up to 2^96 in magnitude do not overflow on the way to O, whatever the scores.
+ * themselves (the bias of a key in another tile than its row, of one 128 tokens farther):
+ * rows all of whose keys are far away, |slope * distance| past 2^12, see that in P.  Values of up to 2^96 in magnitude do not overflow on the way to O, whatever the scores.
  * A value, key, query or gradient outside every span that it would meet does not
  * count, infinities and NaN too; inside one they make what they reach NaN: a value
  * its element of O, a score of plus infinity or NaN its row.

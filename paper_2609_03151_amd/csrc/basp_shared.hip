@@ -10,8 +10,8 @@
 // tokens, 8 heads on 2 of 128: 21.5 us, 8 of them dependent loads, 11 tiles, 5 the join
 // (its bytes alone take 6.7); read sequence by sequence the prompt would be 0.5 GB.
 //
-//   shared_plan   which sequences share, and where their rows go (many sequences; else each
-//                 workgroup of the next kernel finds out by itself)
+//   shared_plan   which sequences share, and where their rows go (past 512 sequences or 128
+//                 groups; else each workgroup of the next kernel finds out by itself)
 //   shared_main   prefix workgroups: 64 or 128 rows of a group and kv head times a
 //                 split of the prefix's keys, as the causal forward's (S^T = K Q^T, O^T =
 //                 V^T P^T on v_mfma_f32_32x32x16_bf16, K and V through LDS, widened to bf16
@@ -450,59 +450,60 @@ __device__ void prefix_unit(const SharedArgs &a, const SharedCut &c, unsigned ch
       } else {
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] *= c2;
-    }
-    if (a.slopes) {
+      }
+      if (a.slopes) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        sc[r] = fmaf(-sl, away - (float)(8 * (r >> 2) + (r & 3)), sc[r]);
-    }
-    if (jl - 4 * hh + 32 > prefix) {  // wave-uniform: the last tile
+        for (int r = 0; r < 16; ++r)
+          sc[r] = fmaf(-sl, away - (float)(8 * (r >> 2) + (r & 3)), sc[r]);
+      }
+      if (jl - 4 * hh + 32 > prefix) {  // wave-uniform: the last tile
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (jl + 8 * (r >> 2) + (r & 3) >= prefix) sc[r] = -INFINITY;
-    }
-    // Against a running maximum with a cap too: that bounds the scores, but with a reference
-    // that stands still P lies in 2^(+-92) at a cap of 64, too wide for its products with V,
-    // and a weight alone in its row is rounded (64 sequences on one prompt of 32K, 8 heads on
-    // 1, a cap of 50: 37.2 us standing still, 35.8).
-    float mx = -INFINITY;
+        for (int r = 0; r < 16; ++r)
+          if (jl + 8 * (r >> 2) + (r & 3) >= prefix) sc[r] = -INFINITY;
+      }
+      // Against a running maximum with a cap too: that bounds the scores, but with a reference
+      // that stands still P lies in 2^(+-92) at a cap of 64, too wide for its products with V,
+      // and a weight alone in its row is rounded (64 sequences on one prompt of 32K, 8 heads on
+      // 1, a cap of 50: 37.2 us standing still, 35.8).
+      float mx = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-    mx = pair_max(mx);
-    const bool grow = mx > m_ref + kRescaleSlack;
-    if (__builtin_amdgcn_ballot_w64(grow)) {  // wave-uniform, rare after the first tiles
-      asm volatile("" ::: "memory");
-      const float alpha = grow ? fast_exp2(m_ref - mx) : 1.f;
-      m_ref = grow ? mx : m_ref;
-      l_run *= alpha;
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+      mx = pair_max(mx);
+      const bool grow = mx > m_ref + kRescaleSlack;
+      if (__builtin_amdgcn_ballot_w64(grow)) {  // wave-uniform, rare after the first tiles
+        asm volatile("" ::: "memory");
+        const float alpha = grow ? fast_exp2(m_ref - mx) : 1.f;
+        m_ref = grow ? mx : m_ref;
+        l_run *= alpha;
+#pragma unroll
+        for (int n = 0; n < C::NE; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[n][r] *= alpha;
+      }
+      const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+      float psum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sc[r] = fast_exp2(sc[r] - m_use);
+        psum += sc[r];
+      }
+      l_run += psum;
+      bf16x8 pf[2];
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const int b8 = 8 * s2;
+        pf[s2] = as_bf16x8(
+            u32x4{pack_bf16x2(sc[b8 + 0], sc[b8 + 1]), pack_bf16x2(sc[b8 + 2], sc[b8 + 3]),
+                  pack_bf16x2(sc[b8 + 4], sc[b8 + 5]), pack_bf16x2(sc[b8 + 6], sc[b8 + 7])});
+      }
 #pragma unroll
       for (int n = 0; n < C::NE; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[n][r] *= alpha;
-    }
-    const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-    float psum = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      sc[r] = fast_exp2(sc[r] - m_use);
-      psum += sc[r];
-    }
-    l_run += psum;
-    bf16x8 pf[2];
-#pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2) {
-      const int b8 = 8 * s2;
-      pf[s2] = as_bf16x8(u32x4{pack_bf16x2(sc[b8 + 0], sc[b8 + 1]), pack_bf16x2(sc[b8 + 2], sc[b8 + 3]),
-                               pack_bf16x2(sc[b8 + 4], sc[b8 + 5]),
-                               pack_bf16x2(sc[b8 + 6], sc[b8 + 7])});
-    }
-#pragma unroll
-    for (int n = 0; n < C::NE; ++n)
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        const int ro = mo + s2 * 16 * T::ROW_BYTES;
-        oacc[n] = mfma32x32x16(tr_operand(Ks, v_off[n][0] + ro, v_off[n][1] + ro), pf[s2], oacc[n]);
-      }
+        for (int s2 = 0; s2 < 2; ++s2) {
+          const int ro = mo + s2 * 16 * T::ROW_BYTES;
+          oacc[n] =
+              mfma32x32x16(tr_operand(Ks, v_off[n][0] + ro, v_off[n][1] + ro), pf[s2], oacc[n]);
+        }
     }
   };
   // One tile of rows and the next one's page numbers in flight over a tile's

@@ -41,14 +41,19 @@ inline SharedCut shared_cut(int b, int n_q, int n_k, int d, int max_len, int n_g
   // a group's rows in whole chunks; no group that shares has fewer than two sequences
   const long long sharing = n_groups < b / 2 ? n_groups : b / 2;
   // A tile's way through LDS is paid once for 64 or 128 rows; a workgroup leaves O of all of
-  // them (us: 128 rows of a kv head 21.7 with 64, 26.2 with 128; 512 rows 39.7, 35.5).
+  // them.  us with 64 and with 128, prompts of 16K, 8 heads on 2 of 128: 64 rows of a kv
+  // head 20.6, 20.7; 128 rows 21.7, 25.9; 192 rows 25.2, 24.9; 256 rows 26.4, 25.9; 512 rows 37.2,
+  // 33.1; four prompts of 8K and 256 rows each 35.6, 28.8, in 8 bits and 64 rows 23.3, 24.7.
   c.rows = b * rep > 192 * sharing ? 128 : 64;
   c.chunks = (int)((b * rep + sharing * (c.rows - 1)) / c.rows);
   if (sharing == 0) c.chunks = 0;
   const long long per_split = (long long)c.chunks * n_k;
-  // A workgroup of either kind per CU, which has room for two: twice as many for the
-  // prefix leave twice the partial results (32 sequences on one prompt of 16K tokens 21.7
-  // us, 31.8 with 512; 64 on one of 32K 35.5, 47.0).
+  // A workgroup of either kind per CU, which has room for two: more for the prefix leave
+  // more partial results, fewer leave CUs without one.  us with 128, 192, 256, 384: the 128
+  // rows above 23.8, 22.7, 21.7, 29.6; 256 rows 30.2, 27.4, 25.9, 35.0; 512 rows of one prompt of 32K 45.3,
+  // 37.3, 33.4, 42.0; four prompts of 8K and 64 rows each 33.5, 33.5, 25.5, 27.5.
+  // The cut goes by what the host knows, not by the prefixes' lengths, and is the same for
+  // all: one long prefix among many short ones is cut into few parts.
   long long splits = per_split == 0 ? 0 : (256 + per_split - 1) / per_split;
   const long long most = ((long long)max_len + 2 * kSharedTile - 1) / (2 * kSharedTile);
   if (splits > most) splits = most;

@@ -82,8 +82,16 @@ inline SpanCut span_cut(const SpanArgs &s) {
 
 // Row groups of the dQ pass: the causal backward's rule, but with spans 128 rows a
 // workgroup up to 96K query rows: documents make workgroups of very different
-// lengths, and twice as many of half the length even out better (42K rows, d = 80,
-// documents of 1200 tokens: 123 -> 115 us; 128K rows of documents of 2048: 419, 421).
+// lengths, and twice as many of half the length even out better; one document wants the
+// larger ones.  The host does not see which it is, and the sides do not cross at one
+// size.  us with 128 and 256 rows (8 heads on 2 of 128, 7 on 1 at 79K; two draws of documents):
+//   rows   one document  of S / 8             of 1200              of 300
+//   42K    247, 239      165 164, 190 190     200 201, 208 222     123 125, 118 136
+//   64K    487, 468      235 232, 323 314     268 267, 372 369     126 126, 195 200
+//   79K    446, 421      289 293, 358 361     376 375, 383 387     199 200, 282 282
+//   96K    985, 985      263 264, 432 417     226 243, 331 343     150 172, 170 209
+//   128K   1686, 1652    391 388, 683 669     278 287, 406 428     196 185, 214 223
+//   192K   3708, 3753    748 928, 1378 1477   459 560, 618 807     264 311, 308 356
 inline int span_row_groups(const SpanArgs &s) {
   const int R = dq_row_groups(span_shape(s, (size_t)-1));
   return R == 8 && s.spans && (long long)s.b * s.Hl * s.S <= 98304 ? 4 : R;

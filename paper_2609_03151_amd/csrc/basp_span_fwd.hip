@@ -813,7 +813,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void span_fwd_kernel(const S
 
 // The workgroup of a call, by its query rows W = b Hl S: few rows need small ones
 // to fill the GPU, and many let a K or V tile feed more products.  Three kinds, us on
-// MI355X (8 heads on 2 of 128; one document | documents of S / 8 tokens | of 300):
+// MI355X (8 heads on 2 of 128; one document | documents of some S / 8 tokens, one draw | of 300):
 //   64 rows, 8 waves; 128 rows, 8 waves, pipelined; 128 rows, 4 waves, pipelined, two a CU
 //   W = 16K, S = 2048  29, 34, -    15, 18, -     15, 19, -
 //   32K, 4096          58, 61, 73   31, 29, 34    25, 22, 24
@@ -824,8 +824,15 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void span_fwd_kernel(const S
 //   128K, 16384        717, 521, 483  393, 306, 354  91, 70, 55
 //   512K, 65536 on 1   9984, 7830, 7413  1685, 1286, 1253  364, 257, 178
 // (256 rows and 8 waves, one workgroup a CU, 493, 300 and 66 at W = 128K, lost to the
-// last kind wherever the others did.)  Caps past kSpanFixedCap take the tiles that follow the
-// running maximum, not pipelined, from 32K rows on in 128-row workgroups.
+// last kind wherever the others did.)  Documents of thousands of tokens end with a few long
+// workgroups, which 8 waves do in half the time; which kind wins past 72K rows is then a
+// matter of the draw, us of three each, 8 waves and 4:
+//   W = 96K   of 1000  77 75, 90 98, 103 135     of 4096  178 212, 314 300, 118 107
+//   128K      of 1000  102 93, 107 109, 121 142  of 2048  126 140, 213 235, 130 118
+//   256K      of 1000  184 155, 226 203, 218 210  of 4096  379 391, 725 720, 407 376
+// Caps past kSpanFixedCap take the tiles that follow the running maximum, not pipelined, past
+// the first line in 128-row workgroups (one document of 32K tokens, 4 heads on 1: 1494 us, 1137
+// with a cap of 50; 16K tokens of documents of 2K, 8 on 2: 184, 167).
 enum class Kind { k64, k128, k128Narrow, k128Running };
 Kind kind_of(const SpanArgs &a) {
   const long long rows = (long long)a.b * a.Hl * a.S;
