@@ -607,7 +607,8 @@ int basp_attn_decode_shared(const void *q, const void *k_pages, const void *v_pa
  * rows all of whose keys are far away, |slope * distance| past 2^12, see that in P.  Values of up to 2^96 in magnitude do not overflow on the way to O, whatever the scores.
  * A value, key, query or gradient outside every span that it would meet does not
  * count, infinities and NaN too; inside one they make what they reach NaN: a value
- * its element of O, a score of plus infinity or NaN its row.
+ * its element of O, a score of plus infinity or NaN its row (with a cap an infinite score
+ * is the cap, of its sign).
  * Conditions: d 64, 80, 96 or 128; scale 2^-40 to 2^40; 16-byte aligned q, k, v, o,
  * d_o and gradients, strides multiples of 8; spans 8, lse and slopes 4.  Errors: NULL, SHAPE
  * (negative size, n_q % n_k != 0, a row stride below n*d), UNSUPPORTED (d, scale, cap;

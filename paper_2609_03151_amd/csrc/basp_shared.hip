@@ -7,8 +7,8 @@
 // pairs, many enough for the matrix cores' 32-row tiles.  Bound by HBM for the keys and
 // values, each read once, up to some 200 rows a kv head, by the matrix cores (and
 // with a cap the vector units) past that.  On MI355X, 32 sequences on one prompt of 16K
-// tokens, 8 heads on 2 of 128: 21.5 us, 8 of them dependent loads, 11 tiles, 5 the join
-// (its bytes alone take 6.7); read sequence by sequence the prompt would be 0.5 GB.
+// tokens, 8 heads on 2 of 128: 21.7 us, 8 of them dependent loads, 11 tiles, 5 the join
+// (its bytes alone take 5.5); read sequence by sequence the prompt would be 0.5 GB.
 //
 //   shared_plan   which sequences share, and where their rows go (past 512 sequences or 128
 //                 groups; else each workgroup of the next kernel finds out by itself)

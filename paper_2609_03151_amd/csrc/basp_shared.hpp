@@ -50,8 +50,8 @@ inline SharedCut shared_cut(int b, int n_q, int n_k, int d, int max_len, int n_g
   const long long per_split = (long long)c.chunks * n_k;
   // A workgroup of either kind per CU, which has room for two: more for the prefix leave
   // more partial results, fewer leave CUs without one.  us with 128, 192, 256, 384: the 128
-  // rows above 23.8, 22.7, 21.7, 29.6; 256 rows 30.2, 27.4, 25.9, 35.0; 512 rows of one prompt of 32K 45.3,
-  // 37.3, 33.4, 42.0; four prompts of 8K and 64 rows each 33.5, 33.5, 25.5, 27.5.
+  // rows above 23.8, 22.7, 21.7, 29.6; 256 rows 30.2, 27.4, 25.9, 35.0; 512 rows on one prompt
+  // of 32K 45.3, 37.3, 33.4, 42.0; four prompts of 8K and 64 rows each 33.5, 33.5, 25.5, 27.5.
   // The cut goes by what the host knows, not by the prefixes' lengths, and is the same for
   // all: one long prefix among many short ones is cut into few parts.
   long long splits = per_split == 0 ? 0 : (256 + per_split - 1) / per_split;

@@ -5,7 +5,7 @@
 // (4 d operations a seen pair) and, with a cap, by the vector units, which form
 // three exponentials or reciprocals a score instead of one.  On MI355X: one document of
 // 32K tokens with a cap, 4 heads on 1 of 128, 1155 us, 950 TFLOP/s (a large matrix product
-// reaches 1250); 16K tokens in documents of some 2K with a bias, 8 heads on 2, 173 us, 514
+// reaches 1600); 16K tokens in documents of some 2K with a bias, 8 heads on 2, 172 us, 517
 // TFLOP/s, the ends of uneven workgroups; no rule, 16K, 8 heads on 2, 488 us.
 //
 // gfx950 mapping, as the causal forward's: a workgroup owns 32 R query rows of one
