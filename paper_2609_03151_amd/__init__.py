@@ -812,7 +812,8 @@ def attn_decode_shared(q, k_pages, v_pages, block_table, lens, groups=None, pref
     ``cap``, less slopes[h] times the key's distance where there are ``slopes`` (fp32 [n_q]).
     ``groups`` int32 [n_groups + 1], ascending: group g is sequences groups[g] .. groups[g+1] - 1,
     those of which that reach prefix_lens[g] (int32 [n_groups]) have their first prefix_lens[g]
-    tokens in common, in the same pages.  Both None: nothing is shared."""
+    tokens in common, in the same pages.  Both None: nothing is shared.  Name prefixes of like
+    length: a long one among many short ones is read by few workgroups."""
     dev = _device(q, "q", 3)
     shape = q.shape
     b, n_q, d = shape
